@@ -385,6 +385,184 @@ moe_status_t moe_select_tree(int n, const int32_t *parent, const double *P, int 
                              double lambda, int mode, int32_t *selected, int32_t *marginal_cost,
                              int32_t *n_selected);
 
+/*
+ * The rest of a layer's verification step: the norm that makes x from the
+ * residual stream, and the attention of the draft tokens.  In the verification
+ * pass the T selected tokens of a draft tree go through the layer at once
+ * ("a tree attention mask", Section 5.1): each attends to everything cached of
+ * its sequence and, of the drafts, to its own ancestors and itself.  The
+ * drafts' keys and values are therefore passed beside the cache, and only the
+ * tokens that the verification accepts are appended to it.
+ */
+
+/* 8-bit output of moe_add_rmsnorm: OCP e4m3fn codes q [T][d], and scales.
+ * The value of a code is e4m3fn(q) * scale, scale being that of its group. */
+typedef enum {
+    MOE_Q_NONE = 0,
+    MOE_Q_FP8_GROUP = 1, /* fp32 scales [T][ceil(d/128)], one per 128 consecutive elements (the last
+                            group may be shorter)                                                     */
+    MOE_Q_MXFP8 = 2,     /* OCP MX: e8m0 codes u8 [T][d/32], by the rule of moe_actq_t                */
+    MOE_Q_FP8_ROW = 3    /* fp32 scales [T][1], one per row                                           */
+} moe_qfmt_t;
+
+/*
+ * Residual addition and root-mean-square norm.  Per row, in fp32:
+ *   v = x + residual (x alone if residual is NULL);  sum = bf16(v);
+ *   u = v / sqrt(mean(v^2) + eps) * weight;  y = bf16(u);
+ *   q = the 8-bit form of u: fp32 scale = max(max |u|, 2^-100) / 448 over the
+ *   group, code = e4m3fn(u / scale), magnitudes from 448 up saturating; or MX.
+ * v and u are not rounded on the way: y and q come from the unrounded sum.
+ *   x, residual, sum, y [T][d] bf16, weight [d] bf16; q, scales by qfmt.
+ *   sum, y or q may be NULL (q and scales exactly when qfmt is MOE_Q_NONE),
+ *   not all three.  sum may be the buffer of x or of residual, and y that of
+ *   x; other overlaps are not allowed.
+ * Limits: T >= 1, d % 32 == 0, d <= 16384, finite eps >= 0; all pointers 16-byte
+ * aligned (scales: 4).  One kernel, deterministic.
+ */
+moe_status_t moe_add_rmsnorm(const void *x, const void *residual, const void *weight, int T, int d, float eps,
+                             int qfmt, void *sum, void *y, void *q, void *scales, void *stream);
+
+/* Draft tokens of one call: N tokens of B sequences, sequence b having tokens
+ * token_offsets[b] .. token_offsets[b+1] - 1 (token_offsets[0] = 0,
+ * token_offsets[B] = N, none decreasing; at most 64 tokens a sequence; a
+ * sequence may have none).  Bit j of mask[t] set: token t attends to the j-th
+ * token of its sequence, itself included (bits past the sequence's tokens are
+ * ignored).  mask NULL: every token attends to itself and those before it.
+ * What a token does not attend to has no effect on it, infinities and NaN
+ * among it.  A token that attends to nothing at all gets zeros, and -inf as
+ * its log-sum.  Device pointers. */
+typedef struct {
+    int N, B;
+    const int32_t *token_offsets; /* [B+1] */
+    const uint64_t *mask;         /* [N] or NULL */
+} moe_drafts_t;
+
+/* Latent cache: one row of r + p bf16 a token (latent part, then rotary part,
+ * shared by all heads) in pages of `page` tokens.  Token i of sequence b is
+ * row i % page of page block_table[b][i / page]; cache_len[b] tokens are
+ * cached (0 <= cache_len[b] <= max_blocks * page).  Requirements: r = 512,
+ * p = 64 (else MOE_ERR_UNSUPPORTED); page 16, 32, 64 or 128; n_pages >= 1;
+ * pages 16-byte aligned. */
+typedef struct {
+    int r, p;
+    int n_pages, page, max_blocks;
+    const void *pages;          /* [n_pages][page][r+p] bf16 */
+    const int32_t *block_table; /* [B][max_blocks], entries in [0, n_pages) */
+    const int32_t *cache_len;   /* [B] */
+} moe_latent_cache_t;
+
+/*
+ * Latent attention, absorbed form: keys and values are the latent rows
+ * themselves, and the key and value expansions are folded into the products
+ * before and after the call.  For token t of sequence b and head h, over the
+ * cached rows of b and the drafts that t attends to:
+ *   s_j = scale * q[t][h] . c_j            (r + p elements)
+ *   o[t][h] = sum_j softmax(s)_j c_j[0:r],   lse[t][h] = log sum_j exp(s_j)
+ *   q [N][H][r+p], kv_new [N][r+p] (the drafts' rows), o [N][H][r]: bf16;
+ *   lse [N][H] fp32 or NULL.
+ *   workspace: device scratch of moe_latent_attn_workspace_size bytes, 256-byte
+ *   aligned; its contents on entry do not matter.
+ * Arithmetic: bf16 products summed in fp32, softmax in fp32, the weights
+ * exp(s - max) rounded to bf16 for the value product, fp32 sums, one rounding
+ * to bf16 at the end.  Deterministic.
+ * Limits: 1 <= H <= 1024, 1 <= B <= 1024, N >= 1, N * H <= 2^24, scale finite.
+ */
+moe_status_t moe_latent_attn_workspace_size(const moe_latent_cache_t *cache, int N, int B, int H, size_t *bytes);
+moe_status_t moe_latent_attn(const moe_latent_cache_t *cache, const moe_drafts_t *drafts, const void *q,
+                             const void *kv_new, int H, float scale, void *o, float *lse, void *workspace,
+                             size_t workspace_bytes, void *stream);
+
+/*
+ * Latent attention, expanded form, for prompts: every head has its own keys
+ * and values, expanded from the latent rows by the caller's products, beside
+ * the shared rotary part.  Sequence b has queries q_offsets[b] ..
+ * q_offsets[b+1] - 1 and keys kv_offsets[b] .. kv_offsets[b+1] - 1 (both from 0
+ * to N and M, none decreasing); its i-th query of n attends to the first
+ * i + 1 + (m - n) of its m keys (the queries are the last n of m tokens).  A
+ * query that attends to nothing gets zeros, and -inf as its log-sum; keys past
+ * a query's have no effect on it, infinities and NaN among them.
+ *   s_j = scale * (q[t][h][0:dn] . k_j[h] + q[t][h][dn:] . k_rope_j)
+ *   o[t][h] = sum_j softmax(s)_j v_j[h],  lse[t][h] = log sum_j exp(s_j)
+ *   q [N][H][dn+p], k_rope [M][p], o [N][H][dv]: bf16; lse [N][H] fp32 or NULL.
+ *   k: head h of key j is the dn elements from k + j * k_stride + h * k_head
+ *   on (strides in elements), v the same with dv elements; so both may be
+ *   parts of one expansion's output.
+ *   max_tokens: at least the most queries of a sequence.
+ * Arithmetic as for moe_latent_attn.  No workspace.
+ * Limits: dn = dv = 128, p = 64 (else MOE_ERR_UNSUPPORTED); 1 <= H <= 1024,
+ * 1 <= B <= 1024, N, M >= 1, scale finite; strides multiples of 8, 16-byte
+ * aligned pointers.
+ */
+typedef struct {
+    int N, M, B, H, dn, p, dv, max_tokens;
+    const int32_t *q_offsets, *kv_offsets; /* [B+1] each */
+    const void *q, *k, *k_rope, *v;
+    int64_t k_stride, k_head, v_stride, v_head;
+    float scale;
+} moe_prompt_t;
+
+moe_status_t moe_latent_prompt(const moe_prompt_t *a, void *o, float *lse, void *stream);
+
+/* Key/value cache of grouped-query attention in 8 bits: OCP e4m3fn codes in
+ * pages of `page` tokens, with one fp32 scale for the keys and one for the
+ * values of each page and head.  Paging as in moe_latent_cache_t.  A page
+ * holds, per head, its keys token by token and its values element by element
+ * (each element's tokens side by side: the operand order of the value
+ * product).  Requirements: D 64 or 128 (else MOE_ERR_UNSUPPORTED); page 16, 32,
+ * 64 or 128; 1 <= Hkv <= 256; k and v 16-byte aligned. */
+typedef struct {
+    int Hkv, D;
+    int n_pages, page, max_blocks;
+    uint8_t *k;                 /* [n_pages][Hkv][page][D] */
+    uint8_t *v;                 /* [n_pages][Hkv][D][page] */
+    float *k_scale, *v_scale;   /* [n_pages][Hkv] */
+    const int32_t *block_table; /* [B][max_blocks], entries in [0, n_pages) */
+    const int32_t *cache_len;   /* [B] */
+} moe_cache_t;
+
+/*
+ * Append to the 8-bit cache.  Sequence b's new tokens are entries
+ * token_offsets[b] .. token_offsets[b+1] - 1 of rows [N] (rows NULL: the
+ * entries themselves), each the index of a row of k_new, v_new [n_rows][Hkv][D]
+ * bf16; they go to positions cache_len[b] on.  (After a verification: rows of
+ * the accepted path.)  Per touched page and head, for keys and values alike:
+ *   need = the smallest power of two >= max |new value| / 448, at least 2^-126
+ *          (infinities and NaN left out of the maximum);
+ *   scale = need if the page begins with a new token, else max(scale, need);
+ *   where the scale grows, the codes of the page's other slots are coded
+ *   again: e4m3fn(value of the code / new scale), ties to even;
+ *   new codes are e4m3fn(value / scale), infinities saturating to 448.
+ * So a page's values stay exact multiples of their codes' grid however often
+ * its scale grows, up to the smallest codes.  cache_len is not changed.  A
+ * position past max_blocks * page is dropped.  No two sequences may share a
+ * page that is written.
+ * max_tokens: at least the most new tokens of a sequence.
+ * Limits: N, n_rows, B >= 1, B <= 1024; k_new, v_new 16-byte aligned.  One
+ * kernel, deterministic.
+ */
+moe_status_t moe_cache_append(const moe_cache_t *cache, const void *k_new, const void *v_new, int n_rows,
+                              const int32_t *rows, int N, int B, const int32_t *token_offsets, int max_tokens,
+                              void *stream);
+
+/*
+ * Grouped-query attention of draft tokens over the 8-bit cache and the drafts
+ * themselves.  Query head h uses key/value head h / (H / Hkv).
+ *   s_j = scale * q[t][h] . k_j,  o[t][h] = sum_j softmax(s)_j v_j,
+ *   lse[t][h] = log sum_j exp(s_j), over the cached tokens (code value times
+ *   its page's scale) and the drafts that t attends to (k_new, v_new).
+ *   q, o [N][H][D], k_new, v_new [N][Hkv][D]: bf16; lse [N][H] fp32 or NULL.
+ *   workspace: device scratch of moe_cache_attn_workspace_size bytes, 256-byte
+ *   aligned; its contents on entry do not matter.
+ * Arithmetic: codes are exact in bf16, scales multiply the fp32 scores and the
+ * fp32 softmax weights; otherwise as for moe_latent_attn.  Deterministic.
+ * Limits: H % Hkv == 0, H <= 1024, 1 <= B <= 1024, N >= 1, N * H <= 2^24,
+ * scale finite.
+ */
+moe_status_t moe_cache_attn_workspace_size(const moe_cache_t *cache, int N, int B, int H, size_t *bytes);
+moe_status_t moe_cache_attn(const moe_cache_t *cache, const moe_drafts_t *drafts, const void *q, const void *k_new,
+                            const void *v_new, int H, float scale, void *o, float *lse, void *workspace,
+                            size_t workspace_bytes, void *stream);
+
 /* Static description of a status code. */
 const char *moe_status_string(moe_status_t status);
 

@@ -18,6 +18,14 @@ the library has not been built, importing the functions that need it raises
     moe_select_tree(parent, P, pred, E, budget) -> (selected, marginal_cost)
     moe_route_union(logits, k, score)           -> Routing   (route + union in one call)
     moe_verify_step(x, logits, weights, k, score) = moe_route_union + moe_verify_layer
+
+and the rest of a layer's verification step:
+
+    moe_add_rmsnorm(x, weight, eps, residual, qfmt) -> (sum, y, q, scales)
+    moe_latent_attn(q, kv_new, token_offsets, pages, block_table, cache_len, r, scale, mask) -> (o, lse)
+    moe_latent_prompt(q, k, k_rope, v, q_offsets, kv_offsets, scale)   -> (o, lse)
+    moe_cache_append(k_new, v_new, token_offsets, k, v, k_scale, v_scale, block_table, cache_len)
+    moe_cache_attn(q, k_new, v_new, token_offsets, k, v, k_scale, v_scale, block_table, cache_len, scale, mask) -> (o, lse)
 """
 from __future__ import annotations
 
@@ -37,10 +45,13 @@ MOE_W_BF16, MOE_W_FP8_E4M3_B128, MOE_W_MXFP4 = 0, 1, 2
 MOE_SEL_COST_RATIO, MOE_SEL_CONFIDENCE, MOE_SEL_GLOBAL_COST, MOE_SEL_COST_DIFF = 0, 1, 2, 3
 MOE_ACT_SWIGLU, MOE_ACT_SWIGLU_OAI = 0, 1
 MOE_ACTQ_BF16, MOE_ACTQ_MXFP8 = 0, 1
+MOE_Q_NONE, MOE_Q_FP8_GROUP, MOE_Q_MXFP8, MOE_Q_FP8_ROW = 0, 1, 2, 3
 
 EXPORTED = ("moe_route_topk", "moe_route_union", "moe_route_topk_grouped", "moe_router_workspace_size", "moe_route_topk_hidden", "moe_expert_union", "moe_verify_workspace_size", "moe_verify_layer",
             "moe_verify_layer_timed", "moe_packed_size", "moe_pack_weights", "moe_pack_gate_up", "moe_pack_down",
-            "moe_select_tree", "moe_status_string", "moe_last_error", "moe_verify_layer_noalloc")
+            "moe_select_tree", "moe_status_string", "moe_last_error", "moe_verify_layer_noalloc",
+            "moe_add_rmsnorm", "moe_latent_attn_workspace_size", "moe_latent_attn", "moe_latent_prompt",
+            "moe_cache_append", "moe_cache_attn_workspace_size", "moe_cache_attn")
 
 
 class MoeError(RuntimeError):
@@ -61,6 +72,26 @@ class moe_weights_t(C.Structure):
 class moe_routing_t(C.Structure):
     _fields_ = [("T", C.c_int), ("k", C.c_int), ("E", C.c_int)] + [
         (n, C.c_void_p) for n in ("topk_idx", "topk_w", "counts", "union_ids", "n_unique", "offsets", "perm")]
+
+
+class moe_drafts_t(C.Structure):
+    _fields_ = [("N", C.c_int), ("B", C.c_int), ("token_offsets", C.c_void_p), ("mask", C.c_void_p)]
+
+
+class moe_latent_cache_t(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("r", "p", "n_pages", "page", "max_blocks")] + [
+        (n, C.c_void_p) for n in ("pages", "block_table", "cache_len")]
+
+
+class moe_prompt_t(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("N", "M", "B", "H", "dn", "p", "dv", "max_tokens")] + [
+        (n, C.c_void_p) for n in ("q_offsets", "kv_offsets", "q", "k", "k_rope", "v")] + [
+        (n, C.c_int64) for n in ("k_stride", "k_head", "v_stride", "v_head")] + [("scale", C.c_float)]
+
+
+class moe_cache_t(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("Hkv", "D", "n_pages", "page", "max_blocks")] + [
+        (n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "block_table", "cache_len")]
 
 
 _lock = threading.Lock()
@@ -94,12 +125,23 @@ def lib() -> C.CDLL:
             L.moe_pack_gate_up.argtypes = [i, i, i, i, p, p, p, p, p, p, p, p]
             L.moe_pack_down.argtypes = [i, i, i, i, p, p, p, p, p]
             L.moe_select_tree.argtypes = [i, p, p, i, i, p, i, p, i, C.c_double, C.c_double, i, p, p, p]
+            st = C.POINTER
+            L.moe_add_rmsnorm.argtypes = [p, p, p, i, i, C.c_float, i, p, p, p, p, p]
+            L.moe_latent_attn_workspace_size.argtypes = [st(moe_latent_cache_t), i, i, i, st(C.c_size_t)]
+            L.moe_latent_attn.argtypes = [st(moe_latent_cache_t), st(moe_drafts_t), p, p, i, C.c_float, p, p, p,
+                                          C.c_size_t, p]
+            L.moe_latent_prompt.argtypes = [st(moe_prompt_t), p, p, p]
+            L.moe_cache_append.argtypes = [st(moe_cache_t), p, p, i, p, i, i, p, i, p]
+            L.moe_cache_attn_workspace_size.argtypes = [st(moe_cache_t), i, i, i, st(C.c_size_t)]
+            L.moe_cache_attn.argtypes = [st(moe_cache_t), st(moe_drafts_t), p, p, p, i, C.c_float, p, p, p, C.c_size_t, p]
             L.moe_status_string.argtypes = [i]
             L.moe_status_string.restype = C.c_char_p
             L.moe_last_error.restype = C.c_char_p
             for f in ("moe_route_topk", "moe_route_union", "moe_route_topk_grouped", "moe_router_workspace_size", "moe_route_topk_hidden", "moe_expert_union", "moe_verify_workspace_size", "moe_verify_layer",
                       "moe_verify_layer_noalloc", "moe_verify_layer_timed", "moe_packed_size", "moe_pack_weights", "moe_pack_gate_up",
-                      "moe_pack_down", "moe_select_tree"):
+                      "moe_pack_down", "moe_select_tree", "moe_add_rmsnorm", "moe_latent_attn_workspace_size",
+                      "moe_latent_attn", "moe_latent_prompt", "moe_cache_append", "moe_cache_attn_workspace_size",
+                      "moe_cache_attn"):
                 getattr(L, f).restype = i
             _lib = L
     return _lib
@@ -465,6 +507,202 @@ def moe_verify_step(x, logits, weights: dict, k: int, score: int, workspace=None
     idx, w = moe_route_topk(logits, k, score)
     r = routing_for(idx, w, logits.shape[1])
     return moe_verify_layer(x, weights, r, y=y, workspace=workspace), r
+
+
+# --------------------------------------------------------------------------- norm
+
+def moe_add_rmsnorm(x, weight, eps: float, residual=None, qfmt: int = MOE_Q_NONE, want_y: bool = True, want_sum: bool = True,
+                    sum=None, y=None, q=None, scales=None):
+    """Residual addition and RMS norm of bf16 rows x [T, d] -> (sum, y, q, scales).
+
+    sum = bf16(x + residual), y = bf16 norm, q (e4m3fn codes, uint8 [T, d]) and scales the norm in 8 bits by `qfmt`;
+    what is not wanted is None.  Outputs given are written in place (sum may be x or residual, y may be x)."""
+    torch = _torch()
+    T, d = x.shape
+    bf16, u8 = torch.bfloat16, torch.uint8
+    if x.dtype != bf16 or weight.dtype != bf16 or weight.numel() != d:
+        raise ValueError("x [T, d] and weight [d] must be bfloat16")
+    if residual is not None and (residual.dtype != bf16 or residual.shape != x.shape):
+        raise ValueError("residual must be bfloat16 [T, d]")
+    for t, what in ((sum, "sum"), (y, "y")):
+        if t is not None and (t.dtype != bf16 or t.shape != x.shape):
+            raise ValueError(f"{what} must be bfloat16 [T, d]")
+    if sum is None and want_sum:
+        sum = torch.empty_like(x)
+    if y is None and want_y:
+        y = torch.empty_like(x)
+    if qfmt != MOE_Q_NONE:
+        if qfmt == MOE_Q_MXFP8:
+            groups, stype = d // 32, u8
+        else:
+            groups, stype = (1 if qfmt == MOE_Q_FP8_ROW else (d + 127) // 128), torch.float32
+        if q is None:
+            q = torch.empty(T, d, dtype=u8, device=x.device)
+        if scales is None:
+            scales = torch.empty(T, groups, dtype=stype, device=x.device)
+        if q.dtype != u8 or q.shape != x.shape or scales.dtype != stype or tuple(scales.shape) != (T, groups):
+            raise ValueError("q must be uint8 [T, d] and scales of the format's type and shape")
+    _check("moe_add_rmsnorm", lib().moe_add_rmsnorm(
+        _dev_ptr(x, "x"), _dev_ptr(residual, "residual"), _dev_ptr(weight, "weight"), T, d, eps, qfmt,
+        _dev_ptr(sum, "sum"), _dev_ptr(y, "y"), _dev_ptr(q, "q"), _dev_ptr(scales, "scales"), _stream(x)))
+    return sum, y, q, scales
+
+
+# --------------------------------------------------------------------------- attention
+
+def _int32_ptr(t, what: str, *shape) -> int:
+    if t.dtype != _torch().int32 or tuple(t.shape) != shape:
+        raise ValueError(f"{what} must be int32 {list(shape)}")
+    return _dev_ptr(t, what)
+
+
+def _bf16_ptr(t, what: str, *shape) -> int:
+    if t.dtype != _torch().bfloat16 or tuple(t.shape) != shape:
+        raise ValueError(f"{what} must be bfloat16 {list(shape)}")
+    return _dev_ptr(t, what)
+
+
+def _drafts(N: int, token_offsets, mask) -> moe_drafts_t:
+    """moe_drafts_t of N tokens; mask: int64 (or uint64) [N], its bit patterns, or None."""
+    B = token_offsets.shape[0] - 1
+    if mask is not None and (mask.element_size() != 8 or mask.is_floating_point() or tuple(mask.shape) != (N,)):
+        raise ValueError("mask must be int64 or uint64 [N]")
+    return moe_drafts_t(N, B, _int32_ptr(token_offsets, "token_offsets", B + 1), _dev_ptr(mask, "mask"))
+
+
+def _attn_outputs(q, width: int, o, lse):
+    torch = _torch()
+    N, H = q.shape[0], q.shape[1]
+    if o is None:
+        o = torch.empty(N, H, width, dtype=torch.bfloat16, device=q.device)
+    if lse is None:
+        lse = torch.empty(N, H, dtype=torch.float32, device=q.device)
+    if lse.dtype != torch.float32 or tuple(lse.shape) != (N, H):
+        raise ValueError("lse must be float32 [N, H]")
+    return o, lse, _bf16_ptr(o, "o", N, H, width), _dev_ptr(lse, "lse")
+
+
+def _scratch(workspace, size_fn, name: str, cache, N: int, B: int, H: int, device):
+    if workspace is None:
+        n = C.c_size_t()
+        _check(name, size_fn(C.byref(cache), N, B, H, C.byref(n)))
+        workspace = _torch().empty(n.value, dtype=_torch().uint8, device=device)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def _latent_cache(pages, block_table, cache_len, B: int, r: int) -> moe_latent_cache_t:
+    n_pages, page, width = pages.shape
+    blocks = block_table.shape[1]
+    return moe_latent_cache_t(r, width - r, n_pages, page, blocks, _bf16_ptr(pages, "pages", n_pages, page, width),
+                              _int32_ptr(block_table, "block_table", B, blocks), _int32_ptr(cache_len, "cache_len", B))
+
+
+def moe_latent_attn_workspace_size(pages, block_table, cache_len, r: int, N: int, H: int) -> int:
+    B, n = block_table.shape[0], C.c_size_t()
+    c = _latent_cache(pages, block_table, cache_len, B, r)
+    _check("moe_latent_attn_workspace_size", lib().moe_latent_attn_workspace_size(C.byref(c), N, B, H, C.byref(n)))
+    return n.value
+
+
+def moe_latent_attn(q, kv_new, token_offsets, pages, block_table, cache_len, r: int, scale: float, mask=None, o=None,
+                    lse=None, workspace=None):
+    """Latent attention in the absorbed form of the draft tokens of B sequences -> (o [N, H, r] bf16, lse [N, H] fp32).
+
+    q [N, H, r + p] and kv_new [N, r + p] bf16; pages [n_pages, page, r + p] bf16, block_table [B, blocks] and
+    cache_len [B] int32; token_offsets [B + 1] int32; mask int64 [N], bit j for the j-th draft of the sequence (None:
+    causal).  All on the device; nothing is read back."""
+    N, H, width = q.shape
+    d = _drafts(N, token_offsets, mask)
+    c = _latent_cache(pages, block_table, cache_len, d.B, r)
+    o, lse, op, lp = _attn_outputs(q, r, o, lse)
+    L = lib()
+    workspace, nbytes = _scratch(workspace, L.moe_latent_attn_workspace_size, "moe_latent_attn_workspace_size", c, N, d.B, H,
+                                 q.device)
+    _check("moe_latent_attn", L.moe_latent_attn(
+        C.byref(c), C.byref(d), _bf16_ptr(q, "q", N, H, c.r + c.p), _bf16_ptr(kv_new, "kv_new", N, c.r + c.p), H, scale, op, lp,
+        _dev_ptr(workspace, "workspace"), nbytes, _stream(q)))
+    return o, lse
+
+
+def _strided_ptr(t, what: str, M: int, H: int) -> tuple[int, int, int, int]:
+    """Pointer, head width, token stride and head stride of bf16 [M, H, width] with contiguous heads."""
+    if not t.is_cuda or t.dtype != _torch().bfloat16 or t.dim() != 3 or t.shape[0] != M or t.shape[1] != H or t.stride(2) != 1:
+        raise ValueError(f"{what} must be bfloat16 [{M}, {H}, width] on the device, contiguous along its last axis")
+    return t.data_ptr(), t.shape[2], t.stride(0), t.stride(1)
+
+
+def moe_latent_prompt(q, k, k_rope, v, q_offsets, kv_offsets, scale: float, max_tokens: int | None = None, o=None, lse=None):
+    """Latent attention in the expanded form, causal, of the prompts of B sequences -> (o [N, H, dv] bf16, lse [N, H] fp32).
+
+    q [N, H, dn + p], k [M, H, dn], k_rope [M, p], v [M, H, dv] bf16 (k and v may be strided views of one expansion);
+    q_offsets, kv_offsets [B + 1] int32.  A sequence's queries are the last of its keys' tokens.  max_tokens: at least
+    the most queries of a sequence (None: N)."""
+    N, H, dq = q.shape
+    M, p = k_rope.shape
+    B = q_offsets.shape[0] - 1
+    kp, dn, ks, kh = _strided_ptr(k, "k", M, H)
+    vp, dv, vs, vh = _strided_ptr(v, "v", M, H)
+    o, lse, op, lp = _attn_outputs(q, dv, o, lse)
+    a = moe_prompt_t(N, M, B, H, dn, p, dv, N if max_tokens is None else max_tokens,
+                     _int32_ptr(q_offsets, "q_offsets", B + 1), _int32_ptr(kv_offsets, "kv_offsets", B + 1),
+                     _bf16_ptr(q, "q", N, H, dn + p), kp, _bf16_ptr(k_rope, "k_rope", M, p), vp, ks, kh, vs, vh, scale)
+    _check("moe_latent_prompt", lib().moe_latent_prompt(C.byref(a), op, lp, _stream(q)))
+    return o, lse
+
+
+def _cache(k, v, k_scale, v_scale, block_table, cache_len, B: int) -> moe_cache_t:
+    torch = _torch()
+    n_pages, heads, page, D = k.shape
+    for t, what, dtype, shape in ((k, "k", torch.uint8, (n_pages, heads, page, D)), (v, "v", torch.uint8, (n_pages, heads, D, page)),
+                                  (k_scale, "k_scale", torch.float32, (n_pages, heads)),
+                                  (v_scale, "v_scale", torch.float32, (n_pages, heads))):
+        if t.dtype != dtype or tuple(t.shape) != shape:
+            raise ValueError(f"{what} must be {dtype} {list(shape)}")
+    blocks = block_table.shape[1]
+    return moe_cache_t(heads, D, n_pages, page, blocks, _dev_ptr(k, "k"), _dev_ptr(v, "v"), _dev_ptr(k_scale, "k_scale"),
+                       _dev_ptr(v_scale, "v_scale"), _int32_ptr(block_table, "block_table", B, blocks),
+                       _int32_ptr(cache_len, "cache_len", B))
+
+
+def moe_cache_append(k_new, v_new, token_offsets, k, v, k_scale, v_scale, block_table, cache_len, rows=None,
+                     max_tokens: int | None = None) -> None:
+    """New tokens into the 8-bit cache, in place: sequence b's, entries token_offsets[b] .. token_offsets[b + 1] - 1 of
+    `rows` (indices into k_new, v_new [n_rows, Hkv, D] bf16; None: the entries themselves), at positions cache_len[b] on.
+    k [n_pages, Hkv, page, D] and v [n_pages, Hkv, D, page] uint8 codes, k_scale, v_scale [n_pages, Hkv] fp32.
+    cache_len is not changed.  max_tokens: at least the most new tokens of a sequence (None: all)."""
+    B = token_offsets.shape[0] - 1
+    c = _cache(k, v, k_scale, v_scale, block_table, cache_len, B)
+    n_rows = k_new.shape[0]
+    N = n_rows if rows is None else rows.shape[0]
+    _check("moe_cache_append", lib().moe_cache_append(
+        C.byref(c), _bf16_ptr(k_new, "k_new", n_rows, c.Hkv, c.D), _bf16_ptr(v_new, "v_new", n_rows, c.Hkv, c.D), n_rows,
+        None if rows is None else _int32_ptr(rows, "rows", N), N, B, _int32_ptr(token_offsets, "token_offsets", B + 1),
+        N if max_tokens is None else max_tokens, _stream(k_new)))
+
+
+def moe_cache_attn_workspace_size(k, v, k_scale, v_scale, block_table, cache_len, N: int, H: int) -> int:
+    B, n = block_table.shape[0], C.c_size_t()
+    c = _cache(k, v, k_scale, v_scale, block_table, cache_len, B)
+    _check("moe_cache_attn_workspace_size", lib().moe_cache_attn_workspace_size(C.byref(c), N, B, H, C.byref(n)))
+    return n.value
+
+
+def moe_cache_attn(q, k_new, v_new, token_offsets, k, v, k_scale, v_scale, block_table, cache_len, scale: float, mask=None,
+                   o=None, lse=None, workspace=None):
+    """Grouped-query attention of draft tokens over the 8-bit cache and each other -> (o [N, H, D] bf16, lse [N, H] fp32).
+
+    q [N, H, D], k_new, v_new [N, Hkv, D] bf16; the cache as for moe_cache_append; mask as for moe_latent_attn."""
+    N, H, D = q.shape
+    d = _drafts(N, token_offsets, mask)
+    c = _cache(k, v, k_scale, v_scale, block_table, cache_len, d.B)
+    o, lse, op, lp = _attn_outputs(q, D, o, lse)
+    L = lib()
+    workspace, nbytes = _scratch(workspace, L.moe_cache_attn_workspace_size, "moe_cache_attn_workspace_size", c, N, d.B, H,
+                                 q.device)
+    _check("moe_cache_attn", L.moe_cache_attn(
+        C.byref(c), C.byref(d), _bf16_ptr(q, "q", N, H, c.D), _bf16_ptr(k_new, "k_new", N, c.Hkv, c.D),
+        _bf16_ptr(v_new, "v_new", N, c.Hkv, c.D), H, scale, op, lp, _dev_ptr(workspace, "workspace"), nbytes, _stream(q)))
+    return o, lse
 
 
 # --------------------------------------------------------------------------- selector (host)
