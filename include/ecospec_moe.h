@@ -442,7 +442,7 @@ typedef struct {
  * row i % page of page block_table[b][i / page]; cache_len[b] tokens are
  * cached (0 <= cache_len[b] <= max_blocks * page).  Requirements: r = 512,
  * p = 64 (else MOE_ERR_UNSUPPORTED); page 16, 32, 64 or 128; n_pages >= 1;
- * pages 16-byte aligned. */
+ * max_blocks * page <= 2^30; pages 16-byte aligned. */
 typedef struct {
     int r, p;
     int n_pages, page, max_blocks;

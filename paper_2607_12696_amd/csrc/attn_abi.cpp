@@ -32,7 +32,7 @@ bool page_ok(int page) { return page == 16 || page == 32 || page == 64 || page =
 moe_status_t check_pages(int n_pages, int page, int max_blocks, const int32_t *table, const int32_t *len)
 {
     if (!table || !len || n_pages < 1 || max_blocks < 1 || !page_ok(page)) return MOE_ERR_INVALID_ARG;
-    if ((long)max_blocks * page > (1L << 31) - 1) return MOE_ERR_INVALID_ARG;  // positions are 32-bit
+    if ((long)max_blocks * page > 1L << 30) return MOE_ERR_INVALID_ARG;  // positions are 32-bit
     return MOE_OK;
 }
 

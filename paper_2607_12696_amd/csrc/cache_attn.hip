@@ -1,62 +1,392 @@
-// Grouped-query attention of draft tokens over the 8-bit cache.
-#include "row_attn.hpp"
+// Grouped-query attention of draft tokens over the 8-bit cache and over each other.
+//
+// Scores are computed transposed, S^T = K Q^T, so that a lane of the 32 x 32 x 16 product holds one query row and 16 of
+// its 32 scores; the other half of the wavefront has the rest.  Row m of the K operand is key pi(m) = 16 ((m >> 2) & 1) +
+// 4 (m >> 3) + (m & 3) of the tile, which puts keys 0..15 into the lower half's registers in order and keys 16..31 into
+// the upper's: they are the value product's operand P^T (its reduction index is the key) without any move between lanes,
+// and its other operand V^T takes 16 consecutive tokens of one element, 16 bytes of the cache as it lies.  So codes go
+// from memory to registers and through the conversion to bf16 into the matrix cores; LDS holds only the queries.
+//
+// Bound by HBM (2 bytes a cached token, head and element) up to some 64 rows a key/value head.  Four wavefronts take the
+// tiles of a workgroup's chunk in turn, each with its own running maximum and sums, joined at the end through LDS.
+#include "attn_plan.hpp"
 
 namespace ecospec {
 namespace {
 
-template <int D>
-struct CacheRow : PagedRow {
-    const CacheArgs &a;
-    int kvh;
-    float q[D / kWave];
-    __device__ CacheRow(const CacheArgs &args) : PagedRow(args), a(args)
-    {
-        kvh = h / (a.H / a.Hkv);
-        for (int i = 0; i < D / kWave; ++i)
-            q[i] = bf16_bits_to_f32(a.q[((long)t * a.H + h) * D + lane_id() * (D / kWave) + i]);
-    }
-    __device__ static float code(uint8_t c) { return __builtin_amdgcn_cvt_f32_fp8((int)c, 0); }
-    __device__ float dot(int j, int lane) const
-    {
-        float s = 0.f;
-        const int e0 = lane * (D / kWave);
-        if (j < len) {
-            const long head = page_of(j) * a.Hkv + kvh;
-            for (int i = 0; i < D / kWave; ++i) s = fmaf(q[i], code(a.k[(head * page + j % page) * D + e0 + i]), s);
-            return s * a.k_scale[head];
-        }
-        const uint16_t *k = a.k_new + ((long)(t0 + j - len) * a.Hkv + kvh) * D + e0;
-        for (int i = 0; i < D / kWave; ++i) s = fmaf(q[i], bf16_bits_to_f32(k[i]), s);
-        return s;
-    }
-    __device__ float value(int j, int e) const
-    {
-        if (j < len) {
-            const long head = page_of(j) * a.Hkv + kvh;
-            return code(a.v[(head * D + e) * page + j % page]) * a.v_scale[head];
-        }
-        return bf16_bits_to_f32(a.v_new[((long)(t0 + j - len) * a.Hkv + kvh) * D + e]);
-    }
-};
+constexpr int kKeys = 32;  // of a tile
+constexpr int kWaves = 4;
+// Powers of two by which a row's weights may outgrow its reference maximum before the sums are scaled down: they are
+// fp32, far from overflow, and the bf16 weights' rounding is relative.
+constexpr float kSlack = 8.f;
 
-template <int D>
-__global__ __launch_bounds__(256) void cache_row_kernel(CacheArgs a)
+// bf16 operand of eight codes.
+__device__ __forceinline__ bf16x8 decode(uint32_t w0, uint32_t w1)
 {
-    const CacheRow<D> r(a);
-    row_attention<D>(r, a.scale, a.o + (long)blockIdx.x * D, a.lse ? a.lse + blockIdx.x : nullptr);
+    u32x4 o;
+    o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.0f, false));
+    o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.0f, true));
+    o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.0f, false));
+    o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.0f, true));
+    return __builtin_bit_cast(bf16x8, o);
+}
+
+// RT: row tiles of 32 rows; D: head width.
+template <int D, int RT>
+__global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape shape, Parts parts)
+{
+    constexpr int kRows = 32 * RT, kSteps = D / 16, kDt = D / 32;
+    constexpr int kQ = RT * kSteps * 64 * 16;                // bytes of the queries, in operand order
+    constexpr int kP = kWaves * 32 * kKeys * 4;              // fp32 weights of a draft tile, for non-finite drafts
+    constexpr int kMerge = 2 * RT * kDt * 4096;              // two wavefronts' sums
+    constexpr int kPlan = 2 * kPlanB * 4;
+    constexpr int kLds0 = kQ + kP > kMerge ? kQ + kP : kMerge, kLds = kLds0 > kPlan ? kLds0 : kPlan;
+    __shared__ __attribute__((aligned(16))) char lds[kLds];
+    __shared__ float2 ml[kWaves][kRows];
+
+    const int G = a.H / a.Hkv;
+    Item it;
+    if (!plan_item(a, G, a.Hkv, shape, parts, reinterpret_cast<int *>(lds), it)) return;
+    __syncthreads();
+    const int kvh = it.group / it.row_tiles, row0 = it.group % it.row_tiles * kRows;
+    const int n_rows = it.n_tok * G;
+    const int lane = lane_id(), wave = threadIdx.x / kWave, col = lane % 32, half = lane / 32;
+
+    // Queries: step s, lane (row, half): elements 32 (s / 2) + 16 half + 8 (s % 2) .. + 7, as the codes' 16 bytes give.
+    u32x4 *q_lds = reinterpret_cast<u32x4 *>(lds);
+    for (int i = threadIdx.x; i < RT * kSteps * 64; i += 256) {
+        const int rt = i / (kSteps * 64), s = i / 64 % kSteps, l = i % 64;
+        const int r = row0 + rt * 32 + l % 32;
+        u32x4 v = {0, 0, 0, 0};
+        if (r < n_rows) {
+            const long at = (long)(it.t0 + r / G) * a.H + kvh * G + r % G;
+            v = *reinterpret_cast<const u32x4 *>(a.q + at * D + 32 * (s / 2) + 16 * (l / 32) + 8 * (s % 2));
+        }
+        q_lds[i] = v;
+    }
+    __syncthreads();
+
+    f32x16 o[RT][kDt];
+    float m[RT], l[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        m[rt] = -INFINITY;
+        l[rt] = 0.f;
+#pragma unroll
+        for (int d = 0; d < kDt; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[rt][d][i] = 0.f;
+    }
+
+    const int pi = (col >> 2 & 1) * 16 + (col >> 3) * 4 + (col & 3);
+    const int *table = a.block_table + (long)it.b * a.max_blocks;
+    const int lp = 31 - __builtin_clz(a.page);
+    const int cached = (it.len + kKeys - 1) / kKeys;  // tiles
+
+    // Running maximum, weights and sums of one row tile's scores s (in powers of two); returns the weights in s.
+    auto softmax = [&](int rt, float *s) {
+        float top = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+        top = halves_max(top);
+        if (__any(top > m[rt] + kSlack)) {
+            const float now = fmaxf(m[rt], top);
+            const float down = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[rt] - now);
+            m[rt] = now;
+            l[rt] *= down;
+#pragma unroll
+            for (int d = 0; d < kDt; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[rt][d][i] *= down;
+        }
+        const float base = m[rt] == -INFINITY ? 0.f : m[rt];
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            s[i] = __builtin_amdgcn_exp2f(s[i] - base);
+            sum += s[i];
+        }
+        l[rt] += sum;
+    };
+
+    // ---- cached tokens
+    const float scale2 = a.scale * kLog2e;
+    u32x4 kr[D / 32], vr[kDt];
+    const long stride = (long)a.page * D;  // of a head's page
+    int id0 = 0, id1 = 0;  // pages of the tile's lower and upper 16 keys
+    auto find = [&](int t) {
+        const int b0 = min(t * kKeys >> lp, a.max_blocks - 1), b1 = min((t * kKeys + 16) >> lp, a.max_blocks - 1);
+        id0 = min(max(table[b0], 0), a.n_pages - 1);
+        id1 = min(max(table[b1], 0), a.n_pages - 1);
+    };
+    auto load_k = [&](int t) {
+        const uint8_t *p = a.k + ((long)(pi & 16 ? id1 : id0) * a.Hkv + kvh) * stride + ((t * kKeys + pi) & (a.page - 1)) * D + 16 * half;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) kr[i] = *reinterpret_cast<const u32x4 *>(p + 32 * i);
+    };
+    auto load_v = [&](int t) {
+        const uint8_t *p = a.v + ((long)(half ? id1 : id0) * a.Hkv + kvh) * stride + ((t * kKeys + 16 * half) & (a.page - 1)) + (long)col * a.page;
+#pragma unroll
+        for (int d = 0; d < kDt; ++d) vr[d] = *reinterpret_cast<const u32x4 *>(p + (long)(32 * d) * a.page);
+    };
+    const int end = min(it.last, cached);
+    int t = it.first + wave;
+    if (t < end) {
+        find(t);
+        load_k(t);
+        load_v(t);
+    }
+    for (; t < end; t += kWaves) {
+        const float ks = a.k_scale[(long)(half ? id1 : id0) * a.Hkv + kvh] * scale2;
+        float vs = a.v_scale[(long)(half ? id1 : id0) * a.Hkv + kvh];
+        const int next = t + kWaves;
+        const int left = it.len - t * kKeys - 16 * half;  // of this half's 16 keys
+        f32x16 s[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[rt][i] = 0.f;
+#pragma unroll
+        for (int st = 0; st < kSteps; ++st) {
+            const bf16x8 k = decode(kr[st / 2][st % 2 * 2], kr[st / 2][st % 2 * 2 + 1]);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+                s[rt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, __builtin_bit_cast(bf16x8, q_lds[(rt * kSteps + st) * 64 + lane]), s[rt], 0, 0, 0);
+        }
+        const bool tail = (t + 1) * kKeys > it.len;
+        if (tail) {
+            // Past the cache's end lies whatever its pages held: no weight, and zeros for the values.
+            if (left <= 0) vs = 0.f;
+#pragma unroll
+            for (int d = 0; d < kDt; ++d)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int n = left - 4 * w;
+                    vr[d][w] &= n >= 4 ? ~0u : n <= 0 ? 0u : (1u << 8 * n) - 1;
+                }
+        }
+        if (next < end) {
+            find(next);
+            load_k(next);
+        }
+        bf16x8 p[RT][2];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float x[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                x[i] = s[rt][i] * ks;
+                if (tail && i >= left) x[i] = -INFINITY;
+            }
+            softmax(rt, x);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] *= vs;
+            p[rt][0] = pack_bf16x8(x);
+            p[rt][1] = pack_bf16x8(x + 8);
+        }
+#pragma unroll
+        for (int d = 0; d < kDt; ++d)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const bf16x8 v = decode(vr[d][2 * h], vr[d][2 * h + 1]);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) o[rt][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[rt][h], o[rt][d], 0, 0, 0);
+            }
+        if (next < end) load_v(next);
+    }
+
+    // ---- drafts
+    const int drafts = min(it.n_tok, kMaxDrafts);
+    for (; t < it.last; t += kWaves) {
+        const int j0 = (t - cached) * kKeys;
+        f32x16 s[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[rt][i] = 0.f;
+        const uint16_t *kp = a.k_new + ((long)(it.t0 + min(j0 + pi, drafts - 1)) * a.Hkv + kvh) * D + 16 * half;
+#pragma unroll
+        for (int st = 0; st < kSteps; ++st) {
+            const bf16x8 k = *reinterpret_cast<const bf16x8 *>(kp + 32 * (st / 2) + 8 * (st % 2));
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+                s[rt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, __builtin_bit_cast(bf16x8, q_lds[(rt * kSteps + st) * 64 + lane]), s[rt], 0, 0, 0);
+        }
+        // Values, element by element; not finite: one of this half's 16 drafts has an infinity or NaN.
+        const int mine = drafts - j0 - 16 * half;
+        const uint16_t *vp = a.v_new + ((long)(it.t0 + j0 + 16 * half) * a.Hkv + kvh) * D + col;
+        u32x4 vb[kDt][2];
+        bool odd = false;
+#pragma unroll
+        for (int d = 0; d < kDt; ++d)
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) {
+                const uint32_t lo = j < mine ? vp[(long)j * a.Hkv * D + 32 * d] : 0u;
+                const uint32_t hi = j + 1 < mine ? vp[(long)(j + 1) * a.Hkv * D + 32 * d] : 0u;
+                odd |= (lo & 0x7f80u) == 0x7f80u || (hi & 0x7f80u) == 0x7f80u;
+                vb[d][j / 8][j % 8 / 2] = lo | hi << 16;
+            }
+        const bool slow = __any(odd);
+        bf16x8 p[RT][2];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const int r = row0 + rt * 32 + col;
+            uint64_t see = 0;
+            if (r < n_rows) {
+                const int tok = r / G;
+                see = (a.mask ? a.mask[it.t0 + tok] : bits_below(tok + 1)) & bits_below(drafts);
+            }
+            const uint32_t bits = (uint32_t)(see >> j0) >> 16 * half;
+            float x[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = bits >> i & 1 ? s[rt][i] * scale2 : -INFINITY;
+            softmax(rt, x);
+            p[rt][0] = pack_bf16x8(x);
+            p[rt][1] = pack_bf16x8(x + 8);
+            if (slow) {
+                // A weight of zero must not meet an infinity: each row adds the drafts that it sees, one by one.
+                float *w = reinterpret_cast<float *>(lds + kQ) + (wave * 32 + col) * kKeys;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[16 * half + i] = x[i];
+                __builtin_amdgcn_wave_barrier();
+                const uint32_t all = (uint32_t)(see >> j0);
+                for (int j = 0; j < min(drafts - j0, kKeys); ++j) {
+                    const float f = *const_cast<volatile float *>(w + j);
+                    const uint16_t *v = a.v_new + ((long)(it.t0 + j0 + j) * a.Hkv + kvh) * D + 4 * half;
+                    if (all >> j & 1)
+#pragma unroll
+                        for (int d = 0; d < kDt; ++d)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[rt][d][i] = fmaf(f, bf16_bits_to_f32(v[32 * d + i / 4 * 8 + i % 4]), o[rt][d][i]);
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+        if (slow) continue;
+#pragma unroll
+        for (int d = 0; d < kDt; ++d)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+                    o[rt][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vb[d][h]), p[rt][h], o[rt][d], 0, 0, 0);
+    }
+
+    // ---- join the four wavefronts: 2 and 3 onto 0 and 1, then 1 onto 0
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        l[rt] = halves_sum(l[rt]);
+        if (half == 0) ml[wave][rt * 32 + col] = make_float2(m[rt], l[rt]);
+    }
+    __syncthreads();
+    float base[RT], total[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w][rt * 32 + col].x);
+        base[rt] = top == -INFINITY ? 0.f : top;
+        total[rt] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float2 v = ml[w][rt * 32 + col];
+            total[rt] = fmaf(v.y, __builtin_amdgcn_exp2f(v.x - base[rt]), total[rt]);
+        }
+        const float f = __builtin_amdgcn_exp2f(m[rt] - base[rt]);
+#pragma unroll
+        for (int d = 0; d < kDt; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[rt][d][i] *= f;
+    }
+    f32x4 *buf = reinterpret_cast<f32x4 *>(lds);
+#pragma unroll
+    for (int n = 2; n >= 1; n /= 2) {
+        if (wave >= n && wave < 2 * n)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int d = 0; d < kDt; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        buf[(((wave - n) * RT + rt) * kDt + d) * 256 + i * 64 + lane] =
+                            f32x4{o[rt][d][4 * i], o[rt][d][4 * i + 1], o[rt][d][4 * i + 2], o[rt][d][4 * i + 3]};
+        __syncthreads();
+        if (wave < n)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int d = 0; d < kDt; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const f32x4 v = buf[((wave * RT + rt) * kDt + d) * 256 + i * 64 + lane];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) o[rt][d][4 * i + j] += v[j];
+                    }
+        __syncthreads();
+    }
+    if (wave) return;
+
+    if (it.chunks > 1) {
+        f32x4 *out = reinterpret_cast<f32x4 *>(parts.o) + (long)it.slot * RT * kDt * 256;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+            for (int d = 0; d < kDt; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    out[(rt * kDt + d) * 256 + i * 64 + lane] =
+                        f32x4{o[rt][d][4 * i], o[rt][d][4 * i + 1], o[rt][d][4 * i + 2], o[rt][d][4 * i + 3]};
+            if (half == 0) parts.ml[(long)it.slot * kRows + rt * 32 + col] = make_float2(total[rt] == 0.f ? -INFINITY : base[rt], total[rt]);
+        }
+        return;
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int r = row0 + rt * 32 + col;
+        if (r >= n_rows) continue;
+        const long at = (long)(it.t0 + r / G) * a.H + kvh * G + r % G;
+        const float inv = total[rt] == 0.f ? 0.f : 1.f / total[rt];
+#pragma unroll
+        for (int d = 0; d < kDt; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<u32x2 *>(a.o + at * D + 32 * d + 8 * i + 4 * half) =
+                    u32x2{pack_bf16x2(o[rt][d][4 * i] * inv, o[rt][d][4 * i + 1] * inv),
+                          pack_bf16x2(o[rt][d][4 * i + 2] * inv, o[rt][d][4 * i + 3] * inv)};
+        if (a.lse && half == 0) a.lse[at] = total[rt] == 0.f ? -INFINITY : (base[rt] + __builtin_amdgcn_logf(total[rt])) / kLog2e;
+    }
+}
+
+// 64 rows a workgroup where the batch's average row group has more than 32.
+int row_tiles(int N, int B, int per_token) { return (long)N * per_token > 32L * B ? 2 : 1; }
+
+constexpr int kSlots = 2 * kCus;
+
+template <int D, int RT>
+hipError_t launch(const CacheArgs &a, void *workspace, hipStream_t stream)
+{
+    const int G = a.H / a.Hkv;
+    const long groups = group_bound(a.N, a.B, G, a.Hkv, 32 * RT);
+    Parts parts;
+    parts_at(workspace, groups, kSlots, 32 * RT, D, &parts);
+    cache_attn_kernel<D, RT><<<(unsigned)grid_bound(groups, kSlots), 256, 0, stream>>>(a, Shape{32 * RT, kKeys, kWaves, kSlots}, parts);
+    join_kernel<32 * RT, D><<<(unsigned)(groups * RT * (D / 32)), 256, 0, stream>>>(a, G, parts);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-size_t cache_workspace(int, int, int, int, int) { return 256; }
-
-hipError_t launch_cache_attn(const CacheArgs &a, void *, hipStream_t stream)
+size_t cache_workspace(int N, int B, int H, int Hkv, int D)
 {
-    if (a.D == 64)
-        cache_row_kernel<64><<<(unsigned)(a.N * a.H), 256, 0, stream>>>(a);
-    else
-        cache_row_kernel<128><<<(unsigned)(a.N * a.H), 256, 0, stream>>>(a);
-    return hipGetLastError();
+    const int rt = row_tiles(N, B, H / Hkv);
+    return parts_at(nullptr, group_bound(N, B, H / Hkv, Hkv, 32 * rt), kSlots, 32 * rt, D, nullptr);
+}
+
+hipError_t launch_cache_attn(const CacheArgs &a, void *workspace, hipStream_t stream)
+{
+    const bool two = row_tiles(a.N, a.B, a.H / a.Hkv) == 2;
+    if (a.D == 64) return two ? launch<64, 2>(a, workspace, stream) : launch<64, 1>(a, workspace, stream);
+    return two ? launch<128, 2>(a, workspace, stream) : launch<128, 1>(a, workspace, stream);
 }
 
 }  // namespace ecospec
