@@ -1,46 +1,336 @@
-// Latent attention of draft tokens, absorbed form.
-#include "row_attn.hpp"
+// Latent attention of draft tokens, absorbed form: T * H query rows of a sequence over the same rows of 576 elements.
+//
+// 2 * (576 + 512) operations a row and key against 1152 bytes a key: with all 128 heads of a layer even one token is at
+// the balance of the matrix cores and HBM, and more tokens are bound by the matrix cores.  A workgroup is one per compute
+// unit, four wavefronts with the whole register file: 128 rows.
+//   Scores: transposed (S^T = K Q^T, a lane holds one row), wavefront w having rows 32 w .. with their queries in 144
+//   registers; every wavefront reads the tile's keys from LDS.
+//   Values: wavefront w has elements 128 w .. of all 128 rows, in 256 accumulator registers, so each value is read from
+//   LDS once; the weights P pass between the wavefronts through LDS as the product's operand (bf16, 8 KiB a tile).
+//   The values' operand V^T is the key rows read with the transposing LDS load.
+// Tiles of 32 keys go from memory straight to LDS (three buffers: one being read, one landed, one in flight), chunks of
+// 16 bytes XORed with the row's low bits so that neither kind of read meets a bank twice.  One barrier a tile.
+#include "attn_plan.hpp"
 
 namespace ecospec {
 namespace {
 
-constexpr int kR = 512, kP = 64, kW = kR + kP;
+constexpr int kR = 512, kW = 576;
+constexpr int kRows = 128, kKeys = 32;
+constexpr int kRowBytes = kW * 2, kChunks = kRowBytes / 16;  // 72 chunks of 16 bytes
+constexpr int kTile = kKeys * kRowBytes;                     // 36864
+constexpr int kSteps = kW / 16;
+constexpr float kSlack = 8.f;  // powers of two by which weights may outgrow their reference before sums are scaled down
 
-struct LatentRow : PagedRow {
-    const LatentArgs &a;
-    float q[kW / kWave];
-    __device__ LatentRow(const LatentArgs &args) : PagedRow(args), a(args)
-    {
-        for (int i = 0; i < kW / kWave; ++i)
-            q[i] = bf16_bits_to_f32(a.q[((long)t * a.H + h) * kW + lane_id() * (kW / kWave) + i]);
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+
+__device__ __forceinline__ u32x2 read_tr(const char *p)
+{
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p));
+}
+
+// Arithmetic on an accumulator tile where it lies, in the accumulation registers: written out, because the compiler would
+// move all sixteen tiles to vector registers, and those to scratch, for it.  The waits at either end cover the matrix
+// instructions around it (19 wait states from a product's write to a read); the tile as an operand keeps them in place.
+__device__ __forceinline__ void acc_wait(f32x16 &o) { asm volatile("s_nop 15\n\ts_nop 7" : "+a"(o)); }
+
+__device__ __forceinline__ void acc_scale(f32x16 &o, float f)
+{
+    acc_wait(o);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        float x = o[i], t;
+        asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_mul_f32 %1, %2, %1\n\tv_accvgpr_write_b32 %0, %1" : "+a"(x), "=&v"(t) : "v"(f));
+        o[i] = x;
     }
-    __device__ const uint16_t *row(int j) const
-    {
-        return j < len ? a.pages + (page_of(j) * page + j % page) * kW : a.kv_new + (long)(t0 + j - len) * kW;
+    acc_wait(o);
+}
+
+__device__ __forceinline__ void acc_add(f32x16 &o, const float *c)
+{
+    acc_wait(o);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        float x = o[i], t;
+        asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_add_f32 %1, %2, %1\n\tv_accvgpr_write_b32 %0, %1" : "+a"(x), "=&v"(t) : "v"(c[i]));
+        o[i] = x;
     }
-    __device__ float dot(int j, int lane) const
-    {
-        const uint16_t *k = row(j) + lane * (kW / kWave);
-        float s = 0.f;
-        for (int i = 0; i < kW / kWave; ++i) s = fmaf(q[i], bf16_bits_to_f32(k[i]), s);
-        return s;
-    }
-    __device__ float value(int j, int e) const { return bf16_bits_to_f32(row(j)[e]); }
+    acc_wait(o);
+}
+
+struct Lds {
+    char tile[3][kTile];
+    u32x4 p[2][4][2][kWave];  // weights: tile parity, row tile, reduction step, lane
+    float down[2][kRows];     // what the sums of a row are multiplied by before the tile is added
+    int scaled[2][4];         // whether that is anything but 1 for a row tile
+    float2 ml[kRows];
 };
 
-__global__ __launch_bounds__(256) void latent_row_kernel(LatentArgs a)
+__global__ __launch_bounds__(256, 1) void latent_attn_kernel(LatentArgs a, Shape shape, Parts parts)
 {
-    const LatentRow r(a);
-    row_attention<kR>(r, a.scale, a.o + (long)blockIdx.x * kR, a.lse ? a.lse + blockIdx.x : nullptr);
+    __shared__ __attribute__((aligned(16))) Lds lds;
+    Item it;
+    if (!plan_item(a, a.H, 1, shape, parts, reinterpret_cast<int *>(lds.tile), it)) return;
+    __syncthreads();
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 32, half = lane / 32;
+    const int row0 = it.group * kRows, n_rows = it.n_tok * a.H;
+    const int *table = a.block_table + (long)it.b * a.max_blocks;
+    const int lp = 31 - __builtin_clz(a.page);
+    const int cached = (it.len + kKeys - 1) / kKeys, drafts = min(it.n_tok, kMaxDrafts);
+
+    // ---- tiles: wavefront w brings rows 8 w .. 8 w + 7, nine loads of 64 chunks; they lie in one page.
+    uint32_t src[9];  // lane's byte offset from the first row
+#pragma unroll
+    for (int n = 0; n < 9; ++n) {
+        const int i = n * 64 + lane, r = i / kChunks, c = i % kChunks;
+        src[n] = (uint32_t)(r * kRowBytes + (c ^ r) * 16);
+    }
+    auto page_id = [&](int t) {
+        const int key = max(min(t * kKeys + 8 * wave, it.len - 1), 0);
+        return min(max(table[key >> lp], 0), a.n_pages - 1);
+    };
+    auto load = [&](int t, int id, int buf) {
+        int key, rows;
+        const uint16_t *base;
+        if (t < cached) {
+            key = min(t * kKeys + 8 * wave, it.len - 1);
+            rows = min(it.len - key, 8);
+            base = a.pages + ((long)id * a.page + (key & (a.page - 1))) * kW;
+        } else {
+            key = min((t - cached) * kKeys + 8 * wave, drafts - 1);
+            rows = min(drafts - key, 8);
+            base = a.kv_new + (long)(it.t0 + key) * kW;
+        }
+        const u32x4 rsrc = rsrc_words(base, (uint32_t)(rows * kRowBytes));
+        const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(lds.tile[buf]) + 8 * wave * kRowBytes);
+        if (rows == 8) {
+#pragma unroll
+            for (int n = 0; n < 9; ++n) load16_lds(rsrc, src[n], dst + n * 1024);
+        } else {  // rows past the end repeat the last one
+#pragma unroll
+            for (int n = 0; n < 9; ++n) {
+                const uint32_t r = src[n] / kRowBytes;
+                load16_lds(rsrc, src[n] - (r - min(r, (uint32_t)(rows - 1))) * kRowBytes, dst + n * 1024);
+            }
+        }
+    };
+
+    int next_id = it.first < cached ? page_id(it.first) : 0;
+    load(it.first, next_id, 0);
+    if (it.first + 1 < it.last) {
+        if (it.first + 1 < cached) next_id = page_id(it.first + 1);
+        load(it.first + 1, next_id, 1);
+    }
+    if (it.first + 2 < cached) next_id = page_id(it.first + 2);
+
+    // ---- queries of the wavefront's 32 rows
+    bf16x8 q[kSteps];
+    uint64_t see = 0;
+    {
+        const int r = row0 + 32 * wave + col;
+        const bool in = r < n_rows;
+        const int tok = in ? r / a.H : 0;
+        const uint16_t *p = a.q + ((long)(it.t0 + tok) * a.H + (in ? r % a.H : 0)) * kW + 8 * half;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) q[s] = *reinterpret_cast<const bf16x8 *>(p + 16 * s);
+        if (in) see = (a.mask ? a.mask[it.t0 + tok] : bits_below(tok + 1)) & bits_below(drafts);
+    }
+
+    f32x16 o[4][4];  // row tile, element tile
+#pragma unroll
+    for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[rt][d][i] = 0.f;
+    float m = -INFINITY, l = 0.f;
+    const float scale2 = a.scale * kLog2e;
+
+    // Lane offsets of the LDS reads: keys, by the step's low bits; values, by the element tile's low bit.
+    uint32_t k_at[4], v_at[2];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) k_at[s] = (uint32_t)(col * kRowBytes + ((2 * s + half) ^ (col & 7)) * 16);
+    {
+        const int i = lane % 16, key = 4 * half + i / 4;
+#pragma unroll
+        for (int d = 0; d < 2; ++d)
+            v_at[d] = (uint32_t)(key * kRowBytes + ((((4 * d + lane / 16 % 2 * 2 + i % 4 / 2) ^ key) + 16 * wave) * 16) + i % 2 * 8);
+    }
+
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+
+    for (int t = it.first; t < it.last; ++t) {
+        const int k = t - it.first, buf = k % 3, par = k & 1;
+        const char *tile = lds.tile[buf];
+        // ---- scores
+        f32x16 s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+        for (int st = 0; st < kSteps; ++st)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(tile + k_at[st % 4] + st / 4 * 128), q[st], s, 0, 0, 0);
+        // ---- weights; register i is key 8 (i / 4) + 4 half + i % 4
+        float x[16];
+        if (t >= cached) {
+            const uint32_t bits = (uint32_t)(see >> (t - cached) * kKeys) >> 4 * half;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = bits >> (i / 4 * 8 + i % 4) & 1 ? s[i] * scale2 : -INFINITY;
+        } else {
+            const int left = it.len - t * kKeys - 4 * half;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = i / 4 * 8 + i % 4 < left ? s[i] * scale2 : -INFINITY;
+        }
+        float top = x[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+        top = halves_max(top);
+        const bool rescale = __any(top > m + kSlack);
+        bool scaled = false;
+        if (rescale) {
+            const float now = fmaxf(m, top), down = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
+            scaled = __any(m != -INFINITY);
+            m = now;
+            l *= down;
+            if (half == 0) lds.down[par][32 * wave + col] = down;
+        }
+        if (lane == 0) lds.scaled[par][wave] = scaled;
+        const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            x[i] = __builtin_amdgcn_exp2f(x[i] - base);
+            l += x[i];
+        }
+        lds.p[par][wave][0][lane] = __builtin_bit_cast(u32x4, pack_bf16x8(x));
+        lds.p[par][wave][1][lane] = __builtin_bit_cast(u32x4, pack_bf16x8(x + 8));
+        // The next tile has landed, and nobody reads the one before this any more.
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (t + 2 < it.last) {
+            load(t + 2, next_id, (k + 2) % 3);
+            if (t + 3 < cached) next_id = page_id(t + 3);
+        }
+        // ---- values
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt)
+            if (lds.scaled[par][rt]) {
+                const float down = lds.down[par][32 * rt + col];
+#pragma unroll
+                for (int d = 0; d < 4; ++d) acc_scale(o[rt][d], down);
+            }
+        if (t >= cached) {
+            // A weight of zero must not meet an infinity or NaN.  Where a draft has one, what it gives the rows that see
+            // it is added by itself, and zeros take its place in the tile.
+            auto bad = [](uint32_t v) { return (v & 0x7f80u) == 0x7f80u; };
+            u32x4 *all = reinterpret_cast<u32x4 *>(lds.tile[buf]);
+            bool odd = false;
+            for (int i = threadIdx.x; i < kTile / 16; i += 256) {
+                const u32x4 v = all[i];
+#pragma unroll
+                for (int w = 0; w < 4; ++w) odd |= bad(v[w]) || bad(v[w] >> 16);
+            }
+            if (__syncthreads_or(odd)) {
+#pragma unroll
+                for (int rt = 0; rt < 4; ++rt) {
+                    const int r = row0 + 32 * rt + col, first = (t - cached) * kKeys;
+                    uint64_t sees = 0;
+                    if (r < n_rows) sees = (a.mask ? a.mask[it.t0 + r / a.H] : bits_below(r / a.H + 1)) & bits_below(drafts);
+                    for (int d = 0; d < 4; ++d) {
+                        float c[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) c[i] = 0.f;
+                        for (int j = 0; j < min(drafts - first, kKeys); ++j) {
+                            if (!(sees >> (first + j) & 1)) continue;
+                            const int e = j / 8 * 4 + j % 4;  // register of key j
+                            const uint32_t w = reinterpret_cast<const uint32_t *>(&lds.p[par][rt][e / 8][j / 4 % 2 * 32 + col])[e % 8 / 2];
+                            const float f = bf16_bits_to_f32((uint16_t)(w >> e % 2 * 16));
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const int el = 128 * wave + 32 * d + i / 4 * 8 + 4 * half + i % 4;
+                                const uint16_t v = *reinterpret_cast<const uint16_t *>(tile + j * kRowBytes + ((el / 8) ^ (j & 7)) * 16 + el % 8 * 2);
+                                if (bad(v)) c[i] = fmaf(f, bf16_bits_to_f32(v), c[i]);
+                            }
+                        }
+                        if (d == 0) acc_add(o[rt][0], c);
+                        else if (d == 1) acc_add(o[rt][1], c);
+                        else if (d == 2) acc_add(o[rt][2], c);
+                        else acc_add(o[rt][3], c);
+                    }
+                }
+                __syncthreads();
+                for (int i = threadIdx.x; i < kTile / 16; i += 256) {
+                    u32x4 v = all[i];
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        if (bad(v[w])) v[w] &= 0xffff0000u;
+                        if (bad(v[w] >> 16)) v[w] &= 0xffffu;
+                    }
+                    all[i] = v;
+                }
+                __syncthreads();
+            }
+        }
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+            bf16x8 w[4];
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) w[rt] = __builtin_bit_cast(bf16x8, lds.p[par][rt][st][lane]);
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                const char *p = tile + v_at[d % 2] + d / 2 * 128 + st * 16 * kRowBytes;
+                const u32x2 lo = read_tr(p), hi = read_tr(p + 8 * kRowBytes);
+                const bf16x8 v = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+#pragma unroll
+                for (int rt = 0; rt < 4; ++rt) o[rt][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[rt], o[rt][d], 0, 0, 0);
+            }
+        }
+    }
+
+    l = halves_sum(l);
+    if (half == 0) lds.ml[32 * wave + col] = make_float2(l == 0.f ? -INFINITY : m, l);
+    __syncthreads();
+    if (it.chunks > 1) {
+        f32x4 *out = reinterpret_cast<f32x4 *>(parts.o) + (long)it.slot * 64 * 256;
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    out[(rt * 16 + 4 * wave + d) * 256 + i * 64 + lane] =
+                        f32x4{o[rt][d][4 * i], o[rt][d][4 * i + 1], o[rt][d][4 * i + 2], o[rt][d][4 * i + 3]};
+        if (threadIdx.x < kRows) parts.ml[(long)it.slot * kRows + threadIdx.x] = lds.ml[threadIdx.x];
+        return;
+    }
+#pragma unroll
+    for (int rt = 0; rt < 4; ++rt) {
+        const int r = row0 + 32 * rt + col;
+        if (r >= n_rows) continue;
+        const long at = (long)(it.t0 + r / a.H) * a.H + r % a.H;
+        const float2 ml = lds.ml[32 * rt + col];
+        const float inv = ml.y == 0.f ? 0.f : 1.f / ml.y;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<u32x2 *>(a.o + at * kR + 128 * wave + 32 * d + 8 * i + 4 * half) =
+                    u32x2{pack_bf16x2(o[rt][d][4 * i] * inv, o[rt][d][4 * i + 1] * inv),
+                          pack_bf16x2(o[rt][d][4 * i + 2] * inv, o[rt][d][4 * i + 3] * inv)};
+        if (a.lse && wave == 0 && half == 0) a.lse[at] = ml.y == 0.f ? -INFINITY : (ml.x + __builtin_amdgcn_logf(ml.y)) / kLog2e;
+    }
 }
 
 }  // namespace
 
-size_t latent_workspace(int, int, int) { return 256; }
+size_t latent_workspace(int N, int B, int H) { return parts_at(nullptr, group_bound(N, B, H, 1, kRows), kCus, kRows, kR, nullptr); }
 
-hipError_t launch_latent_attn(const LatentArgs &a, void *, hipStream_t stream)
+hipError_t launch_latent_attn(const LatentArgs &a, void *workspace, hipStream_t stream)
 {
-    latent_row_kernel<<<(unsigned)(a.N * a.H), 256, 0, stream>>>(a);
+    const long groups = group_bound(a.N, a.B, a.H, 1, kRows);
+    Parts parts;
+    parts_at(workspace, groups, kCus, kRows, kR, &parts);
+    latent_attn_kernel<<<(unsigned)grid_bound(groups, kCus), 256, 0, stream>>>(a, Shape{kRows, kKeys, 2, kCus}, parts);
+    join_kernel<kRows, kR><<<(unsigned)(groups * (kRows / 32) * (kR / 32)), 256, 0, stream>>>(a, a.H, parts);
     return hipGetLastError();
 }
 
