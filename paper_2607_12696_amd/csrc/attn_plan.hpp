@@ -167,26 +167,45 @@ __device__ __forceinline__ bool plan_item(const PagedArgs &a, int per_token, int
 template <int ROWS, int W>
 __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int per_token, Parts p)
 {
-    constexpr int kBlocks = ROWS / 32 * (W / 32);
+    constexpr int kBlocks = ROWS / 32 * (W / 32), kJoin = 64;
+    __shared__ float weight[kJoin * 32], sums[kJoin * 32];
     const int g = blockIdx.x / kBlocks, blk = blockIdx.x % kBlocks;
     if (g >= *p.groups) return;
     const GroupInfo in = p.info[g];
     if (in.chunks <= 1) return;
-    const int lane = lane_id(), row = blk / (W / 32) * 32 + lane % 32;
+    const int lane = lane_id(), col = lane % 32, row = blk / (W / 32) * 32 + col;
+    const float2 *ml = p.ml + (long)in.slot0 * ROWS + row;
+    const long step = (long)in.stride * ROWS;
+    // The largest reference maximum of each row; eight threads a row.
     float top = -INFINITY;
-    for (int c = 0; c < in.chunks; ++c) top = fmaxf(top, p.ml[(long)(in.slot0 + c * in.stride) * ROWS + row].x);
+#pragma unroll 4
+    for (int c = threadIdx.x / 32; c < in.chunks; c += 8) top = fmaxf(top, ml[c * step].x);
+    weight[threadIdx.x] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, weight[i * 32 + col]);
     const float base = top == -INFINITY ? 0.f : top;
     float total = 0.f;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int c = 0; c < in.chunks; ++c) {
-        const long slot = in.slot0 + c * in.stride;
-        const float2 ml = p.ml[slot * ROWS + row];
-        const float f = __builtin_amdgcn_exp2f(ml.x - base);
-        const f32x4 v = reinterpret_cast<const f32x4 *>(p.o)[(slot * kBlocks + blk) * 256 + threadIdx.x];
-        total = fmaf(ml.y, f, total);
+    for (int c0 = 0; c0 < in.chunks; c0 += kJoin) {
+        const int n = min(in.chunks - c0, kJoin);
+        __syncthreads();
+        for (int c = threadIdx.x / 32; c < kJoin; c += 8) {
+            float2 v = make_float2(-INFINITY, 0.f);
+            if (c < n) v = ml[(c0 + c) * step];
+            weight[c * 32 + col] = __builtin_amdgcn_exp2f(v.x - base);
+            sums[c * 32 + col] = v.y;
+        }
+        __syncthreads();
+        const f32x4 *o = reinterpret_cast<const f32x4 *>(p.o) + ((in.slot0 + (long)c0 * in.stride) * kBlocks + blk) * 256 + threadIdx.x;
+#pragma unroll 16
+        for (int c = 0; c < n; ++c) {
+            const float f = weight[c * 32 + col];
+            const f32x4 v = o[(long)c * in.stride * kBlocks * 256];
+            total = fmaf(sums[c * 32 + col], f, total);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] = fmaf(v[i], f, sum[i]);
+            for (int i = 0; i < 4; ++i) sum[i] = fmaf(v[i], f, sum[i]);
+        }
     }
     const int t0 = min(max(a.token_offsets[in.b], 0), a.N), n = min(max(a.token_offsets[in.b + 1], t0), a.N) - t0;
     const int tiles = (int)(((long)n * per_token + ROWS - 1) / ROWS), r = in.group % tiles * ROWS + row;
@@ -213,12 +232,25 @@ __device__ __forceinline__ float halves_sum(float v)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// The same over the two rows of 16 lanes of each half (lanes l and l ^ 16).
+__device__ __forceinline__ float quads_max(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+__device__ __forceinline__ float quads_sum(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 __device__ __forceinline__ bf16x8 pack_bf16x8(const float *f)
 {
-    u32x4 w;
+    bf16x8 w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(f[2 * i], f[2 * i + 1]);
-    return __builtin_bit_cast(bf16x8, w);
+    for (int i = 0; i < 8; ++i) w[i] = static_cast<__bf16>(f[i]);
+    return w;
 }
 
 __device__ __forceinline__ uint64_t bits_below(int n)

@@ -2,14 +2,16 @@
 //
 // 2 * (576 + 512) operations a row and key against 1152 bytes a key: with all 128 heads of a layer even one token is at
 // the balance of the matrix cores and HBM, and more tokens are bound by the matrix cores.  A workgroup is one per compute
-// unit, four wavefronts with the whole register file: 128 rows.
+// unit: 128 rows, four wavefronts with the whole register file.
 //   Scores: transposed (S^T = K Q^T, a lane holds one row), wavefront w having rows 32 w .. with their queries in 144
 //   registers; every wavefront reads the tile's keys from LDS.
 //   Values: wavefront w has elements 128 w .. of all 128 rows, in 256 accumulator registers, so each value is read from
 //   LDS once; the weights P pass between the wavefronts through LDS as the product's operand (bf16, 8 KiB a tile).
 //   The values' operand V^T is the key rows read with the transposing LDS load.
-// Tiles of 32 keys go from memory straight to LDS (three buffers: one being read, one landed, one in flight), chunks of
-// 16 bytes XORed with the row's low bits so that neither kind of read meets a bank twice.  One barrier a tile.
+// Tiles of 32 keys go from memory straight to LDS (three buffers: the tile of the value product, the next one's scores,
+// one in flight), chunks of 16 bytes XORed with the row's low bits so that neither kind of read meets a bank twice.  With
+// one wavefront on a SIMD nothing else hides the softmax: it runs between the value products of the tile before.  One
+// barrier a tile.
 #include "attn_plan.hpp"
 
 namespace ecospec {
@@ -20,6 +22,8 @@ constexpr int kRows = 128, kKeys = 32;
 constexpr int kRowBytes = kW * 2, kChunks = kRowBytes / 16;  // 72 chunks of 16 bytes
 constexpr int kTile = kKeys * kRowBytes;                     // 36864
 constexpr int kSteps = kW / 16;
+constexpr int kWaves = 4, kThreads = kWaves * kWave;
+constexpr int kAhead = 4;       // operands of a group of score products, read while the group before runs
 constexpr float kSlack = 8.f;  // powers of two by which weights may outgrow their reference before sums are scaled down
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
@@ -46,27 +50,32 @@ __device__ __forceinline__ void acc_scale(f32x16 &o, float f)
     acc_wait(o);
 }
 
-__device__ __forceinline__ void acc_add(f32x16 &o, const float *c)
+// The score products, with their sums in vector registers (the accumulation registers are full): the compiler would give
+// them accumulation registers.  Written out, they carry their own waits: a register written by the vector unit needs two
+// wait states before a product reads it, a product's result 19 before the vector unit does.
+__device__ __forceinline__ void mfma_first(f32x16 &s, const bf16x8 &a, const bf16x8 &b)
 {
-    acc_wait(o);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        float x = o[i], t;
-        asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_add_f32 %1, %2, %1\n\tv_accvgpr_write_b32 %0, %1" : "+a"(x), "=&v"(t) : "v"(c[i]));
-        o[i] = x;
-    }
-    acc_wait(o);
+    asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "v"(b));
 }
+
+__device__ __forceinline__ void mfma_next(f32x16 &s, const bf16x8 &a, const bf16x8 &b)
+{
+    asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "v"(b));
+}
+
+__device__ __forceinline__ void mfma_wait(f32x16 &s) { asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s)); }
+
+__device__ __forceinline__ bool not_finite(uint32_t bf16) { return (bf16 & 0x7f80u) == 0x7f80u; }
 
 struct Lds {
     char tile[3][kTile];
-    u32x4 p[2][4][2][kWave];  // weights: tile parity, row tile, reduction step, lane
+    u32x4 p[2][4][2][kWave];  // weights: tile parity, row tile of 32, reduction step of 16 keys, lane
     float down[2][kRows];     // what the sums of a row are multiplied by before the tile is added
-    int scaled[2][4];         // whether that is anything but 1 for a row tile
+    int scaled[2][kWaves];    // whether that is anything but 1 for a row tile
     float2 ml[kRows];
 };
 
-__global__ __launch_bounds__(256, 1) void latent_attn_kernel(LatentArgs a, Shape shape, Parts parts)
+__global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, Shape shape, Parts parts)
 {
     __shared__ __attribute__((aligned(16))) Lds lds;
     Item it;
@@ -79,6 +88,7 @@ __global__ __launch_bounds__(256, 1) void latent_attn_kernel(LatentArgs a, Shape
     const int cached = (it.len + kKeys - 1) / kKeys, drafts = min(it.n_tok, kMaxDrafts);
 
     // ---- tiles: wavefront w brings rows 8 w .. 8 w + 7, nine loads of 64 chunks; they lie in one page.
+    const int row8 = 8 * wave;
     uint32_t src[9];  // lane's byte offset from the first row
 #pragma unroll
     for (int n = 0; n < 9; ++n) {
@@ -86,23 +96,23 @@ __global__ __launch_bounds__(256, 1) void latent_attn_kernel(LatentArgs a, Shape
         src[n] = (uint32_t)(r * kRowBytes + (c ^ r) * 16);
     }
     auto page_id = [&](int t) {
-        const int key = max(min(t * kKeys + 8 * wave, it.len - 1), 0);
+        const int key = max(min(t * kKeys + row8, it.len - 1), 0);
         return min(max(table[key >> lp], 0), a.n_pages - 1);
     };
     auto load = [&](int t, int id, int buf) {
         int key, rows;
         const uint16_t *base;
         if (t < cached) {
-            key = min(t * kKeys + 8 * wave, it.len - 1);
+            key = min(t * kKeys + row8, it.len - 1);
             rows = min(it.len - key, 8);
             base = a.pages + ((long)id * a.page + (key & (a.page - 1))) * kW;
         } else {
-            key = min((t - cached) * kKeys + 8 * wave, drafts - 1);
+            key = min((t - cached) * kKeys + row8, drafts - 1);
             rows = min(drafts - key, 8);
             base = a.kv_new + (long)(it.t0 + key) * kW;
         }
         const u32x4 rsrc = rsrc_words(base, (uint32_t)(rows * kRowBytes));
-        const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(lds.tile[buf]) + 8 * wave * kRowBytes);
+        const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(lds.tile[buf]) + row8 * kRowBytes);
         if (rows == 8) {
 #pragma unroll
             for (int n = 0; n < 9; ++n) load16_lds(rsrc, src[n], dst + n * 1024);
@@ -125,7 +135,6 @@ __global__ __launch_bounds__(256, 1) void latent_attn_kernel(LatentArgs a, Shape
 
     // ---- queries of the wavefront's 32 rows
     bf16x8 q[kSteps];
-    uint64_t see = 0;
     {
         const int r = row0 + 32 * wave + col;
         const bool in = r < n_rows;
@@ -133,7 +142,6 @@ __global__ __launch_bounds__(256, 1) void latent_attn_kernel(LatentArgs a, Shape
         const uint16_t *p = a.q + ((long)(it.t0 + tok) * a.H + (in ? r % a.H : 0)) * kW + 8 * half;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) q[s] = *reinterpret_cast<const bf16x8 *>(p + 16 * s);
-        if (in) see = (a.mask ? a.mask[it.t0 + tok] : bits_below(tok + 1)) & bits_below(drafts);
     }
 
     f32x16 o[4][4];  // row tile, element tile
@@ -144,6 +152,7 @@ __global__ __launch_bounds__(256, 1) void latent_attn_kernel(LatentArgs a, Shape
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[rt][d][i] = 0.f;
     float m = -INFINITY, l = 0.f;
+    int not_finite_drafts = 0;  // bit: draft tile
     const float scale2 = a.scale * kLog2e;
 
     // Lane offsets of the LDS reads: keys, by the step's low bits; values, by the element tile's low bit.
@@ -157,119 +166,106 @@ __global__ __launch_bounds__(256, 1) void latent_attn_kernel(LatentArgs a, Shape
             v_at[d] = (uint32_t)(key * kRowBytes + ((((4 * d + lane / 16 % 2 * 2 + i % 4 / 2) ^ key) + 16 * wave) * 16) + i % 2 * 8);
     }
 
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-
-    for (int t = it.first; t < it.last; ++t) {
-        const int k = t - it.first, buf = k % 3, par = k & 1;
-        const char *tile = lds.tile[buf];
-        // ---- scores
+    // Scores of tile t, in powers of two; register i is key 8 (i / 4) + 4 half + i % 4.
+    auto scores = [&](int t, float *x) {
+        const char *tile = lds.tile[(t - it.first) % 3];
+        bf16x8 k[2][kAhead];
+        auto fetch = [&](int g) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int st = g * kAhead + i;
+                k[g & 1][i] = *reinterpret_cast<const bf16x8 *>(tile + k_at[st % 4] + st / 4 * 128);
+            }
+        };
+        fetch(0);
         f32x16 s;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        for (int g = 0; g < kSteps / kAhead; ++g) {
+            if (g + 1 < kSteps / kAhead) fetch(g + 1);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int st = 0; st < kSteps; ++st)
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(tile + k_at[st % 4] + st / 4 * 128), q[st], s, 0, 0, 0);
-        // ---- weights; register i is key 8 (i / 4) + 4 half + i % 4
-        float x[16];
+            for (int i = 0; i < kAhead; ++i) {
+                if (g == 0 && i == 0) mfma_first(s, k[0][0], q[0]);
+                else mfma_next(s, k[g & 1][i], q[g * kAhead + i]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        mfma_wait(s);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = s[i] * scale2;
         if (t >= cached) {
+            const int r = row0 + 32 * wave + col;
+            uint64_t see = 0;
+            if (r < n_rows) see = (a.mask ? a.mask[it.t0 + r / a.H] : bits_below(r / a.H + 1)) & bits_below(drafts);
             const uint32_t bits = (uint32_t)(see >> (t - cached) * kKeys) >> 4 * half;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = bits >> (i / 4 * 8 + i % 4) & 1 ? s[i] * scale2 : -INFINITY;
-        } else {
+            for (int i = 0; i < 16; ++i)
+                if (!(bits >> (i / 4 * 8 + i % 4) & 1)) x[i] = -INFINITY;
+        } else if ((t + 1) * kKeys > it.len) {
             const int left = it.len - t * kKeys - 4 * half;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = i / 4 * 8 + i % 4 < left ? s[i] * scale2 : -INFINITY;
+            for (int i = 0; i < 16; ++i)
+                if (i / 4 * 8 + i % 4 >= left) x[i] = -INFINITY;
         }
+    };
+    // Weights of the scores x of tile t, the running maximum and sum, and what the sums so far are scaled by; no branch,
+    // so that it can run between the products of values().
+    auto weights = [&](int t, float *x) {
+        const int par = (t - it.first) & 1;
         float top = x[0];
 #pragma unroll
         for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
         top = halves_max(top);
-        const bool rescale = __any(top > m + kSlack);
-        bool scaled = false;
-        if (rescale) {
-            const float now = fmaxf(m, top), down = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
-            scaled = __any(m != -INFINITY);
-            m = now;
-            l *= down;
-            if (half == 0) lds.down[par][32 * wave + col] = down;
-        }
-        if (lane == 0) lds.scaled[par][wave] = scaled;
-        const float base = m == -INFINITY ? 0.f : m;
+        const bool move = __any(top > m + kSlack);
+        const float now = move ? fmaxf(m, top) : m, base = now == -INFINITY ? 0.f : now;
+        const float down = __builtin_amdgcn_exp2f((m == -INFINITY ? base : m) - base);
+        const bool scaled = move && __any(m != -INFINITY);
+        m = now;
+        lds.down[par][32 * wave + col] = down;
+        lds.scaled[par][wave] = scaled;
+        float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             x[i] = __builtin_amdgcn_exp2f(x[i] - base);
-            l += x[i];
+            sum += x[i];
         }
+        l = fmaf(l, down, sum);
         lds.p[par][wave][0][lane] = __builtin_bit_cast(u32x4, pack_bf16x8(x));
         lds.p[par][wave][1][lane] = __builtin_bit_cast(u32x4, pack_bf16x8(x + 8));
-        // The next tile has landed, and nobody reads the one before this any more.
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (t + 2 < it.last) {
-            load(t + 2, next_id, (k + 2) % 3);
-            if (t + 3 < cached) next_id = page_id(t + 3);
-        }
-        // ---- values
+    };
+    // Before tile t's values are added.
+    auto rescale = [&](int t) {
+        const int par = (t - it.first) & 1;
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt)
-            if (lds.scaled[par][rt]) {
+            if (__builtin_amdgcn_readfirstlane(lds.scaled[par][rt])) {
                 const float down = lds.down[par][32 * rt + col];
 #pragma unroll
                 for (int d = 0; d < 4; ++d) acc_scale(o[rt][d], down);
             }
         if (t >= cached) {
-            // A weight of zero must not meet an infinity or NaN.  Where a draft has one, what it gives the rows that see
-            // it is added by itself, and zeros take its place in the tile.
-            auto bad = [](uint32_t v) { return (v & 0x7f80u) == 0x7f80u; };
-            u32x4 *all = reinterpret_cast<u32x4 *>(lds.tile[buf]);
+            // A weight of zero must not meet an infinity or NaN: where a draft has one, zeros take its place, and what it
+            // gives the rows that see it is added at the end.
+            u32x4 *all = reinterpret_cast<u32x4 *>(lds.tile[(t - it.first) % 3]);
             bool odd = false;
-            for (int i = threadIdx.x; i < kTile / 16; i += 256) {
-                const u32x4 v = all[i];
+            for (int i = threadIdx.x; i < kTile / 16; i += kThreads) {
+                u32x4 v = all[i];
+                bool some = false;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) odd |= bad(v[w]) || bad(v[w] >> 16);
-            }
-            if (__syncthreads_or(odd)) {
-#pragma unroll
-                for (int rt = 0; rt < 4; ++rt) {
-                    const int r = row0 + 32 * rt + col, first = (t - cached) * kKeys;
-                    uint64_t sees = 0;
-                    if (r < n_rows) sees = (a.mask ? a.mask[it.t0 + r / a.H] : bits_below(r / a.H + 1)) & bits_below(drafts);
-                    for (int d = 0; d < 4; ++d) {
-                        float c[16];
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) c[i] = 0.f;
-                        for (int j = 0; j < min(drafts - first, kKeys); ++j) {
-                            if (!(sees >> (first + j) & 1)) continue;
-                            const int e = j / 8 * 4 + j % 4;  // register of key j
-                            const uint32_t w = reinterpret_cast<const uint32_t *>(&lds.p[par][rt][e / 8][j / 4 % 2 * 32 + col])[e % 8 / 2];
-                            const float f = bf16_bits_to_f32((uint16_t)(w >> e % 2 * 16));
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                const int el = 128 * wave + 32 * d + i / 4 * 8 + 4 * half + i % 4;
-                                const uint16_t v = *reinterpret_cast<const uint16_t *>(tile + j * kRowBytes + ((el / 8) ^ (j & 7)) * 16 + el % 8 * 2);
-                                if (bad(v)) c[i] = fmaf(f, bf16_bits_to_f32(v), c[i]);
-                            }
-                        }
-                        if (d == 0) acc_add(o[rt][0], c);
-                        else if (d == 1) acc_add(o[rt][1], c);
-                        else if (d == 2) acc_add(o[rt][2], c);
-                        else acc_add(o[rt][3], c);
-                    }
+                for (int w = 0; w < 4; ++w) {
+                    const bool lo = not_finite(v[w]), hi = not_finite(v[w] >> 16);
+                    v[w] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+                    some |= lo || hi;
                 }
-                __syncthreads();
-                for (int i = threadIdx.x; i < kTile / 16; i += 256) {
-                    u32x4 v = all[i];
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        if (bad(v[w])) v[w] &= 0xffff0000u;
-                        if (bad(v[w] >> 16)) v[w] &= 0xffffu;
-                    }
-                    all[i] = v;
-                }
-                __syncthreads();
+                if (some) all[i] = v;
+                odd |= some;
             }
+            if (__syncthreads_or(odd)) not_finite_drafts |= 1 << (t - cached);
         }
+    };
+    auto values = [&](int t) {
+        const int par = (t - it.first) & 1;
+        const char *tile = lds.tile[(t - it.first) % 3];
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
             bf16x8 w[4];
@@ -284,11 +280,52 @@ __global__ __launch_bounds__(256, 1) void latent_attn_kernel(LatentArgs a, Shape
                 for (int rt = 0; rt < 4; ++rt) o[rt][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[rt], o[rt][d], 0, 0, 0);
             }
         }
+    };
+    // The loads so far have landed, and every wavefront is past the tile before.
+    auto step = [] {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
+
+    step();
+    float x[16];
+    scores(it.first, x);
+    weights(it.first, x);
+    step();
+    for (int t = it.first + 1; t < it.last; ++t) {
+        if (t + 1 < it.last) {
+            load(t + 1, next_id, (t + 1 - it.first) % 3);
+            if (t + 2 < cached) next_id = page_id(t + 2);
+        }
+        scores(t, x);
+        rescale(t - 1);
+        values(t - 1);
+        weights(t, x);
+        step();
     }
+    rescale(it.last - 1);
+    values(it.last - 1);
 
     l = halves_sum(l);
     if (half == 0) lds.ml[32 * wave + col] = make_float2(l == 0.f ? -INFINITY : m, l);
     __syncthreads();
+    // What the infinities and NaN of drafts give element el (and the next three) of a row; the weights of a tile of drafts
+    // still lie in LDS.
+    auto add_drafts = [&](int rt, int el, f32x4 &v) {
+        const int r = row0 + 32 * rt + col;
+        if (r >= n_rows) return;
+        const uint64_t sees = (a.mask ? a.mask[it.t0 + r / a.H] : bits_below(r / a.H + 1)) & bits_below(drafts);
+        for (int j = 0; j < drafts; ++j) {
+            const int t = j / kKeys, k = j % kKeys;
+            if (!(not_finite_drafts >> t & 1) || !(sees >> j & 1)) continue;
+            const u32x4 &p = lds.p[(cached + t - it.first) & 1][rt][k / 16][k / 4 % 2 * 32 + col];
+            const float w = bf16_bits_to_f32(reinterpret_cast<const uint16_t *>(&p)[k / 8 % 2 * 4 + k % 4]);
+            for (int i = 0; i < 4; ++i) {
+                const uint16_t c = a.kv_new[(long)(it.t0 + j) * kW + el + i];
+                if (not_finite(c)) v[i] = fmaf(w, bf16_bits_to_f32(c), v[i]);
+            }
+        }
+    };
     if (it.chunks > 1) {
         f32x4 *out = reinterpret_cast<f32x4 *>(parts.o) + (long)it.slot * 64 * 256;
 #pragma unroll
@@ -296,9 +333,11 @@ __global__ __launch_bounds__(256, 1) void latent_attn_kernel(LatentArgs a, Shape
 #pragma unroll
             for (int d = 0; d < 4; ++d)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    out[(rt * 16 + 4 * wave + d) * 256 + i * 64 + lane] =
-                        f32x4{o[rt][d][4 * i], o[rt][d][4 * i + 1], o[rt][d][4 * i + 2], o[rt][d][4 * i + 3]};
+                for (int i = 0; i < 4; ++i) {
+                    f32x4 v = {o[rt][d][4 * i], o[rt][d][4 * i + 1], o[rt][d][4 * i + 2], o[rt][d][4 * i + 3]};
+                    if (not_finite_drafts) add_drafts(rt, 128 * wave + 32 * d + 8 * i + 4 * half, v);
+                    out[(rt * 16 + 4 * wave + d) * 256 + i * 64 + lane] = v;
+                }
         if (threadIdx.x < kRows) parts.ml[(long)it.slot * kRows + threadIdx.x] = lds.ml[threadIdx.x];
         return;
     }
@@ -312,10 +351,13 @@ __global__ __launch_bounds__(256, 1) void latent_attn_kernel(LatentArgs a, Shape
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *reinterpret_cast<u32x2 *>(a.o + at * kR + 128 * wave + 32 * d + 8 * i + 4 * half) =
-                    u32x2{pack_bf16x2(o[rt][d][4 * i] * inv, o[rt][d][4 * i + 1] * inv),
-                          pack_bf16x2(o[rt][d][4 * i + 2] * inv, o[rt][d][4 * i + 3] * inv)};
+            for (int i = 0; i < 4; ++i) {
+                const int el = 128 * wave + 32 * d + 8 * i + 4 * half;
+                f32x4 v = {o[rt][d][4 * i], o[rt][d][4 * i + 1], o[rt][d][4 * i + 2], o[rt][d][4 * i + 3]};
+                if (not_finite_drafts) add_drafts(rt, el, v);
+                *reinterpret_cast<u32x2 *>(a.o + at * kR + el) =
+                    u32x2{pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv)};
+            }
         if (a.lse && wave == 0 && half == 0) a.lse[at] = ml.y == 0.f ? -INFINITY : (ml.x + __builtin_amdgcn_logf(ml.y)) / kLog2e;
     }
 }
@@ -329,7 +371,7 @@ hipError_t launch_latent_attn(const LatentArgs &a, void *workspace, hipStream_t 
     const long groups = group_bound(a.N, a.B, a.H, 1, kRows);
     Parts parts;
     parts_at(workspace, groups, kCus, kRows, kR, &parts);
-    latent_attn_kernel<<<(unsigned)grid_bound(groups, kCus), 256, 0, stream>>>(a, Shape{kRows, kKeys, 2, kCus}, parts);
+    latent_attn_kernel<<<(unsigned)grid_bound(groups, kCus), kThreads, 0, stream>>>(a, Shape{kRows, kKeys, 2, kCus}, parts);
     join_kernel<kRows, kR><<<(unsigned)(groups * (kRows / 32) * (kR / 32)), 256, 0, stream>>>(a, a.H, parts);
     return hipGetLastError();
 }
