@@ -113,32 +113,37 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
     const float scale2 = a.scale * kLog2e;
     u32x4 kr[D / 32], vr[kDt];
     const long stride = (long)a.page * D;  // of a head's page
-    int id0 = 0, id1 = 0;  // pages of the tile's lower and upper 16 keys
-    auto find = [&](int t) {
-        const int b0 = min(t * kKeys >> lp, a.max_blocks - 1), b1 = min((t * kKeys + 16) >> lp, a.max_blocks - 1);
-        id0 = min(max(table[b0], 0), a.n_pages - 1);
-        id1 = min(max(table[b1], 0), a.n_pages - 1);
-    };
-    auto load_k = [&](int t) {
-        const uint8_t *p = a.k + ((long)(pi & 16 ? id1 : id0) * a.Hkv + kvh) * stride + ((t * kKeys + pi) & (a.page - 1)) * D + 16 * half;
+    // Pages of a tile are read two tiles of the wavefront ahead, its codes and scales one: this half's 16 keys for the
+    // values and the scales, the 16 of key pi for the keys.  Through vector registers: a scalar load would make every wait
+    // for LDS wait for it too.
+    auto page_id = [&](int t, int group) { return table[min((t * kKeys + 16 * group) >> lp, a.max_blocks - 1)]; };
+    auto head = [&](int id) { return (long)min(max(id, 0), a.n_pages - 1) * a.Hkv + kvh; };
+    auto load_k = [&](int t, int id) {
+        const uint8_t *p = a.k + head(id) * stride + ((t * kKeys + pi) & (a.page - 1)) * D + 16 * half;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) kr[i] = *reinterpret_cast<const u32x4 *>(p + 32 * i);
     };
-    auto load_v = [&](int t) {
-        const uint8_t *p = a.v + ((long)(half ? id1 : id0) * a.Hkv + kvh) * stride + ((t * kKeys + 16 * half) & (a.page - 1)) + (long)col * a.page;
+    auto load_v = [&](int t, int id) {
+        const uint8_t *p = a.v + head(id) * stride + ((t * kKeys + 16 * half) & (a.page - 1)) + (long)col * a.page;
 #pragma unroll
         for (int d = 0; d < kDt; ++d) vr[d] = *reinterpret_cast<const u32x4 *>(p + (long)(32 * d) * a.page);
     };
     const int end = min(it.last, cached);
-    int t = it.first + wave;
+    int t = it.first + wave, k_id = 0, v_id = 0;
+    float ks_next = 0.f, vs_next = 0.f;
     if (t < end) {
-        find(t);
-        load_k(t);
-        load_v(t);
+        k_id = page_id(t, pi >> 4);
+        v_id = page_id(t, half);
+        load_k(t, k_id);
+        load_v(t, v_id);
+        ks_next = a.k_scale[head(v_id)];
+        vs_next = a.v_scale[head(v_id)];
+        k_id = page_id(min(t + kWaves, end - 1), pi >> 4);
+        v_id = page_id(min(t + kWaves, end - 1), half);
     }
     for (; t < end; t += kWaves) {
-        const float ks = a.k_scale[(long)(half ? id1 : id0) * a.Hkv + kvh] * scale2;
-        float vs = a.v_scale[(long)(half ? id1 : id0) * a.Hkv + kvh];
+        const float ks = ks_next * scale2;
+        float vs = vs_next;
         const int next = t + kWaves;
         const int left = it.len - t * kKeys - 16 * half;  // of this half's 16 keys
         f32x16 s[RT];
@@ -165,9 +170,13 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
                     vr[d][w] &= n >= 4 ? ~0u : n <= 0 ? 0u : (1u << 8 * n) - 1;
                 }
         }
+        const int id = v_id;
         if (next < end) {
-            find(next);
-            load_k(next);
+            load_k(next, k_id);
+            ks_next = a.k_scale[head(id)];
+            vs_next = a.v_scale[head(id)];
+            k_id = page_id(min(next + kWaves, end - 1), pi >> 4);
+            v_id = page_id(min(next + kWaves, end - 1), half);
         }
         bf16x8 p[RT][2];
 #pragma unroll
@@ -192,7 +201,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) o[rt][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[rt][h], o[rt][d], 0, 0, 0);
             }
-        if (next < end) load_v(next);
+        if (next < end) load_v(next, id);
     }
 
     // ---- drafts

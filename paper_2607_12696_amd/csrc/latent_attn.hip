@@ -23,7 +23,7 @@ constexpr int kRowBytes = kW * 2, kChunks = kRowBytes / 16;  // 72 chunks of 16 
 constexpr int kTile = kKeys * kRowBytes;                     // 36864
 constexpr int kSteps = kW / 16;
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
-constexpr int kAhead = 4;       // operands of a group of score products, read while the group before runs
+constexpr int kAhead = 4, kRing = 3;  // operands of a group of score products; groups in registers, running or being read
 constexpr float kSlack = 8.f;  // powers of two by which weights may outgrow their reference before sums are scaled down
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
@@ -95,11 +95,15 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
         const int i = n * 64 + lane, r = i / kChunks, c = i % kChunks;
         src[n] = (uint32_t)(r * kRowBytes + (c ^ r) * 16);
     }
+    // The page of the rows of tile t, unclamped: read a tile ahead, through a vector register, because a scalar load
+    // would make every wait for LDS wait for it too.
     auto page_id = [&](int t) {
-        const int key = max(min(t * kKeys + row8, it.len - 1), 0);
-        return min(max(table[key >> lp], 0), a.n_pages - 1);
+        int block = max(min(t * kKeys + row8, it.len - 1), 0) >> lp;
+        asm volatile("" : "+v"(block));
+        return table[block];
     };
     auto load = [&](int t, int id, int buf) {
+        id = __builtin_amdgcn_readfirstlane(min(max(id, 0), a.n_pages - 1));
         int key, rows;
         const uint16_t *base;
         if (t < cached) {
@@ -113,25 +117,16 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
         }
         const u32x4 rsrc = rsrc_words(base, (uint32_t)(rows * kRowBytes));
         const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(lds.tile[buf]) + row8 * kRowBytes);
-        if (rows == 8) {
 #pragma unroll
-            for (int n = 0; n < 9; ++n) load16_lds(rsrc, src[n], dst + n * 1024);
-        } else {  // rows past the end repeat the last one
-#pragma unroll
-            for (int n = 0; n < 9; ++n) {
-                const uint32_t r = src[n] / kRowBytes;
-                load16_lds(rsrc, src[n] - (r - min(r, (uint32_t)(rows - 1))) * kRowBytes, dst + n * 1024);
-            }
-        }
+        for (int n = 0; n < 9; ++n) load16_lds(rsrc, src[n], dst + n * 1024);  // rows past the end: zeros
     };
 
     int next_id = it.first < cached ? page_id(it.first) : 0;
-    load(it.first, next_id, 0);
-    if (it.first + 1 < it.last) {
-        if (it.first + 1 < cached) next_id = page_id(it.first + 1);
-        load(it.first + 1, next_id, 1);
+#pragma unroll 1
+    for (int t = it.first; t < min(it.first + 2, it.last); ++t) {
+        load(t, next_id, t - it.first);
+        if (t + 1 < cached) next_id = page_id(t + 1);
     }
-    if (it.first + 2 < cached) next_id = page_id(it.first + 2);
 
     // ---- queries of the wavefront's 32 rows
     bf16x8 q[kSteps];
@@ -169,24 +164,26 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
     // Scores of tile t, in powers of two; register i is key 8 (i / 4) + 4 half + i % 4.
     auto scores = [&](int t, float *x) {
         const char *tile = lds.tile[(t - it.first) % 3];
-        bf16x8 k[2][kAhead];
+        bf16x8 k[kRing][kAhead];
         auto fetch = [&](int g) {
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 const int st = g * kAhead + i;
-                k[g & 1][i] = *reinterpret_cast<const bf16x8 *>(tile + k_at[st % 4] + st / 4 * 128);
+                k[g % kRing][i] = *reinterpret_cast<const bf16x8 *>(tile + k_at[st % 4] + st / 4 * 128);
             }
         };
-        fetch(0);
+        constexpr int kGroups = kSteps / kAhead;
+#pragma unroll
+        for (int g = 0; g < kRing - 1; ++g) fetch(g);
         f32x16 s;
 #pragma unroll
-        for (int g = 0; g < kSteps / kAhead; ++g) {
-            if (g + 1 < kSteps / kAhead) fetch(g + 1);
+        for (int g = 0; g < kGroups; ++g) {
+            if (g + kRing - 1 < kGroups) fetch(g + kRing - 1);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 if (g == 0 && i == 0) mfma_first(s, k[0][0], q[0]);
-                else mfma_next(s, k[g & 1][i], q[g * kAhead + i]);
+                else mfma_next(s, k[g % kRing][i], q[g * kAhead + i]);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -216,10 +213,11 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
 #pragma unroll
         for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
         top = halves_max(top);
-        const bool move = __any(top > m + kSlack);
+        int move = __any(top > m + kSlack);
+        asm("" : "+v"(move));  // a select, not a branch
         const float now = move ? fmaxf(m, top) : m, base = now == -INFINITY ? 0.f : now;
         const float down = __builtin_amdgcn_exp2f((m == -INFINITY ? base : m) - base);
-        const bool scaled = move && __any(m != -INFINITY);
+        const int scaled = move & __any(m != -INFINITY);
         m = now;
         lds.down[par][32 * wave + col] = down;
         lds.scaled[par][wave] = scaled;
@@ -266,19 +264,39 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
     auto values = [&](int t) {
         const int par = (t - it.first) & 1;
         const char *tile = lds.tile[(t - it.first) % 3];
+        bf16x8 w[2][4], v[2];
+        auto fetch_w = [&](int st) {
 #pragma unroll
-        for (int st = 0; st < 2; ++st) {
-            bf16x8 w[4];
+            for (int rt = 0; rt < 4; ++rt) w[st][rt] = __builtin_bit_cast(bf16x8, lds.p[par][rt][st][lane]);
+        };
+        auto fetch_v = [&](int g) {
+            const char *p = tile + v_at[g % 2] + g % 4 / 2 * 128 + g / 4 * 16 * kRowBytes;
+            const u32x2 lo = read_tr(p), hi = read_tr(p + 8 * kRowBytes);
+            v[g % 2] = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+        };
+        fetch_w(0);
+        fetch_v(0);
+        fetch_v(1);
+        fetch_w(1);
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt) w[rt] = __builtin_bit_cast(bf16x8, lds.p[par][rt][st][lane]);
+        for (int g = 0; g < 8; ++g) {
 #pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                const char *p = tile + v_at[d % 2] + d / 2 * 128 + st * 16 * kRowBytes;
-                const u32x2 lo = read_tr(p), hi = read_tr(p + 8 * kRowBytes);
-                const bf16x8 v = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+            for (int rt = 0; rt < 4; ++rt) o[rt][g % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[g % 2], w[g / 4][rt], o[rt][g % 4], 0, 0, 0);
+            if (g + 2 < 8) fetch_v(g + 2);
+        }
+    };
+    // Order of the instructions of values() and weights() in one block: operands two groups of products ahead, and the
+    // softmax in the time that the products take.
+    auto interleave = [] {
+        __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
 #pragma unroll
-                for (int rt = 0; rt < 4; ++rt) o[rt][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[rt], o[rt][d], 0, 0, 0);
+        for (int g = 0; g < 8; ++g) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
             }
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         }
     };
     // The loads so far have landed, and every wavefront is past the tile before.
@@ -301,6 +319,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
         rescale(t - 1);
         values(t - 1);
         weights(t, x);
+        interleave();
         step();
     }
     rescale(it.last - 1);
@@ -309,56 +328,60 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
     l = halves_sum(l);
     if (half == 0) lds.ml[32 * wave + col] = make_float2(l == 0.f ? -INFINITY : m, l);
     __syncthreads();
-    // What the infinities and NaN of drafts give element el (and the next three) of a row; the weights of a tile of drafts
-    // still lie in LDS.
-    auto add_drafts = [&](int rt, int el, f32x4 &v) {
-        const int r = row0 + 32 * rt + col;
-        if (r >= n_rows) return;
-        const uint64_t sees = (a.mask ? a.mask[it.t0 + r / a.H] : bits_below(r / a.H + 1)) & bits_below(drafts);
-        for (int j = 0; j < drafts; ++j) {
-            const int t = j / kKeys, k = j % kKeys;
-            if (!(not_finite_drafts >> t & 1) || !(sees >> j & 1)) continue;
-            const u32x4 &p = lds.p[(cached + t - it.first) & 1][rt][k / 16][k / 4 % 2 * 32 + col];
-            const float w = bf16_bits_to_f32(reinterpret_cast<const uint16_t *>(&p)[k / 8 % 2 * 4 + k % 4]);
-            for (int i = 0; i < 4; ++i) {
-                const uint16_t c = a.kv_new[(long)(it.t0 + j) * kW + el + i];
-                if (not_finite(c)) v[i] = fmaf(w, bf16_bits_to_f32(c), v[i]);
-            }
-        }
-    };
-    if (it.chunks > 1) {
-        f32x4 *out = reinterpret_cast<f32x4 *>(parts.o) + (long)it.slot * 64 * 256;
+    const bool part = it.chunks > 1;
+    float *part_o = parts.o + (long)it.slot * kRows * kR;
+    if (part) {
+        f32x4 *out = reinterpret_cast<f32x4 *>(part_o);
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt)
 #pragma unroll
             for (int d = 0; d < 4; ++d)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    f32x4 v = {o[rt][d][4 * i], o[rt][d][4 * i + 1], o[rt][d][4 * i + 2], o[rt][d][4 * i + 3]};
-                    if (not_finite_drafts) add_drafts(rt, 128 * wave + 32 * d + 8 * i + 4 * half, v);
-                    out[(rt * 16 + 4 * wave + d) * 256 + i * 64 + lane] = v;
-                }
+                for (int i = 0; i < 4; ++i)
+                    out[(rt * 16 + 4 * wave + d) * 256 + i * 64 + lane] =
+                        f32x4{o[rt][d][4 * i], o[rt][d][4 * i + 1], o[rt][d][4 * i + 2], o[rt][d][4 * i + 3]};
         if (threadIdx.x < kRows) parts.ml[(long)it.slot * kRows + threadIdx.x] = lds.ml[threadIdx.x];
-        return;
+    } else {
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt) {
+            const int r = row0 + 32 * rt + col;
+            if (r >= n_rows) continue;
+            const long at = (long)it.t0 * a.H + r;
+            const float2 ml = lds.ml[32 * rt + col];
+            const float inv = ml.y == 0.f ? 0.f : 1.f / ml.y;
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<u32x2 *>(a.o + at * kR + 128 * wave + 32 * d + 8 * i + 4 * half) =
+                        u32x2{pack_bf16x2(o[rt][d][4 * i] * inv, o[rt][d][4 * i + 1] * inv),
+                              pack_bf16x2(o[rt][d][4 * i + 2] * inv, o[rt][d][4 * i + 3] * inv)};
+            if (a.lse && wave == 0 && half == 0) a.lse[at] = ml.y == 0.f ? -INFINITY : (ml.x + __builtin_amdgcn_logf(ml.y)) / kLog2e;
+        }
     }
-#pragma unroll
-    for (int rt = 0; rt < 4; ++rt) {
-        const int r = row0 + 32 * rt + col;
-        if (r >= n_rows) continue;
-        const long at = (long)(it.t0 + r / a.H) * a.H + r % a.H;
-        const float2 ml = lds.ml[32 * rt + col];
-        const float inv = ml.y == 0.f ? 0.f : 1.f / ml.y;
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int el = 128 * wave + 32 * d + 8 * i + 4 * half;
-                f32x4 v = {o[rt][d][4 * i], o[rt][d][4 * i + 1], o[rt][d][4 * i + 2], o[rt][d][4 * i + 3]};
-                if (not_finite_drafts) add_drafts(rt, el, v);
-                *reinterpret_cast<u32x2 *>(a.o + at * kR + el) =
-                    u32x2{pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv)};
-            }
-        if (a.lse && wave == 0 && half == 0) a.lse[at] = ml.y == 0.f ? -INFINITY : (ml.x + __builtin_amdgcn_logf(ml.y)) / kLog2e;
+    if (!not_finite_drafts) return;
+    // What the infinities and NaN of drafts give the rows that see them, added to what was just written; the weights of the
+    // draft tiles still lie in LDS.
+    __syncthreads();
+    for (int i = threadIdx.x; i < kRows * kR; i += kThreads) {
+        const int row = i / kR, el = i % kR, r = row0 + row;
+        if (r >= n_rows) break;
+        const uint64_t sees = (a.mask ? a.mask[it.t0 + r / a.H] : bits_below(r / a.H + 1)) & bits_below(drafts);
+        float c = 0.f;
+        for (int j = 0; j < drafts; ++j) {
+            const int t = j / kKeys, k = j % kKeys;
+            const uint16_t v = a.kv_new[(long)(it.t0 + j) * kW + el];
+            if (!(not_finite_drafts >> t & 1) || !(sees >> j & 1) || !not_finite(v)) continue;
+            const u32x4 &p = lds.p[(cached + t - it.first) & 1][row / 32][k / 16][k / 4 % 2 * 32 + row % 32];
+            c = fmaf(bf16_bits_to_f32(reinterpret_cast<const uint16_t *>(&p)[k / 8 % 2 * 4 + k % 4]), bf16_bits_to_f32(v), c);
+        }
+        if (c == 0.f) continue;
+        if (part) {
+            part_o[((row / 32 * 16 + el / 32) * 256 + el % 32 / 8 * 64 + el / 4 % 2 * 32 + row % 32) * 4 + el % 4] += c;
+        } else {
+            uint16_t *p = a.o + ((long)it.t0 * a.H + r) * kR + el;
+            *p = f32_to_bf16_bits(bf16_bits_to_f32(*p) + c);
+        }
     }
 }
 
