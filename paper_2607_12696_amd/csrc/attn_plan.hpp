@@ -76,11 +76,11 @@ inline size_t parts_at(void *workspace, long groups, int slots, int rows, int wi
 
 __device__ __forceinline__ int wave_sum_int(int v) { return __builtin_amdgcn_readlane(wave_inclusive_sum(v), 63); }
 
+// Sum of values up to 2^40, in two halves for the lane moves.
 __device__ __forceinline__ long wave_sum_long(long v)
 {
-#pragma unroll
-    for (int s = 32; s >= 1; s >>= 1) v += __shfl_xor(v, s, kWave);
-    return v;
+    v = v < (1L << 40) ? v : 1L << 40;
+    return ((long)wave_sum_int((int)(v >> 16)) << 16) + wave_sum_int((int)(v & 0xffff));
 }
 
 // This workgroup's item.  work: 2 * B ints of LDS, free again after the call's last barrier.  per_token: query rows of a

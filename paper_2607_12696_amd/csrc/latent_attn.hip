@@ -18,15 +18,21 @@ namespace ecospec {
 namespace {
 
 constexpr int kR = 512, kW = 576;
-constexpr int kRows = 128, kKeys = 32;
+constexpr int kRows = 128, kKeys = 32;  // at most
 constexpr int kRowBytes = kW * 2, kChunks = kRowBytes / 16;  // 72 chunks of 16 bytes
 constexpr int kTile = kKeys * kRowBytes;                     // 36864
 constexpr int kSteps = kW / 16;
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
 constexpr int kAhead = 4, kRing = 3;  // operands of a group of score products; groups in registers, running or being read
+constexpr int kLoadEvery = 2;
 constexpr float kSlack = 8.f;  // powers of two by which weights may outgrow their reference before sums are scaled down
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
+
+// LDS has 64 banks and reads 256 bytes a cycle.  Chunk c of row r lies at place c ^ twist(r) of its row: rows are 72 chunks,
+// so that two rows with the same place are half the banks apart, and the twist keeps 16 consecutive rows' chunks c (a
+// quarter of a read of keys) and 4 rows' four neighbouring chunks (half a read of values) in different banks.
+__device__ __forceinline__ uint32_t twist(uint32_t r) { return (r >> 1 & 1) << 2 | (r >> 2 & 3); }
 
 __device__ __forceinline__ u32x2 read_tr(const char *p)
 {
@@ -63,20 +69,30 @@ __device__ __forceinline__ void mfma_next(f32x16 &s, const bf16x8 &a, const bf16
     asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "v"(b));
 }
 
-__device__ __forceinline__ void mfma_wait(f32x16 &s) { asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s)); }
+__device__ __forceinline__ void mfma_wait(f32x16 &s, f32x16 &t) { asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s), "+v"(t)); }
 
 __device__ __forceinline__ bool not_finite(uint32_t bf16) { return (bf16 & 0x7f80u) == 0x7f80u; }
 
-struct Lds {
-    char tile[3][kTile];
-    u32x4 p[2][4][2][kWave];  // weights: tile parity, row tile of 32, reduction step of 16 keys, lane
+struct Weights {
+    u32x4 p[2][4][2][kWave];  // tile parity, row tile of 32, reduction step of 16 keys, lane
     float down[2][kRows];     // what the sums of a row are multiplied by before the tile is added
-    int scaled[2][kWaves];    // whether that is anything but 1 for a row tile
+    int scaled[2][4];         // whether that is anything but 1 for a row tile
     float2 ml[kRows];
 };
 
+union Lds {
+    char rows[4][kTile];  // the queries of each wavefront, before the loop
+    struct {
+        char tile[3][kTile];
+        Weights w;
+    };
+};
+
+// RT: row tiles of 32 rows that the workgroup has, wavefront w scoring tile w (fewer than four where a call has few rows).
+template <int RT>
 __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, Shape shape, Parts parts)
 {
+    constexpr int kRows = 32 * RT;
     __shared__ __attribute__((aligned(16))) Lds lds;
     Item it;
     if (!plan_item(a, a.H, 1, shape, parts, reinterpret_cast<int *>(lds.tile), it)) return;
@@ -86,14 +102,16 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
     const int *table = a.block_table + (long)it.b * a.max_blocks;
     const int lp = 31 - __builtin_clz(a.page);
     const int cached = (it.len + kKeys - 1) / kKeys, drafts = min(it.n_tok, kMaxDrafts);
+    const bool scoring = RT == 4 || wave < RT;
 
-    // ---- tiles: wavefront w brings rows 8 w .. 8 w + 7, nine loads of 64 chunks; they lie in one page.
+    // ---- rows to LDS: nine loads of 64 chunks bring eight rows.  Wavefront w brings rows 8 w .. 8 w + 7 of a tile, which
+    // lie in one page.  Rows past the end become zeros.
     const int row8 = 8 * wave;
     uint32_t src[9];  // lane's byte offset from the first row
 #pragma unroll
     for (int n = 0; n < 9; ++n) {
         const int i = n * 64 + lane, r = i / kChunks, c = i % kChunks;
-        src[n] = (uint32_t)(r * kRowBytes + (c ^ r) * 16);
+        src[n] = (uint32_t)(r * kRowBytes + (c ^ twist(r + row8)) * 16);
     }
     // The page of the rows of tile t, unclamped: read a tile ahead, through a vector register, because a scalar load
     // would make every wait for LDS wait for it too.
@@ -102,11 +120,16 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
         asm volatile("" : "+v"(block));
         return table[block];
     };
-    auto load = [&](int t, int id, int buf) {
-        id = __builtin_amdgcn_readfirstlane(min(max(id, 0), a.n_pages - 1));
+    u32x4 rsrc;
+    uint32_t dst;
+    auto aim = [&](int t, int id) {  // the loads of tile t; past the chunk they bring nothing but zeros
         int key, rows;
         const uint16_t *base;
-        if (t < cached) {
+        if (t >= it.last) {
+            rows = 0;
+            base = a.q;
+        } else if (t < cached) {
+            id = __builtin_amdgcn_readfirstlane(min(max(id, 0), a.n_pages - 1));
             key = min(t * kKeys + row8, it.len - 1);
             rows = min(it.len - key, 8);
             base = a.pages + ((long)id * a.page + (key & (a.page - 1))) * kW;
@@ -115,33 +138,50 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
             rows = min(drafts - key, 8);
             base = a.kv_new + (long)(it.t0 + key) * kW;
         }
-        const u32x4 rsrc = rsrc_words(base, (uint32_t)(rows * kRowBytes));
-        const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(lds.tile[buf]) + row8 * kRowBytes);
-#pragma unroll
-        for (int n = 0; n < 9; ++n) load16_lds(rsrc, src[n], dst + n * 1024);  // rows past the end: zeros
+        rsrc = rsrc_words(base, (uint32_t)(rows * kRowBytes));
+        dst = __builtin_amdgcn_readfirstlane(lds_addr(lds.tile[(t - it.first) % 3]) + row8 * kRowBytes);
     };
+    auto load = [&](int n) { load16_lds(rsrc, src[n], dst + n * 1024); };
 
-    int next_id = it.first < cached ? page_id(it.first) : 0;
-#pragma unroll 1
-    for (int t = it.first; t < min(it.first + 2, it.last); ++t) {
-        load(t, next_id, t - it.first);
-        if (t + 1 < cached) next_id = page_id(t + 1);
-    }
-
-    // ---- queries of the wavefront's 32 rows
-    bf16x8 q[kSteps];
+    // Lane offsets of the LDS reads: keys (and queries), by the step's low bits; values, by the element tile's low bit.
+    uint32_t k_at[4], v_at[2];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) k_at[s] = (uint32_t)(col * kRowBytes + ((2 * s + half) ^ twist(col)) * 16);
     {
-        const int r = row0 + 32 * wave + col;
-        const bool in = r < n_rows;
-        const int tok = in ? r / a.H : 0;
-        const uint16_t *p = a.q + ((long)(it.t0 + tok) * a.H + (in ? r % a.H : 0)) * kW + 8 * half;
+        const int i = lane % 16, key = 4 * half + i / 4;
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) q[s] = *reinterpret_cast<const bf16x8 *>(p + 16 * s);
+        for (int d = 0; d < 2; ++d)
+            v_at[d] = (uint32_t)(key * kRowBytes + ((((4 * d + lane / 16 % 2 * 2 + i % 4 / 2) ^ twist(key)) + 16 * wave) * 16) + i % 2 * 8);
     }
 
-    f32x16 o[4][4];  // row tile, element tile
+    // ---- queries of the wavefront's 32 rows, consecutive in memory, through LDS
+    int next_id = it.first < cached ? page_id(it.first) : 0;
+    bf16x8 q[kSteps];
+    if (scoring) {
+        const int r = row0 + 32 * wave, rows = max(min(n_rows - r, 32), 0);
+        const u32x4 from = rsrc_words(a.q + ((long)it.t0 * a.H + min(r, n_rows - 1)) * kW, (uint32_t)(rows * kRowBytes));
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds_addr(lds.rows[wave]));
+#pragma unroll 1
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
-    for (int rt = 0; rt < 4; ++rt)
+            for (int n = 0; n < 9; ++n)  // src is for the wavefront's rows of a tile: twist(r + 8) again
+                load16_lds(from, (src[n] ^ ((e ^ wave) & 1) * 32) + e * 8 * kRowBytes, to + e * 8 * kRowBytes + n * 1024);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) q[s] = *reinterpret_cast<const bf16x8 *>(lds.rows[wave] + k_at[s % 4] + s / 4 * 128);
+    }
+    __syncthreads();
+    auto aim_next = [&](int t) {
+        aim(t, next_id);
+        if (t + 1 < cached) next_id = page_id(t + 1);
+    };
+    aim_next(it.first);
+#pragma unroll
+    for (int n = 0; n < 9; ++n) load(n);
+
+    f32x16 o[RT][4];  // row tile, element tile
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -149,19 +189,10 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
     float m = -INFINITY, l = 0.f;
     int not_finite_drafts = 0;  // bit: draft tile
     const float scale2 = a.scale * kLog2e;
+    Weights &ws = lds.w;
 
-    // Lane offsets of the LDS reads: keys, by the step's low bits; values, by the element tile's low bit.
-    uint32_t k_at[4], v_at[2];
-#pragma unroll
-    for (int s = 0; s < 4; ++s) k_at[s] = (uint32_t)(col * kRowBytes + ((2 * s + half) ^ (col & 7)) * 16);
-    {
-        const int i = lane % 16, key = 4 * half + i / 4;
-#pragma unroll
-        for (int d = 0; d < 2; ++d)
-            v_at[d] = (uint32_t)(key * kRowBytes + ((((4 * d + lane / 16 % 2 * 2 + i % 4 / 2) ^ key) + 16 * wave) * 16) + i % 2 * 8);
-    }
-
-    // Scores of tile t, in powers of two; register i is key 8 (i / 4) + 4 half + i % 4.
+    // Scores of tile t, in powers of two; register i is key 8 (i / 4) + 4 half + i % 4.  Even and odd steps are summed
+    // apart.
     auto scores = [&](int t, float *x) {
         const char *tile = lds.tile[(t - it.first) % 3];
         bf16x8 k[kRing][kAhead];
@@ -175,21 +206,21 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
         constexpr int kGroups = kSteps / kAhead;
 #pragma unroll
         for (int g = 0; g < kRing - 1; ++g) fetch(g);
-        f32x16 s;
+        f32x16 s[2];
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
             if (g + kRing - 1 < kGroups) fetch(g + kRing - 1);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                if (g == 0 && i == 0) mfma_first(s, k[0][0], q[0]);
-                else mfma_next(s, k[g % kRing][i], q[g * kAhead + i]);
+                if (g == 0 && i < 2) mfma_first(s[i], k[0][i], q[i]);
+                else mfma_next(s[i % 2], k[g % kRing][i], q[g * kAhead + i]);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        mfma_wait(s);
+        mfma_wait(s[0], s[1]);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = s[i] * scale2;
+        for (int i = 0; i < 16; ++i) x[i] = (s[0][i] + s[1][i]) * scale2;
         if (t >= cached) {
             const int r = row0 + 32 * wave + col;
             uint64_t see = 0;
@@ -205,41 +236,48 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
                 if (i / 4 * 8 + i % 4 >= left) x[i] = -INFINITY;
         }
     };
-    // Weights of the scores x of tile t, the running maximum and sum, and what the sums so far are scaled by; no branch,
-    // so that it can run between the products of values().
-    auto weights = [&](int t, float *x) {
+    // Weights of the scores x of tile t, the running maximum and sum, and what the sums so far are scaled by: 32 pieces
+    // without a branch, to run one behind each value product.
+    float top, base, down, sum;
+    auto weights = [&](int t, float *x, int piece) {
         const int par = (t - it.first) & 1;
-        float top = x[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
-        top = halves_max(top);
-        int move = __any(top > m + kSlack);
-        asm("" : "+v"(move));  // a select, not a branch
-        const float now = move ? fmaxf(m, top) : m, base = now == -INFINITY ? 0.f : now;
-        const float down = __builtin_amdgcn_exp2f((m == -INFINITY ? base : m) - base);
-        const int scaled = move & __any(m != -INFINITY);
-        m = now;
-        lds.down[par][32 * wave + col] = down;
-        lds.scaled[par][wave] = scaled;
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
+        if (piece == 0) top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), x[6]));
+        if (piece == 1) top = fmaxf(top, fmaxf(fmaxf(fmaxf(x[7], x[8]), fmaxf(x[9], x[10])), fmaxf(x[11], x[12])));
+        if (piece == 2) top = halves_max(fmaxf(top, fmaxf(fmaxf(x[13], x[14]), x[15])));
+        if (piece == 3) {
+            int move = __any(top > m + kSlack);
+            const int scaled = move & __any(m != -INFINITY);
+            asm("" : "+v"(move));  // a select, not a branch
+            const float now = move ? fmaxf(m, top) : m;
+            base = now == -INFINITY ? 0.f : now;
+            down = (m == -INFINITY ? base : m) - base;
+            m = now;
+            ws.scaled[par][wave] = scaled;
+        }
+        if (piece == 4) {
+            down = __builtin_amdgcn_exp2f(down);
+            ws.down[par][32 * wave + col] = down;
+            sum = 0.f;
+        }
+        if (piece >= 5 && piece < 21) {
+            const int i = piece - 5;
             x[i] = __builtin_amdgcn_exp2f(x[i] - base);
             sum += x[i];
         }
-        l = fmaf(l, down, sum);
-        lds.p[par][wave][0][lane] = __builtin_bit_cast(u32x4, pack_bf16x8(x));
-        lds.p[par][wave][1][lane] = __builtin_bit_cast(u32x4, pack_bf16x8(x + 8));
+        if (piece == 21) ws.p[par][wave][0][lane] = __builtin_bit_cast(u32x4, pack_bf16x8(x));
+        if (piece == 22) ws.p[par][wave][1][lane] = __builtin_bit_cast(u32x4, pack_bf16x8(x + 8));
+        if (piece == 23) l = fmaf(l, down, sum);
     };
-    // Before tile t's values are added.
-    auto rescale = [&](int t) {
+    // Whether the sums have to be scaled before tile t's values are added: read early.
+    auto flags = [&](int t) { return *reinterpret_cast<const u32x4 *>(ws.scaled[(t - it.first) & 1]); };
+    auto rescale = [&](int t, u32x4 scaled) {
         const int par = (t - it.first) & 1;
 #pragma unroll
-        for (int rt = 0; rt < 4; ++rt)
-            if (__builtin_amdgcn_readfirstlane(lds.scaled[par][rt])) {
-                const float down = lds.down[par][32 * rt + col];
+        for (int rt = 0; rt < RT; ++rt)
+            if (__builtin_amdgcn_readfirstlane(scaled[rt])) {
+                const float f = ws.down[par][32 * rt + col];
 #pragma unroll
-                for (int d = 0; d < 4; ++d) acc_scale(o[rt][d], down);
+                for (int d = 0; d < 4; ++d) acc_scale(o[rt][d], f);
             }
         if (t >= cached) {
             // A weight of zero must not meet an infinity or NaN: where a draft has one, zeros take its place, and what it
@@ -261,17 +299,18 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
             if (__syncthreads_or(odd)) not_finite_drafts |= 1 << (t - cached);
         }
     };
-    auto values = [&](int t) {
+    // Adds tile t's values; `between(c)` runs behind product c of 8 * RT.
+    auto values = [&](int t, auto between) {
         const int par = (t - it.first) & 1;
         const char *tile = lds.tile[(t - it.first) % 3];
-        bf16x8 w[2][4], v[2];
+        bf16x8 w[2][RT], v[2];
         auto fetch_w = [&](int st) {
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt) w[st][rt] = __builtin_bit_cast(bf16x8, lds.p[par][rt][st][lane]);
+            for (int rt = 0; rt < RT; ++rt) w[st][rt] = __builtin_bit_cast(bf16x8, ws.p[par][rt][st][lane]);
         };
         auto fetch_v = [&](int g) {
-            const char *p = tile + v_at[g % 2] + g % 4 / 2 * 128 + g / 4 * 16 * kRowBytes;
-            const u32x2 lo = read_tr(p), hi = read_tr(p + 8 * kRowBytes);
+            const char *p = tile + g % 4 / 2 * 128 + g / 4 * 16 * kRowBytes;
+            const u32x2 lo = read_tr(p + v_at[g % 2]), hi = read_tr(p + (v_at[g % 2] ^ 32) + 8 * kRowBytes);  // twist(r + 8)
             v[g % 2] = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
         };
         fetch_w(0);
@@ -281,73 +320,80 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
 #pragma unroll
         for (int g = 0; g < 8; ++g) {
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt) o[rt][g % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[g % 2], w[g / 4][rt], o[rt][g % 4], 0, 0, 0);
+            for (int rt = 0; rt < RT; ++rt) {
+                __builtin_amdgcn_sched_barrier(0);
+                o[rt][g % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[g % 2], w[g / 4][rt], o[rt][g % 4], 0, 0, 0);
+                between(g * RT + rt);
+            }
             if (g + 2 < 8) fetch_v(g + 2);
         }
-    };
-    // Order of the instructions of values() and weights() in one block: operands two groups of products ahead, and the
-    // softmax in the time that the products take.
-    auto interleave = [] {
-        __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
-#pragma unroll
-        for (int g = 0; g < 8; ++g) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-        }
+        __builtin_amdgcn_sched_barrier(0);
     };
     // The loads so far have landed, and every wavefront is past the tile before.
     auto step = [] {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
     };
+    auto all_weights = [&](int t, float *x) {
+#pragma unroll
+        for (int c = 0; c < 24; ++c) weights(t, x, c);
+    };
 
     step();
     float x[16];
-    scores(it.first, x);
-    weights(it.first, x);
+    if (scoring) {
+        scores(it.first, x);
+        all_weights(it.first, x);
+    }
+    aim_next(it.first + 1);
+#pragma unroll
+    for (int n = 0; n < 9; ++n) load(n);
     step();
     for (int t = it.first + 1; t < it.last; ++t) {
-        if (t + 1 < it.last) {
-            load(t + 1, next_id, (t + 1 - it.first) % 3);
-            if (t + 2 < cached) next_id = page_id(t + 2);
+        aim_next(t + 1);
+        const u32x4 scaled = flags(t - 1);
+        if (scoring) scores(t, x);
+        rescale(t - 1, scaled);
+        // The next tile's loads go out between the value products, which leave LDS time for them.
+        if (RT == 4) {
+            values(t - 1, [&](int c) {
+                if (c % kLoadEvery == 0 && c / kLoadEvery < 9) load(c / kLoadEvery);
+                weights(t, x, c);
+            });
+        } else {
+#pragma unroll
+            for (int n = 0; n < 9; ++n) load(n);
+            if (scoring) all_weights(t, x);
+            values(t - 1, [](int) {});
         }
-        scores(t, x);
-        rescale(t - 1);
-        values(t - 1);
-        weights(t, x);
-        interleave();
         step();
     }
-    rescale(it.last - 1);
-    values(it.last - 1);
+    rescale(it.last - 1, flags(it.last - 1));
+    values(it.last - 1, [](int) {});
 
     l = halves_sum(l);
-    if (half == 0) lds.ml[32 * wave + col] = make_float2(l == 0.f ? -INFINITY : m, l);
+    if (scoring && half == 0) ws.ml[32 * wave + col] = make_float2(l == 0.f ? -INFINITY : m, l);
     __syncthreads();
     const bool part = it.chunks > 1;
     float *part_o = parts.o + (long)it.slot * kRows * kR;
     if (part) {
         f32x4 *out = reinterpret_cast<f32x4 *>(part_o);
 #pragma unroll
-        for (int rt = 0; rt < 4; ++rt)
+        for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
             for (int d = 0; d < 4; ++d)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     out[(rt * 16 + 4 * wave + d) * 256 + i * 64 + lane] =
                         f32x4{o[rt][d][4 * i], o[rt][d][4 * i + 1], o[rt][d][4 * i + 2], o[rt][d][4 * i + 3]};
-        if (threadIdx.x < kRows) parts.ml[(long)it.slot * kRows + threadIdx.x] = lds.ml[threadIdx.x];
+        if (threadIdx.x < kRows) parts.ml[(long)it.slot * kRows + threadIdx.x] = ws.ml[threadIdx.x];
     } else {
 #pragma unroll
-        for (int rt = 0; rt < 4; ++rt) {
+        for (int rt = 0; rt < RT; ++rt) {
             const int r = row0 + 32 * rt + col;
             if (r >= n_rows) continue;
             const long at = (long)it.t0 * a.H + r;
-            const float2 ml = lds.ml[32 * rt + col];
+            const float2 ml = ws.ml[32 * rt + col];
             const float inv = ml.y == 0.f ? 0.f : 1.f / ml.y;
 #pragma unroll
             for (int d = 0; d < 4; ++d)
@@ -372,7 +418,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
             const int t = j / kKeys, k = j % kKeys;
             const uint16_t v = a.kv_new[(long)(it.t0 + j) * kW + el];
             if (!(not_finite_drafts >> t & 1) || !(sees >> j & 1) || !not_finite(v)) continue;
-            const u32x4 &p = lds.p[(cached + t - it.first) & 1][row / 32][k / 16][k / 4 % 2 * 32 + row % 32];
+            const u32x4 &p = ws.p[(cached + t - it.first) & 1][row / 32][k / 16][k / 4 % 2 * 32 + row % 32];
             c = fmaf(bf16_bits_to_f32(reinterpret_cast<const uint16_t *>(&p)[k / 8 % 2 * 4 + k % 4]), bf16_bits_to_f32(v), c);
         }
         if (c == 0.f) continue;
@@ -385,18 +431,40 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
     }
 }
 
-}  // namespace
-
-size_t latent_workspace(int N, int B, int H) { return parts_at(nullptr, group_bound(N, B, H, 1, kRows), kCus, kRows, kR, nullptr); }
-
-hipError_t launch_latent_attn(const LatentArgs &a, void *workspace, hipStream_t stream)
+// Row tiles of a workgroup: as few as hold the average sequence's rows.
+int row_tiles(int N, int B, int H)
 {
+    const long rows = (long)N * H;
+    return rows <= 32L * B ? 1 : rows <= 64L * B ? 2 : 4;
+}
+
+template <int RT>
+hipError_t launch(const LatentArgs &a, void *workspace, hipStream_t stream)
+{
+    constexpr int kRows = 32 * RT;
     const long groups = group_bound(a.N, a.B, a.H, 1, kRows);
     Parts parts;
     parts_at(workspace, groups, kCus, kRows, kR, &parts);
-    latent_attn_kernel<<<(unsigned)grid_bound(groups, kCus), kThreads, 0, stream>>>(a, Shape{kRows, kKeys, 2, kCus}, parts);
-    join_kernel<kRows, kR><<<(unsigned)(groups * (kRows / 32) * (kR / 32)), 256, 0, stream>>>(a, a.H, parts);
+    latent_attn_kernel<RT><<<(unsigned)grid_bound(groups, kCus), kThreads, 0, stream>>>(a, Shape{kRows, kKeys, 2, kCus}, parts);
+    join_kernel<kRows, kR><<<(unsigned)(groups * RT * (kR / 32)), 256, 0, stream>>>(a, a.H, parts);
     return hipGetLastError();
+}
+
+}  // namespace
+
+size_t latent_workspace(int N, int B, int H)
+{
+    const int rows = 32 * row_tiles(N, B, H);
+    return parts_at(nullptr, group_bound(N, B, H, 1, rows), kCus, rows, kR, nullptr);
+}
+
+hipError_t launch_latent_attn(const LatentArgs &a, void *workspace, hipStream_t stream)
+{
+    switch (row_tiles(a.N, a.B, a.H)) {
+    case 1: return launch<1>(a, workspace, stream);
+    case 2: return launch<2>(a, workspace, stream);
+    default: return launch<4>(a, workspace, stream);
+    }
 }
 
 }  // namespace ecospec
