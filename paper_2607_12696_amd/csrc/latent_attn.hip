@@ -23,7 +23,7 @@ constexpr int kRowBytes = kW * 2, kChunks = kRowBytes / 16;  // 72 chunks of 16 
 constexpr int kTile = kKeys * kRowBytes;                     // 36864
 constexpr int kSteps = kW / 16;
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
-constexpr int kAhead = 4, kRing = 3;  // operands of a group of score products; groups in registers, running or being read
+constexpr int kAhead = 4, kRing = 2;  // operands of a group of score products; groups in registers, running or being read
 constexpr int kLoadEvery = 2;
 constexpr float kSlack = 8.f;  // powers of two by which weights may outgrow their reference before sums are scaled down
 
@@ -69,7 +69,7 @@ __device__ __forceinline__ void mfma_next(f32x16 &s, const bf16x8 &a, const bf16
     asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "v"(b));
 }
 
-__device__ __forceinline__ void mfma_wait(f32x16 &s, f32x16 &t) { asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s), "+v"(t)); }
+__device__ __forceinline__ void mfma_wait(f32x16 &s) { asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s)); }
 
 __device__ __forceinline__ bool not_finite(uint32_t bf16) { return (bf16 & 0x7f80u) == 0x7f80u; }
 
@@ -191,8 +191,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
     const float scale2 = a.scale * kLog2e;
     Weights &ws = lds.w;
 
-    // Scores of tile t, in powers of two; register i is key 8 (i / 4) + 4 half + i % 4.  Even and odd steps are summed
-    // apart.
+    // Scores of tile t, in powers of two; register i is key 8 (i / 4) + 4 half + i % 4.
     auto scores = [&](int t, float *x) {
         const char *tile = lds.tile[(t - it.first) % 3];
         bf16x8 k[kRing][kAhead];
@@ -206,21 +205,21 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
         constexpr int kGroups = kSteps / kAhead;
 #pragma unroll
         for (int g = 0; g < kRing - 1; ++g) fetch(g);
-        f32x16 s[2];
+        f32x16 s;
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
             if (g + kRing - 1 < kGroups) fetch(g + kRing - 1);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                if (g == 0 && i < 2) mfma_first(s[i], k[0][i], q[i]);
-                else mfma_next(s[i % 2], k[g % kRing][i], q[g * kAhead + i]);
+                if (g == 0 && i == 0) mfma_first(s, k[0][0], q[0]);
+                else mfma_next(s, k[g % kRing][i], q[g * kAhead + i]);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        mfma_wait(s[0], s[1]);
+        mfma_wait(s);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = (s[0][i] + s[1][i]) * scale2;
+        for (int i = 0; i < 16; ++i) x[i] = s[i] * scale2;
         if (t >= cached) {
             const int r = row0 + 32 * wave + col;
             uint64_t see = 0;
@@ -316,7 +315,6 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
         fetch_w(0);
         fetch_v(0);
         fetch_v(1);
-        fetch_w(1);
 #pragma unroll
         for (int g = 0; g < 8; ++g) {
 #pragma unroll
@@ -325,6 +323,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
                 o[rt][g % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[g % 2], w[g / 4][rt], o[rt][g % 4], 0, 0, 0);
                 between(g * RT + rt);
             }
+            if (g == 2) fetch_w(1);
             if (g + 2 < 8) fetch_v(g + 2);
         }
         __builtin_amdgcn_sched_barrier(0);
