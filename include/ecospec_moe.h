@@ -491,7 +491,8 @@ moe_status_t moe_latent_attn(const moe_latent_cache_t *cache, const moe_drafts_t
  * Arithmetic as for moe_latent_attn.  No workspace.
  * Limits: dn = dv = 128, p = 64 (else MOE_ERR_UNSUPPORTED); 1 <= H <= 1024,
  * 1 <= B <= 1024, N, M >= 1, scale finite; strides multiples of 8, 16-byte
- * aligned pointers.
+ * aligned pointers; k_stride, v_stride <= 2^23, N * H <= 2^30 and B * H *
+ * max_tokens <= 2^30 (else MOE_ERR_UNSUPPORTED).
  */
 typedef struct {
     int N, M, B, H, dn, p, dv, max_tokens;

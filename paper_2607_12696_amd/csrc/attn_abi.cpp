@@ -26,6 +26,8 @@ constexpr int kMaxBatch = 1024;
 constexpr int kMaxHeads = 1024;
 constexpr long kMaxRows = 1L << 24;  // query rows (token, head) of a call
 constexpr int kMaxWidth = 16384;     // of a normalised row
+constexpr long kMaxPromptRows = 1L << 30;
+constexpr int64_t kMaxStride = 1L << 23;  // elements between a prompt's keys
 
 bool page_ok(int page) { return page == 16 || page == 32 || page == 64 || page == 128; }
 
@@ -143,7 +145,11 @@ moe_status_t moe_latent_prompt(const moe_prompt_t *p, void *o, float *lse, void 
     const int64_t str[] = {p->k_stride, p->k_head, p->v_stride, p->v_head};
     for (int64_t x : str)
         if (x < 0 || x % 8) return MOE_ERR_INVALID_ARG;
+    // A tile of 64 keys is addressed through a 32-bit buffer range.
+    if (p->k_stride > kMaxStride || p->v_stride > kMaxStride) return MOE_ERR_UNSUPPORTED;
     if (p->dn != 128 || p->p != 64 || p->dv != 128) return MOE_ERR_UNSUPPORTED;
+    const long most = p->max_tokens < p->N ? p->max_tokens : p->N;
+    if ((long)p->N * p->H > kMaxPromptRows || (long)p->B * p->H * most > kMaxPromptRows) return MOE_ERR_UNSUPPORTED;  // the grid
     ecospec::PromptArgs a{};
     a.N = p->N;
     a.M = p->M;
