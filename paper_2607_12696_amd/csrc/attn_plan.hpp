@@ -219,6 +219,13 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int per_token, P
         a.lse[at] = total == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(total)) / kLog2e;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
 // Larger of the two halves' values of a row (lanes l and l ^ 32), and their sum.
 __device__ __forceinline__ float halves_max(float v)
 {
@@ -243,6 +250,23 @@ __device__ __forceinline__ float quads_sum(float v)
 {
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Arithmetic on an accumulator tile where it lies, in the accumulation registers: written out, because the compiler would
+// move all sixteen tiles to vector registers, and those to scratch, for it.  The waits at either end cover the matrix
+// instructions around it (19 wait states from a product's write to a read); the tile as an operand keeps them in place.
+__device__ __forceinline__ void acc_wait(f32x16 &o) { asm volatile("s_nop 15\n\ts_nop 7" : "+a"(o)); }
+
+__device__ __forceinline__ void acc_scale(f32x16 &o, float f)
+{
+    acc_wait(o);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        float x = o[i], t;
+        asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_mul_f32 %1, %2, %1\n\tv_accvgpr_write_b32 %0, %1" : "+a"(x), "=&v"(t) : "v"(f));
+        o[i] = x;
+    }
+    acc_wait(o);
 }
 
 __device__ __forceinline__ bf16x8 pack_bf16x8(const float *f)

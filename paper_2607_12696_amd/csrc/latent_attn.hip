@@ -39,23 +39,6 @@ __device__ __forceinline__ u32x2 read_tr(const char *p)
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p));
 }
 
-// Arithmetic on an accumulator tile where it lies, in the accumulation registers: written out, because the compiler would
-// move all sixteen tiles to vector registers, and those to scratch, for it.  The waits at either end cover the matrix
-// instructions around it (19 wait states from a product's write to a read); the tile as an operand keeps them in place.
-__device__ __forceinline__ void acc_wait(f32x16 &o) { asm volatile("s_nop 15\n\ts_nop 7" : "+a"(o)); }
-
-__device__ __forceinline__ void acc_scale(f32x16 &o, float f)
-{
-    acc_wait(o);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        float x = o[i], t;
-        asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_mul_f32 %1, %2, %1\n\tv_accvgpr_write_b32 %0, %1" : "+a"(x), "=&v"(t) : "v"(f));
-        o[i] = x;
-    }
-    acc_wait(o);
-}
-
 // The score products, with their sums in vector registers (the accumulation registers are full): the compiler would give
 // them accumulation registers.  Written out, they carry their own waits: a register written by the vector unit needs two
 // wait states before a product reads it, a product's result 19 before the vector unit does.

@@ -2,24 +2,28 @@
 // share) and 128-element values, causal.
 //
 // 640 operations a row, key and head against 512 bytes a key and head: bound by the matrix cores.  A workgroup takes 256
-// consecutive queries of one head, 32 each of eight wavefronts, two on a SIMD, and tiles of 64 keys from LDS.
+// consecutive queries of one head, one a compute unit, 32 rows each of eight wavefronts, two on a SIMD.
 //   Scores are transposed (S^T = K Q^T): a lane holds one row, its scores are the value product's operand as they stand
 //   (O^T = V^T P^T), and V^T is read with the transposing LDS load.
-//   The two wavefronts of a SIMD work in turn: while the first four multiply keys, the other four do the softmax and the
-//   value product of the tile before, so that the matrix cores and the vector unit are both in use; a barrier after each
-//   half step keeps them apart.
-//   Keys and values go from memory straight to LDS, two buffers each, issued two half steps before they are read; chunks
-//   of 16 bytes are XORed with row bits so that 16 rows' chunks (a quarter of a read) lie in different banks.
+//   Three tiles are under way: while the matrix cores multiply the keys of tile t + 1 and the values of tile t - 1, the
+//   vector unit works out the weights of tile t, a piece behind each product.
+//   Keys and values go from memory straight to LDS, two tiles ahead (rings of three tiles of keys, five of values), in
+//   panels: of 64 elements for keys (rows of 128 bytes, chunks of 16 XORed with row bits, so that 16 rows' chunks, a quarter
+//   of a read, lie in different banks), of 32 for values (rows of 64 bytes: half a read is 256 in a row).  So a read's
+//   place in the tile is an immediate offset.  One barrier a tile of 32 keys.
 #include "attn_plan.hpp"
 
 namespace ecospec {
 namespace {
 
 constexpr int kDn = 128, kP = 64, kDv = 128, kDq = kDn + kP;
-constexpr int kKeys = 64;
-constexpr int kWaves = 8, kRows = 32 * kWaves, kThreads = 64 * kWaves;
+constexpr int kKeys = 32;
+constexpr int kRt = 1, kWaves = 8, kRows = 32 * kRt * kWaves, kThreads = 64 * kWaves;  // kRt: row tiles of a wavefront
 constexpr int kSteps = kDq / 16;
-constexpr int kRing = 4;  // steps of score operands in registers
+constexpr int kRing = 4, kAhead = 3;  // key and value operands in registers
+constexpr int kLoads = 3;             // loads of a tile by a wavefront
+constexpr int kScore = kRt * kSteps, kProducts = kScore + kRt * 8;  // of a tile
+constexpr int kEdge = kRows / kKeys + 1;  // most tiles that some rows of a workgroup see in part
 constexpr float kSlack = 8.f;
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
@@ -31,253 +35,361 @@ __device__ __forceinline__ u32x2 read_tr(const char *p)
 
 __device__ __forceinline__ bool not_finite(uint32_t bf16) { return (bf16 & 0x7f80u) == 0x7f80u; }
 
-__device__ __forceinline__ bf16x8 finite(bf16x8 v)
-{
-    u32x4 w = __builtin_bit_cast(u32x4, v);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] &= (not_finite(w[i]) ? 0u : 0xffffu) | (not_finite(w[i] >> 16) ? 0u : 0xffff0000u);
-    return __builtin_bit_cast(bf16x8, w);
-}
+constexpr int kPanel = kKeys * 128;              // 64 elements of a tile's keys
+constexpr int kKeyTile = 3 * kPanel, kValueTile = kKeys * kDv * 2;
 
-struct Lds {
-    char k[2][kKeys * kDn * 2];     // row r, chunk c of 16 bytes at place c ^ (r & 15)
-    char rope[2][kKeys * kP * 2];   // at c ^ (r >> 1 & 7)
-    char v[2][kKeys * kDv * 2];     // at c ^ (r & 3) << 2
-    uint16_t p[kWaves][2][32][kKeys];  // weights of even and odd tiles with infinities or NaN among the values
+struct Tiles {
+    char k[3][kKeyTile];    // panel, row r, chunk c of 16 bytes at place c ^ (r >> 1 & 7); the last panel is the rotary part
+    char v[5][kValueTile];  // panel of 32 elements, row
+    uint32_t some[kEdge][kThreads];  // which weights of a lane are not zero, in a tile with infinities or NaN
+    char nothing[1024];
 };
 
-__global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int blocks)
+union Lds {
+    char q[kWaves][32 * kRt * kDq * 2];  // the queries of each wavefront, before the loop: at c ^ (r >> 1 & 7)
+    Tiles t;
+};
+
+// The score products, sums in vector registers, which the vector unit works on; a register written by the vector
+// unit needs two wait states before a product reads it.
+__device__ __forceinline__ void mfma_first(f32x16 &s, const bf16x8 &k, const bf16x8 &q)
+{
+    asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(k), "v"(q));
+}
+
+__device__ __forceinline__ void mfma_next(f32x16 &s, const bf16x8 &k, const bf16x8 &q)
+{
+    asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(k), "v"(q));
+}
+
+__global__ __launch_bounds__(kThreads, kWaves / 4) void prompt_kernel(PromptArgs a, int blocks)
 {
     __shared__ __attribute__((aligned(16))) Lds lds;
-    // All row blocks of a head on one XCD, one after the other, so that its L2 has the head's keys; long ones first.
-    const int pair = blockIdx.x % 8 + 8 * (int)(blockIdx.x / 8 / blocks), block = blocks - 1 - (int)(blockIdx.x / 8) % blocks;
+    // A head's row blocks on one XCD; the longest of all heads first, so that no long one is left for the end.
+    const int pairs = (a.B * a.H + 7) / 8, pair = blockIdx.x % 8 + 8 * (int)(blockIdx.x / 8 % pairs), block = blocks - 1 - (int)(blockIdx.x / 8 / pairs);
     if (pair >= a.B * a.H) return;
     const int b = pair / a.H, h = pair % a.H;
-    const int q0 = min(max(a.q_offsets[b], 0), a.N), nq = min(max(a.q_offsets[b + 1], q0), a.N) - q0;
-    const int k0 = min(max(a.kv_offsets[b], 0), a.M), nk = min(max(a.kv_offsets[b + 1], k0), a.M) - k0;
+    const int q0 = __builtin_amdgcn_readfirstlane(min(max(a.q_offsets[b], 0), a.N)), nq = __builtin_amdgcn_readfirstlane(min(max(a.q_offsets[b + 1], q0), a.N)) - q0;
+    const int k0 = __builtin_amdgcn_readfirstlane(min(max(a.kv_offsets[b], 0), a.M));
+    const int nk = __builtin_amdgcn_readfirstlane(min(max(a.kv_offsets[b + 1], k0), a.M)) - k0;
     const int row0 = block * kRows;
     if (row0 >= nq) return;
 
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 32, half = lane / 32;
     auto limit = [&](int row) { return min(max(row + 1 + nk - nq, 0), nk); };  // keys that a query sees
     const int tiles = (limit(min(row0 + kRows, nq) - 1) + kKeys - 1) / kKeys;
-    const int first = row0 + 32 * wave, row = first + col;
-    const int all_see = limit(first), some_see = first < nq ? limit(min(first + 32, nq) - 1) : 0;  // of the wavefront's rows
-    const int mine = limit(row);
+    const int edge = limit(row0) / kKeys;  // first tile that some row of the workgroup does not see to its end
+    const int first = row0 + 32 * kRt * wave;
+    const int all_see = limit(first);      // keys that all rows of the wavefront see
 
-    // ---- loads: wavefront w brings rows 8 w .. 8 w + 7 of a tile
-    uint32_t k_off[2], v_off[2], rope_off;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const int r = 8 * wave + 4 * e + lane / 16;
-        k_off[e] = (uint32_t)(r * (uint32_t)a.k_stride * 2 + ((lane % 16) ^ (r & 15)) * 16);
-        v_off[e] = (uint32_t)(r * (uint32_t)a.v_stride * 2 + ((lane % 16) ^ (r & 3) << 2) * 16);
-    }
+    // ---- queries through LDS
+    bf16x8 q[kRt][kSteps];
     {
-        const int r = 8 * wave + lane / 8;
-        rope_off = (uint32_t)(r * kP * 2 + ((lane % 8) ^ (r >> 1 & 7)) * 16);
-    }
-    const uint16_t *kh = a.k + h * a.k_head + k0 * a.k_stride, *vh = a.v + h * a.v_head + k0 * a.v_stride;
-    const uint16_t *rh = a.k_rope + (long)k0 * kP;
-    // Rows past the last key become zeros; tiles past the last bring nothing but zeros.
-    auto load_k = [&](int t) {
-        const int rows = t < tiles ? min(nk - t * kKeys, kKeys) : 0, at = min(t, tiles - 1) * kKeys;
-        const u32x4 r = rsrc_words(kh + at * a.k_stride, rows ? (uint32_t)((rows - 1) * a.k_stride + kDn) * 2 : 0);
-        const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(lds.k[t & 1]) + wave * 2048);
-        load16_lds(r, k_off[0], dst);
-        load16_lds(r, k_off[1], dst + 1024);
-        load16_lds(rsrc_words(rh + (long)at * kP, (uint32_t)rows * kP * 2), rope_off,
-                   __builtin_amdgcn_readfirstlane(lds_addr(lds.rope[t & 1]) + wave * 1024));
-    };
-    auto load_v = [&](int t) {
-        const int rows = t < tiles ? min(nk - t * kKeys, kKeys) : 0, at = min(t, tiles - 1) * kKeys;
-        const u32x4 r = rsrc_words(vh + at * a.v_stride, rows ? (uint32_t)((rows - 1) * a.v_stride + kDv) * 2 : 0);
-        const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(lds.v[t & 1]) + wave * 2048);
-        load16_lds(r, v_off[0], dst);
-        load16_lds(r, v_off[1], dst + 1024);
-    };
-
-    bf16x8 q[kSteps];
-    {
-        const uint16_t *p = a.q + ((long)(q0 + min(row, nq - 1)) * a.H + h) * kDq + 8 * half;
+        const int rows = max(min(nq - first, 32 * kRt), 0), stride = a.H * kDq * 2;
+        const u32x4 from = rsrc_words(a.q + ((long)(q0 + min(first, nq - 1)) * a.H + h) * kDq,
+                                      rows ? (uint32_t)((rows - 1) * stride + kDq * 2) : 0);
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds_addr(lds.q[wave]));
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) q[s] = *reinterpret_cast<const bf16x8 *>(p + 16 * s);
-    }
-    if (tiles) {
-        load_k(0);
-        load_v(0);
-    }
-
-    f32x16 o[kDv / 32], s[2];
+        for (int n = 0; n < 12 * kRt; ++n) {
+            const int i = n * 64 + lane, r = i / 24, c = i % 24;
+            load16_lds(from, (uint32_t)(r * stride + (c ^ (r >> 1 & 7)) * 16), to + n * 1024);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-    for (int d = 0; d < kDv / 32; ++d)
+        for (int rt = 0; rt < kRt; ++rt)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-    float m = -INFINITY, l = 0.f;
-    int not_finite_tiles = 0, last_odd = 0;  // bit: even or odd tile; a wavefront sees at most two tiles in part
-    const float scale2 = a.scale * kLog2e;
-
-    const uint32_t k_at = (uint32_t)(col * 256 + (half ^ (col & 15)) * 16), rope_at = (uint32_t)(col * 128 + (half ^ (col >> 1 & 7)) * 16);
-    const int i16 = lane % 16;
-    const uint32_t v_at = (uint32_t)((4 * half + i16 / 4) * 256 + ((lane / 16 % 2 * 2 + i16 % 4 / 2) ^ (i16 / 4) << 2) * 16 + i16 % 2 * 8);
-
-    auto scores = [&](int t) {
-        if (t * kKeys >= some_see) return;
-        const char *k = lds.k[t & 1], *rope = lds.rope[t & 1];
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[kt][i] = 0.f;
-        bf16x8 f[kRing][2];  // operands of a step's two products
-        auto fetch = [&](int st) {
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt) {
-                const char *p = st < 8 ? k + (k_at ^ (st * 32)) + kt * 32 * 256 : rope + (rope_at ^ ((st - 8) * 32)) + kt * 32 * 128;
-                f[st % kRing][kt] = *reinterpret_cast<const bf16x8 *>(p);
+            for (int st = 0; st < kSteps; ++st) {
+                u32x4 w = *reinterpret_cast<const u32x4 *>(lds.q[wave] + (32 * rt + col) * kDq * 2 + ((2 * st + half) ^ (col >> 1 & 7)) * 16);
+                if (a.scale < 0.f) w ^= 0x80008000u;  // the scale is positive from here on: the largest product is the largest score
+                q[rt][st] = __builtin_bit_cast(bf16x8, w);
             }
-        };
+    }
+    __syncthreads();
+
+    // ---- loads: of the first four wavefronts, w brings rows 8 w .. 8 w + 7 of a tile's keys, a panel a load; of the others,
+    // w + 4 brings panel w of its values, 16 rows a load (and a load of nothing, so that all count alike).  Rows past the last
+    // key, and tiles past the last, become zeros.
+    const bool keys = wave < 4;
+    const uint16_t *src = keys ? a.k + h * a.k_head + k0 * a.k_stride : a.v + h * a.v_head + k0 * a.v_stride;
+    const uint16_t *rope = a.k_rope + (long)k0 * kP;
+    const uint32_t stride2 = (uint32_t)(keys ? a.k_stride : a.v_stride) * 2;
+    const int e = 8 * wave + lane / 8, place = (lane % 8) ^ (e >> 1 & 7);
+    const uint32_t off = keys ? e * stride2 + place * 16 : lane / 4 * stride2 + (wave - 4) * 64 + lane % 4 * 16;
+    const uint32_t off1 = keys ? off + 128 : off + 16 * stride2, rope_off = (uint32_t)(e * kP * 2 + place * 16);
+    // The tile to load next: its place in memory and in the rings.
+    const uint32_t ring = __builtin_amdgcn_readfirstlane(keys ? lds_addr(lds.t.k) + wave * 1024 : lds_addr(lds.t.v) + (wave - 4) * 2048);
+    const uint32_t turn = keys ? kKeyTile : kValueTile, around = keys ? 3 * kKeyTile : 5 * kValueTile;
+    const uint32_t step1 = keys ? kPanel : 1024, nothing = __builtin_amdgcn_readfirstlane(lds_addr(lds.t.nothing));
+    int left_k = tiles ? nk : 0;  // keys from the tile on
+    uint32_t to = 0;
+    u32x4 row_src, rope_src;
+    auto aim = [&] {
+        const int rows = max(min(left_k, kKeys), 0);
+        row_src = rsrc_words(src, rows ? (uint32_t)(rows - 1) * stride2 + kDn * 2 : 0);
+        rope_src = rsrc_words(rope, keys ? (uint32_t)rows * kP * 2 : 0);
+    };
+    auto advance = [&] {
+        left_k -= kKeys;
+        if (left_k > 0) {
+            src += kKeys / 2 * stride2;
+            rope += kKeys * kP;
+        }
+        to = to + turn == around ? 0 : to + turn;
+    };
+    auto load = [&](int n) {
+        if (n == 0) load16_lds(row_src, off, ring + to);
+        else if (n == 1) load16_lds(row_src, off1, ring + to + step1);
+        else load16_lds(rope_src, rope_off, keys ? ring + to + 2 * kPanel : nothing);
+    };
+#pragma unroll 1
+    for (int t = 0; t < 2; ++t) {
+        aim();
 #pragma unroll
-        for (int st = 0; st < kRing - 1; ++st) fetch(st);
+        for (int n = 0; n < kLoads; ++n) load(n);
+        advance();
+    }
+    // The values of tile -1, whose weights are zeros.
+    for (int i = threadIdx.x; i < kKeys * kDv * 2 / 16; i += kThreads) reinterpret_cast<u32x4 *>(lds.t.v[4])[i] = u32x4{0, 0, 0, 0};
+
+    f32x16 o[kRt][kDv / 32];
+#pragma unroll
+    for (int rt = 0; rt < kRt; ++rt)
+#pragma unroll
+        for (int d = 0; d < kDv / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[rt][d][i] = 0.f;
+    float m[kRt], l[kRt], down[kRt];
+    int scaled[kRt];
+#pragma unroll
+    for (int rt = 0; rt < kRt; ++rt) {
+        m[rt] = -INFINITY;
+        l[rt] = 0.f;
+        down[rt] = 1.f;
+        scaled[rt] = 0;
+    }
+    bf16x8 p[kRt][2] = {};  // weights of the tile before: row tile, 16 keys
+    uint32_t odd_tiles = 0;  // edge tiles with infinities or NaN among the values
+    const float scale2 = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-126f);  // not zero: it meets infinities
+
+    uint32_t k_at[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) k_at[i] = (uint32_t)(col * 128 + ((2 * i + half) ^ (col >> 1 & 7)) * 16);
+    const int i16 = lane % 16;
+    const uint32_t v_at = (uint32_t)((4 * half + i16 / 4) * 64 + lane / 16 % 2 * 32 + i16 % 4 * 8);
+
+    // Behind product c, a piece of the weights of the scores s of a tile.  Register i of a row tile is key
+    // 8 (i / 4) + 4 half + i % 4.
+    float top[kRt], base[kRt], sum[kRt];
+    u32x4 packed[kRt][2];
+    auto weights = [&](f32x16 (&s)[kRt], int c) {
+        if (c < kRt) {
+            f32x16 &x = s[c];
+            top[c] = max3(max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), x[6]), max3(max3(x[7], x[8], x[9]), max3(x[10], x[11], x[12]), x[13]),
+                          fmaxf(x[14], x[15]));
+        } else if (c < 2 * kRt) {
+            top[c - kRt] = halves_max(top[c - kRt]) * scale2;
+        } else if (c < 3 * kRt) {
+            const int rt = c - 2 * kRt;
+            int move = __any(top[rt] > m[rt] + kSlack);
+            scaled[rt] = move & __any(m[rt] != -INFINITY);
+            asm("" : "+v"(move));  // a select, not a branch
+            const float now = move ? fmaxf(m[rt], top[rt]) : m[rt];
+            base[rt] = now == -INFINITY ? 0.f : now;
+            down[rt] = __builtin_amdgcn_exp2f((m[rt] == -INFINITY ? base[rt] : m[rt]) - base[rt]);
+            m[rt] = now;
+            sum[rt] = 0.f;
+        } else {
+            const int e = c - 3 * kRt;  // of 16 kRt elements
+            if (e < 16 * kRt) s[e / 16][e % 16] = __builtin_amdgcn_exp2f(fmaf(s[e / 16][e % 16], scale2, -base[e / 16]));
+            // The element before: its sum, and pairs to bf16.  Written out to stay here, where the compiler would sink them
+            // behind all products; a piece later, because the result of an exp2 needs a wait state.
+            if (e > 0 && e <= 16 * kRt) {
+                const int rt = (e - 1) / 16, i = (e - 1) % 16;
+                asm volatile("v_add_f32 %0, %0, %1" : "+v"(sum[rt]) : "v"(s[rt][i]));
+                if (i % 2) {
+                    uint32_t w;
+                    asm volatile("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(w) : "v"(s[rt][i - 1]), "v"(s[rt][i]));
+                    packed[rt][i / 8][i % 8 / 2] = w;
+                }
+                if (i == 15) l[rt] = fmaf(l[rt], down[rt], sum[rt]);
+            }
+        }
+    };
+    static_assert(kProducts >= 19 * kRt + 1, "all pieces");
+    // Operands of the tiles at these ring offsets.
+    uint32_t key_at[4], value_at = v_at + 4 * kValueTile;
+    auto k_frag = [&](int st) { return *reinterpret_cast<const bf16x8 *>(lds.t.k[0] + key_at[st % 4] + st / 4 * kPanel); };
+    auto v_frag = [&](int n) {  // n: 4 * (16 keys) + element tile
+        const char *w = lds.t.v[0] + value_at + n % 4 * (kKeys * 64) + n / 4 * 16 * 64;
+        const u32x2 lo = read_tr(w), hi = read_tr(w + 8 * 64);
+        return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+    };
+    bf16x8 k[kRing], v[kAhead];
+    auto first_keys = [&] {
+#pragma unroll
+        for (int st = 0; st < kRing - 1; ++st) k[st] = k_frag(st);
+    };
+    // Products of a tile's keys (the first ones fetched) into s, then of a tile's values, `between(c)` behind product c.
+    auto products = [&](f32x16 (&s)[kRt], auto between) {
 #pragma unroll
         for (int st = 0; st < kSteps; ++st) {
-            if (st + kRing - 1 < kSteps) fetch(st + kRing - 1);
-            __builtin_amdgcn_sched_barrier(0);
+            if (st + kRing - 1 < kSteps) k[(st + kRing - 1) % kRing] = k_frag(st + kRing - 1);
+            else v[st + kRing - 1 - kSteps] = v_frag(st + kRing - 1 - kSteps);
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[st % kRing][kt], q[st], s[kt], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int rt = 0; rt < kRt; ++rt) {
+                __builtin_amdgcn_sched_barrier(0);
+                if (st == 0) mfma_first(s[rt], k[0], q[rt][0]);
+                else mfma_next(s[rt], k[st % kRing], q[rt][st]);
+                between(kRt * st + rt);
+            }
         }
+        static_assert(kRing - 1 == kAhead, "the last steps fetch the first value operands");
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+#pragma unroll
+            for (int rt = 0; rt < kRt; ++rt) {
+                __builtin_amdgcn_sched_barrier(0);
+                o[rt][n % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[n % kAhead], p[rt][n / 4], o[rt][n % 4], 0, 0, 0);
+                between(kScore + kRt * n + rt);
+            }
+            if (n + kAhead < 8) v[n % kAhead] = v_frag(n + kAhead);
+        }
+        __builtin_amdgcn_sched_barrier(0);
     };
-    // Register i of key tile kt is key 32 kt + 8 (i / 4) + 4 half + i % 4.
-    auto values = [&](int t) {
-        if (t * kKeys >= some_see) return;
-        const char *v = lds.v[t & 1];
-        const bool part = (t + 1) * kKeys > all_see;
-        float x[32];
+
+    uint32_t key_to = 0, value_to = 4 * kValueTile;
+    auto turn_rings = [&] {  // to the keys and the values after
+        key_to = key_to == 2 * kKeyTile ? 0 : key_to + kKeyTile;
+        value_to = value_to == 4 * kValueTile ? 0 : value_to + kValueTile;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) x[i] = s[i / 16][i % 16] * scale2;
-        if (part) {
-            const int left = mine - t * kKeys - 4 * half;
+        for (int i = 0; i < 4; ++i) key_at[i] = k_at[i] + key_to;
+        value_at = v_at + value_to;
+    };
+
+    // One tile: s its scores, next the scores of the tile after.
+    auto tile = [&](int t, f32x16 (&s)[kRt], f32x16 (&next)[kRt]) {
+        // Tile t + 1 has landed; every wavefront is past the scores of tile t and the values of tile t - 2.
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads) : "memory");
+        first_keys();
+        aim();
+        if (t >= edge && t < tiles) {
+            // A weight of zero must not meet an infinity or NaN: where a tile that not all rows see to its end has one,
+            // zeros take its place, and what it gives the rows that see it is added at the end.
+            u32x4 *all = reinterpret_cast<u32x4 *>(lds.t.v[t % 5]);
+            bool odd = false;
+            for (int i = threadIdx.x; i < kKeys * kDv * 2 / 16; i += kThreads) {
+                u32x4 v = all[i];
+                bool any = false;
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (i / 4 * 8 + i % 4 >= left) x[i] = -INFINITY;
-        }
-        float top = x[0];
-#pragma unroll
-        for (int i = 1; i < 32; ++i) top = fmaxf(top, x[i]);
-        top = halves_max(top);
-        if (__any(top > m + kSlack)) {
-            const float now = fmaxf(m, top), down = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
-            m = now;
-            l *= down;
-#pragma unroll
-            for (int d = 0; d < kDv / 32; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[d][i] *= down;
-        }
-        const float base = m == -INFINITY ? 0.f : m;
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            x[i] = __builtin_amdgcn_exp2f(x[i] - base);
-            sum += x[i];
-        }
-        l += sum;
-        bf16x8 p[4];
-#pragma unroll
-        for (int st = 0; st < 4; ++st) p[st] = pack_bf16x8(x + 8 * st);
-        bool odd = false;
-        if (part) {
-            // A weight of zero must not meet an infinity or NaN: where the tile has one, zeros take its place, and what it
-            // gives the rows that see it is added at the end.
-            for (int i = lane; i < kKeys * kDv * 2 / 16; i += kWave) {
-                const u32x4 w = reinterpret_cast<const u32x4 *>(v)[i];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) odd |= not_finite(w[j]) || not_finite(w[j] >> 16);
+                for (int w = 0; w < 4; ++w) {
+                    const bool lo = not_finite(v[w]), hi = not_finite(v[w] >> 16);
+                    v[w] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+                    any |= lo || hi;
+                }
+                if (any) all[i] = v;
+                odd |= any;
             }
-            odd = __any(odd);
-            if (odd) {
-                not_finite_tiles |= 1 << (t & 1);
-                last_odd = t;
+            if (__syncthreads_or(odd)) odd_tiles |= 1u << (t - edge);
+        }
+        // The sums so far, for the reference maximum that the weights of tile t - 1 have.
 #pragma unroll
-                for (int i = 0; i < 32; i += 4)
-                    *reinterpret_cast<u32x2 *>(&lds.p[wave][t & 1][col][i / 4 * 8 + 4 * half]) = u32x2{pack_bf16x2(x[i], x[i + 1]), pack_bf16x2(x[i + 2], x[i + 3])};
+        for (int rt = 0; rt < kRt; ++rt)
+            if (scaled[rt]) {
+#pragma unroll
+                for (int d = 0; d < kDv / 32; ++d) acc_scale(o[rt][d], down[rt]);
+                scaled[rt] = 0;
+            }
+        if ((t + 1) * kKeys > all_see) {
+#pragma unroll
+            for (int rt = 0; rt < kRt; ++rt) {
+                const int left = limit(first + 32 * rt + col) - t * kKeys - 4 * half;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (i / 4 * 8 + i % 4 >= left) s[rt][i] = -INFINITY;
             }
         }
-        bf16x8 f[3];
-        auto fetch = [&](int n) {
-            const char *w = v + (v_at ^ (n % 4 * 64)) + n / 4 * 16 * 256;
-            const u32x2 lo = read_tr(w), hi = read_tr(w + 8 * 256);
-            f[n % 3] = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
-        };
-        fetch(0);
-        fetch(1);
+        products(next, [&](int c) {
+            weights(s, c);
+            if (c >= kScore && c < kScore + 2 * kLoads && (c - kScore) % 2 == 0) load((c - kScore) / 2);
+        });
 #pragma unroll
-        for (int n = 0; n < 16; ++n) {
-            if (n + 2 < 16) fetch(n + 2);
-            if (odd) f[n % 3] = finite(f[n % 3]);
-            __builtin_amdgcn_sched_barrier(0);
-            o[n % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[n % 3], p[n / 4], o[n % 4], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
+        for (int rt = 0; rt < kRt; ++rt)
+#pragma unroll
+            for (int st = 0; st < 2; ++st) p[rt][st] = __builtin_bit_cast(bf16x8, packed[rt][st]);
+        advance();
+        turn_rings();
+        if (odd_tiles >> (t - edge) & (t >= edge ? 1 : 0)) {
+            uint32_t some = 0;
+#pragma unroll
+            for (int i = 0; i < 16 * kRt; ++i) some |= (s[i / 16][i % 16] != 0.f ? 1u : 0u) << i;
+            lds.t.some[t - edge][threadIdx.x] = some;
         }
     };
 
-    // Half step 2 t: the first four wavefronts take the scores of tile t, the others the values of tile t - 1; half step
-    // 2 t + 1: values of tile t and scores of tile t.  Every wavefront issues its share of keys t + 1 in half step 2 t (they
-    // have landed at the end of 2 t + 1) and of values t + 1 in half step 2 t + 1 (at the end of 2 t + 2).
-    const bool second = wave >= 4;
-    auto keys_step = [&] {  // ends a half step that issued keys (three loads): the values before them have landed
-        asm volatile("s_waitcnt vmcnt(3) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    };
-    auto values_step = [&] {
-        asm volatile("s_waitcnt vmcnt(2) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    };
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (second && tiles) {
-        load_k(1);
-        keys_step();
+    aim();
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) load(n);
+    advance();
+    f32x16 s0[kRt], s1[kRt];
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) key_at[i] = k_at[i];
+#pragma unroll
+        for (int st = 0; st < kSteps; ++st)
+#pragma unroll
+            for (int rt = 0; rt < kRt; ++rt) {
+                if (st == 0) mfma_first(s0[rt], k_frag(0), q[rt][0]);
+                else mfma_next(s0[rt], k_frag(st), q[rt][st]);
+            }
+#pragma unroll
+        for (int rt = 0; rt < kRt; ++rt) asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s0[rt]));
     }
-    for (int t = 0; t < tiles; ++t) {
-        if (second) load_v(t + 1);
-        else load_k(t + 1);
-        scores(t);
-        if (second) values_step();
-        else keys_step();
-        if (second) load_k(t + 2);
-        else load_v(t + 1);
-        values(t);
-        if (second) {
-            if (t + 1 < tiles) keys_step();
-        } else {
-            values_step();
-        }
+    key_to = kKeyTile;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) key_at[i] = k_at[i] + kKeyTile;
+    // Tiles 0 .. tiles: the last adds the values of the last but one.
+#pragma unroll 1
+    for (int t = 0; t <= tiles; t += 2) {
+        tile(t, s0, s1);
+        if (t + 1 <= tiles) tile(t + 1, s1, s0);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing is on its way to LDS when the workgroup ends
 
-    if (row >= nq) return;
-    l = halves_sum(l);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const long at = (long)(q0 + row) * a.H + h;
 #pragma unroll
-    for (int d = 0; d < kDv / 32; ++d)
+    for (int rt = 0; rt < kRt; ++rt) {
+        const int row = first + 32 * rt + col;
+        l[rt] = halves_sum(l[rt]);
+        if (row >= nq) continue;
+        const float inv = l[rt] == 0.f ? 0.f : 1.f / l[rt];
+        const long at = (long)(q0 + row) * a.H + h;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<u32x2 *>(a.o + at * kDv + 32 * d + 8 * i + 4 * half) =
-                u32x2{pack_bf16x2(o[d][4 * i] * inv, o[d][4 * i + 1] * inv), pack_bf16x2(o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv)};
-    if (a.lse && half == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) / kLog2e;
-    if (!not_finite_tiles) return;
-    for (int n = 0; n < 64; ++n) {  // the lane's own elements, as above
-        const int el = n / 16 * 32 + n % 16 / 4 * 8 + 4 * half + n % 4;
+        for (int d = 0; d < kDv / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<u32x2 *>(a.o + at * kDv + 32 * d + 8 * i + 4 * half) =
+                    u32x2{pack_bf16x2(o[rt][d][4 * i] * inv, o[rt][d][4 * i + 1] * inv),
+                          pack_bf16x2(o[rt][d][4 * i + 2] * inv, o[rt][d][4 * i + 3] * inv)};
+        if (a.lse && half == 0) a.lse[at] = l[rt] == 0.f ? -INFINITY : (m[rt] + __builtin_amdgcn_logf(l[rt])) / kLog2e;
+    }
+    if (!odd_tiles) return;
+    for (int n = 0; n < 64 * kRt; ++n) {  // the lane's own elements, as above
+        const int rt = n / 64, row = first + 32 * rt + col, el = n % 64 / 16 * 32 + n % 16 / 4 * 8 + 4 * half + n % 4;
+        if (row >= nq) continue;
         float c = 0.f;
-        for (int t = max(last_odd - 1, 0); t <= last_odd; ++t) {
-            if (!(not_finite_tiles >> (t & 1) & 1)) continue;
-            for (int j = 0; j < min(mine - t * kKeys, kKeys); ++j) {
-                const uint16_t e = vh[(long)(t * kKeys + j) * a.v_stride + el];
-                if (not_finite(e)) c = fmaf(bf16_bits_to_f32(lds.p[wave][t & 1][col][j]), bf16_bits_to_f32(e), c);
+        for (int e = 0; e < kEdge; ++e) {
+            if (!(odd_tiles >> e & 1)) continue;
+            const int at = (edge + e) * kKeys;
+            for (int j = 0; j < min(limit(row) - at, kKeys); ++j) {
+                const uint16_t v = a.v[h * a.v_head + (long)(k0 + at + j) * a.v_stride + el];
+                if (!not_finite(v)) continue;
+                const uint32_t some = lds.t.some[e][wave * kWave + j / 4 % 2 * 32 + col] >> (16 * rt + j / 8 * 4 + j % 4) & 1;
+                c = fmaf(some ? 1.f : 0.f, bf16_bits_to_f32(v), c);
             }
         }
         if (c == 0.f) continue;
-        uint16_t *p = a.o + at * kDv + el;
-        *p = f32_to_bf16_bits(bf16_bits_to_f32(*p) + c);
+        uint16_t *to = a.o + ((long)(q0 + row) * a.H + h) * kDv + el;
+        *to = f32_to_bf16_bits(bf16_bits_to_f32(*to) + c);
     }
 }
 
