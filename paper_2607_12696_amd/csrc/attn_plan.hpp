@@ -17,7 +17,6 @@ namespace ecospec {
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 constexpr int kCus = 256;        // compute units of an MI355X
-constexpr int kPlanB = 1024;     // most sequences of a call
 constexpr float kLog2e = 1.44269504088896341f;
 
 struct Shape {
@@ -83,24 +82,37 @@ __device__ __forceinline__ long wave_sum_long(long v)
     return ((long)wave_sum_int((int)(v >> 16)) << 16) + wave_sum_int((int)(v & 0xffff));
 }
 
-// This workgroup's item.  work: 2 * B ints of LDS, free again after the call's last barrier.  per_token: query rows of a
-// token for one key/value head; heads: key/value heads.
-__device__ __forceinline__ bool plan_item(const PagedArgs &a, int per_token, int heads, const Shape &s, const Parts &parts,
-                                          int *work, Item &it)
+// A sequence of the batch: its tokens and cache, and the row groups and key tiles that they make.
+struct Sequence {
+    int t0, n, len, groups, tiles;
+};
+
+__device__ __forceinline__ Sequence sequence(const PagedArgs &a, int b, int per_token, int heads, const Shape &s)
 {
-    for (int b = threadIdx.x; b < a.B; b += blockDim.x) {
-        const int t0 = min(max(a.token_offsets[b], 0), a.N), n = min(max(a.token_offsets[b + 1], t0), a.N) - t0;
-        const int len = min(max(a.cache_len[b], 0), a.max_blocks * a.page);
-        work[2 * b] = (int)(((long)n * per_token + s.rows - 1) / s.rows) * heads;
-        work[2 * b + 1] = n ? (len + s.keys - 1) / s.keys + (min(n, kMaxDrafts) + s.keys - 1) / s.keys : 0;
-    }
-    __syncthreads();
+    Sequence q{0, 0, 0, 0, 0};
+    if (b >= a.B) return q;
+    const int from = a.token_offsets[b], to = a.token_offsets[b + 1], len = a.cache_len[b];
+    q.t0 = min(max(from, 0), a.N);
+    q.n = min(max(to, q.t0), a.N) - q.t0;
+    q.len = min(max(len, 0), a.max_blocks * a.page);
+    q.groups = (int)(((long)q.n * per_token + s.rows - 1) / s.rows) * heads;
+    q.tiles = q.n ? (q.len + s.keys - 1) / s.keys + (min(q.n, kMaxDrafts) + s.keys - 1) / s.keys : 0;
+    return q;
+}
+
+// This workgroup's item; every wavefront works it out for itself, a lane a sequence.  per_token: query rows of a token for
+// one key/value head; heads: key/value heads.
+__device__ __forceinline__ bool plan_item(const PagedArgs &a, int per_token, int heads, const Shape &s, const Parts &parts,
+                                          Item &it)
+{
     const int lane = lane_id();
-    int groups = 0;
-    long total = 0;
-    for (int b = lane; b < a.B; b += kWave) {
-        groups += work[2 * b];
-        total += (long)work[2 * b] * work[2 * b + 1];
+    const Sequence mine = sequence(a, lane, per_token, heads, s);  // the first 64; others are read where they are needed
+    int groups = mine.groups;
+    long total = (long)mine.groups * mine.tiles;
+    for (int b = lane + kWave; b < a.B; b += kWave) {
+        const Sequence q = sequence(a, b, per_token, heads, s);
+        groups += q.groups;
+        total += (long)q.groups * q.tiles;
     }
     groups = wave_sum_int(groups);
     total = wave_sum_long(total);
@@ -108,17 +120,17 @@ __device__ __forceinline__ bool plan_item(const PagedArgs &a, int per_token, int
     if (groups < kRounds * s.slots) {
         const int room = s.slots * ((groups + s.slots - 1) / s.slots);
         auto count = [&](int len) {
-            int n = 0;
-            for (int b = lane; b < a.B; b += kWave) n += work[2 * b] * ((work[2 * b + 1] + len - 1) / len);
+            int n = mine.groups * ((mine.tiles + len - 1) / len);
+            for (int b = lane + kWave; b < a.B; b += kWave) {
+                const Sequence q = sequence(a, b, per_token, heads, s);
+                n += q.groups * ((q.tiles + len - 1) / len);
+            }
             return wave_sum_int(n);
         };
-        c = max(s.min_tiles, (int)((total + room - 1) / max(room, 1)));
+        c = max(s.min_tiles, (int)((float)total / (float)max(room, 1)));
         items = count(c);
-        for (int i = 0; i < 12 && items > room; ++i) items = count(c += max(1, c / 16));
-        if (items > room) {  // always fits: a row group has at most one chunk more than its share
-            c = room > groups ? max(c, (int)((total + room - groups - 1) / (room - groups))) : 1 << 30;
-            items = count(c);
-        }
+        // Ends: chunks as long as the longest row group make one item of each, and there is room for those.
+        for (int i = 0; items > room; ++i) items = count(c += max(1, i < 12 ? c / 16 : c / 4));
     }
     // Neighbouring items (the row groups of one chunk read the same keys) run on one XCD, whose L2 they share:
     // workgroups are dealt to the eight XCDs in turn.
@@ -129,29 +141,29 @@ __device__ __forceinline__ bool plan_item(const PagedArgs &a, int per_token, int
     if ((int)(blockIdx.x / 8) >= per || want >= items) return false;
     int before = 0, groups_before = 0;
     for (int b0 = 0;; b0 += kWave) {
-        const int b = b0 + lane;
-        const int g = b < a.B ? work[2 * b] : 0, tiles = b < a.B ? work[2 * b + 1] : 0, n = (tiles + c - 1) / c;
-        const int upto = wave_inclusive_sum(g * n), gsum = wave_inclusive_sum(g);
+        const Sequence q = b0 ? sequence(a, b0 + lane, per_token, heads, s) : mine;
+        const int n = (q.tiles + c - 1) / c;
+        const int upto = wave_inclusive_sum(q.groups * n), gsum = wave_inclusive_sum(q.groups);
         const uint64_t past = __ballot(before + upto > want);
-        if (!past && b0 + kWave < a.B) {
+        if (!past) {
+            if (b0 + kWave >= a.B) return false;  // cannot be: want < items
             before += __builtin_amdgcn_readlane(upto, 63);
             groups_before += __builtin_amdgcn_readlane(gsum, 63);
             continue;
         }
-        if (!past) return false;  // cannot be: want < items
         const int at = __ffsll((unsigned long long)past) - 1;
-        const int gb = __builtin_amdgcn_readlane(g, at), tb = __builtin_amdgcn_readlane(tiles, at);
+        const int gb = __builtin_amdgcn_readlane(q.groups, at), tb = __builtin_amdgcn_readlane(q.tiles, at);
         const int nb = __builtin_amdgcn_readlane(n, at);
         const int rest = want - before - (__builtin_amdgcn_readlane(upto, at) - gb * nb);
         const int chunk = rest / gb;
         it.b = b0 + at;
         it.group = rest % gb;
         it.row_tiles = gb / heads;
-        it.t0 = min(max(a.token_offsets[it.b], 0), a.N);
-        it.n_tok = min(max(a.token_offsets[it.b + 1], it.t0), a.N) - it.t0;
-        it.len = min(max(a.cache_len[it.b], 0), a.max_blocks * a.page);
-        it.first = (int)((long)chunk * tb / nb);
-        it.last = (int)((long)(chunk + 1) * tb / nb);
+        it.t0 = __builtin_amdgcn_readlane(q.t0, at);
+        it.n_tok = __builtin_amdgcn_readlane(q.n, at);
+        it.len = __builtin_amdgcn_readlane(q.len, at);
+        it.first = chunk * (tb / nb) + min(chunk, tb % nb);
+        it.last = it.first + tb / nb + (chunk < tb % nb);
         it.chunks = nb;
         it.slot = want;
         const int record = groups_before + __builtin_amdgcn_readlane(gsum, at) - gb + it.group;
@@ -161,50 +173,62 @@ __device__ __forceinline__ bool plan_item(const PagedArgs &a, int per_token, int
     }
 }
 
-// Adds up the parts of a row group: one workgroup for each 32 x 32 block of its output (rows x elements), thread t having
-// the four consecutive elements that lane t % 64 and registers 4 * (t / 64) .. of the accumulators hold.
+// Adds up the parts of a row group, 32 rows x 32 elements at a time.  A wavefront has a quarter of such a block: lane l the
+// four consecutive elements that registers 4 * quarter .. of lane l of the accumulators hold.  Of a SPLIT workgroup the four
+// wavefronts have one quarter and take every fourth part, so that few row groups of many parts still fill the card;
+// otherwise they have the four quarters and all parts.
 // ROWS: rows of a group; W: width of an output row; blocks of a part: row tile * (W / 32) + element tile.
-template <int ROWS, int W>
+template <int ROWS, int W, bool SPLIT>
 __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int per_token, Parts p)
 {
-    constexpr int kBlocks = ROWS / 32 * (W / 32), kJoin = 64;
-    __shared__ float weight[kJoin * 32], sums[kJoin * 32];
-    const int g = blockIdx.x / kBlocks, blk = blockIdx.x % kBlocks;
+    constexpr int kBlocks = ROWS / 32 * (W / 32);
+    __shared__ float tops[4][32];
+    __shared__ f32x4 sums[3][kWave];
+    __shared__ float totals[3][kWave];
+    const int block = SPLIT ? blockIdx.x / 4 : blockIdx.x, wave = threadIdx.x / kWave;
+    const int g = block / kBlocks, blk = block % kBlocks, quarter = SPLIT ? blockIdx.x % 4 : wave;
     if (g >= *p.groups) return;
     const GroupInfo in = p.info[g];
     if (in.chunks <= 1) return;
     const int lane = lane_id(), col = lane % 32, row = blk / (W / 32) * 32 + col;
     const float2 *ml = p.ml + (long)in.slot0 * ROWS + row;
-    const long step = (long)in.stride * ROWS;
-    // The largest reference maximum of each row; eight threads a row.
+    const f32x4 *o = reinterpret_cast<const f32x4 *>(p.o) + ((long)in.slot0 * kBlocks + blk) * 256 + quarter * 64 + lane;
+    const long ml_step = (long)in.stride * ROWS, o_step = (long)in.stride * kBlocks * 256;
+    const int first = SPLIT ? wave : 0;
+    constexpr int kStep = SPLIT ? 4 : 1;
     float top = -INFINITY;
-#pragma unroll 4
-    for (int c = threadIdx.x / 32; c < in.chunks; c += 8) top = fmaxf(top, ml[c * step].x);
-    weight[threadIdx.x] = top;
-    __syncthreads();
+#pragma unroll 8
+    for (int c = first; c < in.chunks; c += kStep) top = fmaxf(top, ml[c * ml_step].x);
+    if (SPLIT) {
+        tops[wave][col] = top;
+        __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = fmaxf(top, weight[i * 32 + col]);
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, tops[w][col]);
+    }
     const float base = top == -INFINITY ? 0.f : top;
     float total = 0.f;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int c0 = 0; c0 < in.chunks; c0 += kJoin) {
-        const int n = min(in.chunks - c0, kJoin);
-        __syncthreads();
-        for (int c = threadIdx.x / 32; c < kJoin; c += 8) {
-            float2 v = make_float2(-INFINITY, 0.f);
-            if (c < n) v = ml[(c0 + c) * step];
-            weight[c * 32 + col] = __builtin_amdgcn_exp2f(v.x - base);
-            sums[c * 32 + col] = v.y;
+#pragma unroll 8
+    for (int c = first; c < in.chunks; c += kStep) {
+        const f32x4 v = o[c * o_step];
+        const float2 part = ml[c * ml_step];
+        const float f = __builtin_amdgcn_exp2f(part.x - base);
+        total = fmaf(part.y, f, total);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] = fmaf(v[i], f, sum[i]);
+    }
+    if (SPLIT) {
+        if (wave) {
+            sums[wave - 1][lane] = sum;
+            totals[wave - 1][lane] = total;
         }
         __syncthreads();
-        const f32x4 *o = reinterpret_cast<const f32x4 *>(p.o) + ((in.slot0 + (long)c0 * in.stride) * kBlocks + blk) * 256 + threadIdx.x;
-#pragma unroll 16
-        for (int c = 0; c < n; ++c) {
-            const float f = weight[c * 32 + col];
-            const f32x4 v = o[(long)c * in.stride * kBlocks * 256];
-            total = fmaf(sums[c * 32 + col], f, total);
+        if (wave) return;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum[i] = fmaf(v[i], f, sum[i]);
+        for (int w = 0; w < 3; ++w) {
+            total += totals[w][lane];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] += sums[w][lane][i];
         }
     }
     const int t0 = min(max(a.token_offsets[in.b], 0), a.N), n = min(max(a.token_offsets[in.b + 1], t0), a.N) - t0;
@@ -212,11 +236,21 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int per_token, P
     if (r >= n * per_token) return;
     const long at = (long)(t0 + r / per_token) * a.H + in.group / tiles * per_token + r % per_token;
     const float inv = total == 0.f ? 0.f : 1.f / total;
-    const int e = blk % (W / 32) * 32 + threadIdx.x / 64 * 8 + lane / 32 * 4;
+    const int e = blk % (W / 32) * 32 + quarter * 8 + lane / 32 * 4;
     *reinterpret_cast<u32x2 *>(a.o + at * W + e) = u32x2{pack_bf16x2(sum[0] * inv, sum[1] * inv),
                                                          pack_bf16x2(sum[2] * inv, sum[3] * inv)};
-    if (a.lse && blk % (W / 32) == 0 && threadIdx.x < 32)
+    if (a.lse && blk % (W / 32) == 0 && quarter == 0 && lane < 32)
         a.lse[at] = total == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(total)) / kLog2e;
+}
+
+template <int ROWS, int W>
+void launch_join(const PagedArgs &a, int per_token, const Parts &p, long groups, hipStream_t stream)
+{
+    // 512 blocks put two workgroups on a compute unit; with more, the four wavefronts need not share one.  (24000 blocks of
+    // 4 or 5 parts: 17 us whole, 32 us split; 64 blocks of 103 parts: 13 us whole, 8 us split.)
+    const long blocks = groups * (ROWS / 32) * (W / 32);
+    if (blocks < 2 * kCus) join_kernel<ROWS, W, true><<<(unsigned)(blocks * 4), 256, 0, stream>>>(a, per_token, p);
+    else join_kernel<ROWS, W, false><<<(unsigned)blocks, 256, 0, stream>>>(a, per_token, p);
 }
 
 __device__ __forceinline__ float max3(float a, float b, float c)

@@ -37,17 +37,15 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
 {
     constexpr int kRows = 32 * RT, kSteps = D / 16, kDt = D / 32;
     constexpr int kQ = RT * kSteps * 64 * 16;                // bytes of the queries, in operand order
-    constexpr int kP = kWaves * 32 * kKeys * 4;              // fp32 weights of a draft tile, for non-finite drafts
+    constexpr int kP = kWaves * kRows * kKeys * 2;           // weights of a draft tile, for non-finite drafts
     constexpr int kMerge = 2 * RT * kDt * 4096;              // two wavefronts' sums
-    constexpr int kPlan = 2 * kPlanB * 4;
-    constexpr int kLds0 = kQ + kP > kMerge ? kQ + kP : kMerge, kLds = kLds0 > kPlan ? kLds0 : kPlan;
+    constexpr int kLds = kQ + kP > kMerge ? kQ + kP : kMerge;
     __shared__ __attribute__((aligned(16))) char lds[kLds];
     __shared__ float2 ml[kWaves][kRows];
 
     const int G = a.H / a.Hkv;
     Item it;
-    if (!plan_item(a, G, a.Hkv, shape, parts, reinterpret_cast<int *>(lds), it)) return;
-    __syncthreads();
+    if (!plan_item(a, G, a.Hkv, shape, parts, it)) return;
     const int kvh = it.group / it.row_tiles, row0 = it.group % it.row_tiles * kRows;
     const int n_rows = it.n_tok * G;
     const int lane = lane_id(), wave = threadIdx.x / kWave, col = lane % 32, half = lane / 32;
@@ -61,6 +59,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
         if (r < n_rows) {
             const long at = (long)(it.t0 + r / G) * a.H + kvh * G + r % G;
             v = *reinterpret_cast<const u32x4 *>(a.q + at * D + 32 * (s / 2) + 16 * (l / 32) + 8 * (s % 2));
+            if (a.scale < 0.f) v ^= 0x80008000u;
         }
         q_lds[i] = v;
     }
@@ -83,12 +82,12 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
     const int lp = 31 - __builtin_clz(a.page);
     const int cached = (it.len + kKeys - 1) / kKeys;  // tiles
 
-    // Running maximum, weights and sums of one row tile's scores s (in powers of two); returns the weights in s.
-    auto softmax = [&](int rt, float *s) {
-        float top = s[0];
+    // Running maximum, weights and sums of one row tile's scores x, in powers of two once multiplied by `unit` > 0.
+    auto softmax = [&](int rt, f32x16 &x, float unit) {
+        float tops[2];
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-        top = halves_max(top);
+        for (int h = 0; h < 2; ++h) tops[h] = max3(max3(x[8 * h], x[8 * h + 1], x[8 * h + 2]), max3(x[8 * h + 3], x[8 * h + 4], x[8 * h + 5]), x[8 * h + 6]);
+        const float top = halves_max(max3(tops[0], tops[1], fmaxf(x[7], x[15])) * unit);
         if (__any(top > m[rt] + kSlack)) {
             const float now = fmaxf(m[rt], top);
             const float down = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[rt] - now);
@@ -100,17 +99,24 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
                 for (int i = 0; i < 16; ++i) o[rt][d][i] *= down;
         }
         const float base = m[rt] == -INFINITY ? 0.f : m[rt];
-        float sum = 0.f;
+        float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            s[i] = __builtin_amdgcn_exp2f(s[i] - base);
-            sum += s[i];
+            x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], unit, -base));
+            sum[i % 2] += x[i];
         }
-        l[rt] += sum;
+        l[rt] += sum[0] + sum[1];
+    };
+    // The sums of the score products are read by an instruction that the compiler does not see: 19 wait states after them.
+    auto settle = [&](f32x16 (&s)[RT]) {
+        if constexpr (RT == 2) asm volatile("s_nop 15\n\ts_nop 3" : "+v"(s[0]), "+v"(s[1]));
+        else asm volatile("s_nop 15\n\ts_nop 3" : "+v"(s[0]));
     };
 
     // ---- cached tokens
-    const float scale2 = a.scale * kLog2e;
+    // Positive and not zero: the largest product is the largest score (a negative scale turned the queries' signs), and it
+    // meets infinities.
+    const float scale2 = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-126f);
     u32x4 kr[D / 32], vr[kDt];
     const long stride = (long)a.page * D;  // of a head's page
     // Pages of a tile are read two tiles of the wavefront ahead, its codes and scales one: this half's 16 keys for the
@@ -178,20 +184,19 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
             k_id = page_id(min(next + kWaves, end - 1), pi >> 4);
             v_id = page_id(min(next + kWaves, end - 1), half);
         }
+        settle(s);
+        if (tail)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (i >= left) s[rt][i] = -INFINITY;
         bf16x8 p[RT][2];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            float x[16];
+            softmax(rt, s[rt], fmaxf(ks, 0x1p-126f));
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                x[i] = s[rt][i] * ks;
-                if (tail && i >= left) x[i] = -INFINITY;
-            }
-            softmax(rt, x);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] *= vs;
-            p[rt][0] = pack_bf16x8(x);
-            p[rt][1] = pack_bf16x8(x + 8);
+            for (int i = 0; i < 16; ++i) p[rt][i / 8][i % 8] = static_cast<__bf16>(s[rt][i] * vs);
         }
 #pragma unroll
         for (int d = 0; d < kDt; ++d)
@@ -221,22 +226,11 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
             for (int rt = 0; rt < RT; ++rt)
                 s[rt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, __builtin_bit_cast(bf16x8, q_lds[(rt * kSteps + st) * 64 + lane]), s[rt], 0, 0, 0);
         }
-        // Values, element by element; not finite: one of this half's 16 drafts has an infinity or NaN.
-        const int mine = drafts - j0 - 16 * half;
-        const uint16_t *vp = a.v_new + ((long)(it.t0 + j0 + 16 * half) * a.Hkv + kvh) * D + col;
-        u32x4 vb[kDt][2];
-        bool odd = false;
-#pragma unroll
-        for (int d = 0; d < kDt; ++d)
-#pragma unroll
-            for (int j = 0; j < 16; j += 2) {
-                const uint32_t lo = j < mine ? vp[(long)j * a.Hkv * D + 32 * d] : 0u;
-                const uint32_t hi = j + 1 < mine ? vp[(long)(j + 1) * a.Hkv * D + 32 * d] : 0u;
-                odd |= (lo & 0x7f80u) == 0x7f80u || (hi & 0x7f80u) == 0x7f80u;
-                vb[d][j / 8][j % 8 / 2] = lo | hi << 16;
-            }
-        const bool slow = __any(odd);
+        settle(s);
+        // Weights as the products' operand, and in LDS (row, draft) for drafts that are not finite.
+        uint16_t *w = reinterpret_cast<uint16_t *>(lds + kQ) + wave * kRows * kKeys;
         bf16x8 p[RT][2];
+        uint32_t all[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             const int r = row0 + rt * 32 + col;
@@ -245,40 +239,52 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
                 const int tok = r / G;
                 see = (a.mask ? a.mask[it.t0 + tok] : bits_below(tok + 1)) & bits_below(drafts);
             }
-            const uint32_t bits = (uint32_t)(see >> j0) >> 16 * half;
-            float x[16];
+            all[rt] = (uint32_t)(see >> j0);
+            const uint32_t bits = all[rt] >> 16 * half;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = bits >> i & 1 ? s[rt][i] * scale2 : -INFINITY;
-            softmax(rt, x);
-            p[rt][0] = pack_bf16x8(x);
-            p[rt][1] = pack_bf16x8(x + 8);
-            if (slow) {
-                // A weight of zero must not meet an infinity: each row adds the drafts that it sees, one by one.
-                float *w = reinterpret_cast<float *>(lds + kQ) + (wave * 32 + col) * kKeys;
+            for (int i = 0; i < 16; ++i)
+                if (!(bits >> i & 1)) s[rt][i] = -INFINITY;
+            softmax(rt, s[rt], scale2);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) w[16 * half + i] = x[i];
-                __builtin_amdgcn_wave_barrier();
-                const uint32_t all = (uint32_t)(see >> j0);
-                for (int j = 0; j < min(drafts - j0, kKeys); ++j) {
-                    const float f = *const_cast<volatile float *>(w + j);
-                    const uint16_t *v = a.v_new + ((long)(it.t0 + j0 + j) * a.Hkv + kvh) * D + 4 * half;
-                    if (all >> j & 1)
+            for (int i = 0; i < 16; ++i) p[rt][i / 8][i % 8] = static_cast<__bf16>(s[rt][i]);
 #pragma unroll
-                        for (int d = 0; d < kDt; ++d)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) o[rt][d][i] = fmaf(f, bf16_bits_to_f32(v[32 * d + i / 4 * 8 + i % 4]), o[rt][d][i]);
-                }
-                __builtin_amdgcn_wave_barrier();
-            }
+            for (int h = 0; h < 2; ++h) *reinterpret_cast<bf16x8 *>(w + (rt * 32 + col) * kKeys + 16 * half + 8 * h) = p[rt][h];
         }
-        if (slow) continue;
+        __builtin_amdgcn_wave_barrier();
+        const int mine = drafts - j0 - 16 * half;
+        const uint16_t *vp = a.v_new + ((long)(it.t0 + j0 + 16 * half) * a.Hkv + kvh) * D + col;
 #pragma unroll
-        for (int d = 0; d < kDt; ++d)
+        for (int d = 0; d < kDt; ++d) {
+            u32x4 vb[2];
+            bool odd = false;
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) {
+                const uint32_t lo = j < mine ? vp[(long)j * a.Hkv * D + 32 * d] : 0u;
+                const uint32_t hi = j + 1 < mine ? vp[(long)(j + 1) * a.Hkv * D + 32 * d] : 0u;
+                odd |= (lo & 0x7f80u) == 0x7f80u || (hi & 0x7f80u) == 0x7f80u;
+                vb[j / 8][j % 8 / 2] = lo | hi << 16;
+            }
+            if (__any(odd)) {
+                // A weight of zero must not meet an infinity or NaN: each row adds the drafts that it sees, one by one.
+                for (int j = 0; j < min(drafts - j0, kKeys); ++j) {
+                    const uint16_t *v = a.v_new + ((long)(it.t0 + j0 + j) * a.Hkv + kvh) * D + 32 * d + 4 * half;
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        const float f = bf16_bits_to_f32(*const_cast<volatile uint16_t *>(w + (rt * 32 + col) * kKeys + j));
+                        if (all[rt] >> j & 1)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[rt][d][i] = fmaf(f, bf16_bits_to_f32(v[i / 4 * 8 + i % 4]), o[rt][d][i]);
+                    }
+                }
+                continue;
+            }
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
-                    o[rt][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vb[d][h]), p[rt][h], o[rt][d], 0, 0, 0);
+                    o[rt][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vb[h]), p[rt][h], o[rt][d], 0, 0, 0);
+        }
+        __builtin_amdgcn_wave_barrier();
     }
 
     // ---- join the four wavefronts: 2 and 3 onto 0 and 1, then 1 onto 0
@@ -366,8 +372,10 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
     }
 }
 
-// 64 rows a workgroup where the batch's average row group has more than 32.
-int row_tiles(int N, int B, int per_token) { return (long)N * per_token > 32L * B ? 2 : 1; }
+// Row tiles of a workgroup: two for heads of 64 elements where the average row group has more than 32 rows (37 drafts over
+// 130001 tokens: 142 us against 170 us with one); one for heads of 128, whose sums of two leave the loads no registers
+// (16 sequences of four drafts over 16383 tokens: 49 us, 58 us with two).
+int row_tiles(int N, int B, int per_token, int D) { return D == 64 && (long)N * per_token > 32L * B ? 2 : 1; }
 
 constexpr int kSlots = 2 * kCus;
 
@@ -379,7 +387,7 @@ hipError_t launch(const CacheArgs &a, void *workspace, hipStream_t stream)
     Parts parts;
     parts_at(workspace, groups, kSlots, 32 * RT, D, &parts);
     cache_attn_kernel<D, RT><<<(unsigned)grid_bound(groups, kSlots), 256, 0, stream>>>(a, Shape{32 * RT, kKeys, kWaves, kSlots}, parts);
-    join_kernel<32 * RT, D><<<(unsigned)(groups * RT * (D / 32)), 256, 0, stream>>>(a, G, parts);
+    launch_join<32 * RT, D>(a, G, parts, groups, stream);
     return hipGetLastError();
 }
 
@@ -387,15 +395,14 @@ hipError_t launch(const CacheArgs &a, void *workspace, hipStream_t stream)
 
 size_t cache_workspace(int N, int B, int H, int Hkv, int D)
 {
-    const int rt = row_tiles(N, B, H / Hkv);
+    const int rt = row_tiles(N, B, H / Hkv, D);
     return parts_at(nullptr, group_bound(N, B, H / Hkv, Hkv, 32 * rt), kSlots, 32 * rt, D, nullptr);
 }
 
 hipError_t launch_cache_attn(const CacheArgs &a, void *workspace, hipStream_t stream)
 {
-    const bool two = row_tiles(a.N, a.B, a.H / a.Hkv) == 2;
-    if (a.D == 64) return two ? launch<64, 2>(a, workspace, stream) : launch<64, 1>(a, workspace, stream);
-    return two ? launch<128, 2>(a, workspace, stream) : launch<128, 1>(a, workspace, stream);
+    if (a.D == 128) return launch<128, 1>(a, workspace, stream);
+    return row_tiles(a.N, a.B, a.H / a.Hkv, a.D) == 2 ? launch<64, 2>(a, workspace, stream) : launch<64, 1>(a, workspace, stream);
 }
 
 }  // namespace ecospec

@@ -78,8 +78,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
     constexpr int kRows = 32 * RT;
     __shared__ __attribute__((aligned(16))) Lds lds;
     Item it;
-    if (!plan_item(a, a.H, 1, shape, parts, reinterpret_cast<int *>(lds.tile), it)) return;
-    __syncthreads();
+    if (!plan_item(a, a.H, 1, shape, parts, it)) return;
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 32, half = lane / 32;
     const int row0 = it.group * kRows, n_rows = it.n_tok * a.H;
     const int *table = a.block_table + (long)it.b * a.max_blocks;
@@ -428,7 +427,7 @@ hipError_t launch(const LatentArgs &a, void *workspace, hipStream_t stream)
     Parts parts;
     parts_at(workspace, groups, kCus, kRows, kR, &parts);
     latent_attn_kernel<RT><<<(unsigned)grid_bound(groups, kCus), kThreads, 0, stream>>>(a, Shape{kRows, kKeys, 2, kCus}, parts);
-    join_kernel<kRows, kR><<<(unsigned)(groups * RT * (kR / 32)), 256, 0, stream>>>(a, a.H, parts);
+    launch_join<kRows, kR>(a, a.H, parts, groups, stream);
     return hipGetLastError();
 }
 
