@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
     if (!plan_item(a, G, a.Hkv, shape, parts, it)) return;
     const int kvh = it.group / it.row_tiles, row0 = it.group % it.row_tiles * kRows;
     const int n_rows = it.n_tok * G;
-    const int lane = lane_id(), wave = threadIdx.x / kWave, col = lane % 32, half = lane / 32;
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 32, half = lane / 32;
 
     // Queries: step s, lane (row, half): elements 32 (s / 2) + 16 half + 8 (s % 2) .. + 7, as the codes' 16 bytes give.
     u32x4 *q_lds = reinterpret_cast<u32x4 *>(lds);
