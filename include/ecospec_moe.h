@@ -539,8 +539,10 @@ typedef struct {
  * position past max_blocks * page is dropped.  No two sequences may share a
  * page that is written.
  * max_tokens: at least the most new tokens of a sequence.
- * Limits: N, n_rows, B >= 1, B <= 1024; k_new, v_new 16-byte aligned.  One
- * kernel, deterministic.
+ * Limits: N, n_rows, B >= 1, B <= 1024; k_new, v_new 16-byte aligned;
+ * a launch of more than 2^31 threads is MOE_ERR_UNSUPPORTED, which
+ * (N + 2 * B * page) * Hkv * D <= 2^35 rules out.  One kernel,
+ * deterministic.
  */
 moe_status_t moe_cache_append(const moe_cache_t *cache, const void *k_new, const void *v_new, int n_rows,
                               const int32_t *rows, int N, int B, const int32_t *token_offsets, int max_tokens,

@@ -49,6 +49,7 @@ struct AppendArgs {
     uint8_t *k, *v;
     float *k_scale, *v_scale;
 };
+bool cache_append_fits(const AppendArgs &a);  // the launch's grid
 hipError_t launch_cache_append(const AppendArgs &a, hipStream_t stream);
 
 struct PromptArgs {

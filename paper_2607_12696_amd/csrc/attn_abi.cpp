@@ -202,6 +202,7 @@ moe_status_t moe_cache_append(const moe_cache_t *cache, const void *k_new, const
     a.v = cache->v;
     a.k_scale = cache->k_scale;
     a.v_scale = cache->v_scale;
+    if (!ecospec::cache_append_fits(a)) return MOE_ERR_UNSUPPORTED;
     return from_hip(ecospec::launch_cache_append(a, (hipStream_t)stream));
 }
 
