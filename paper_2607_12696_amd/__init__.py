@@ -551,13 +551,13 @@ def moe_add_rmsnorm(x, weight, eps: float, residual=None, qfmt: int = MOE_Q_NONE
 # --------------------------------------------------------------------------- attention
 
 def _int32_ptr(t, what: str, *shape) -> int:
-    if t.dtype != _torch().int32 or tuple(t.shape) != shape:
+    if t.dtype != _torch().int32 or t.shape != shape:
         raise ValueError(f"{what} must be int32 {list(shape)}")
     return _dev_ptr(t, what)
 
 
 def _bf16_ptr(t, what: str, *shape) -> int:
-    if t.dtype != _torch().bfloat16 or tuple(t.shape) != shape:
+    if t.dtype != _torch().bfloat16 or t.shape != shape:
         raise ValueError(f"{what} must be bfloat16 {list(shape)}")
     return _dev_ptr(t, what)
 
@@ -656,7 +656,7 @@ def _cache(k, v, k_scale, v_scale, block_table, cache_len, B: int) -> moe_cache_
     for t, what, dtype, shape in ((k, "k", torch.uint8, (n_pages, heads, page, D)), (v, "v", torch.uint8, (n_pages, heads, D, page)),
                                   (k_scale, "k_scale", torch.float32, (n_pages, heads)),
                                   (v_scale, "v_scale", torch.float32, (n_pages, heads))):
-        if t.dtype != dtype or tuple(t.shape) != shape:
+        if t.dtype != dtype or t.shape != shape:
             raise ValueError(f"{what} must be {dtype} {list(shape)}")
     blocks = block_table.shape[1]
     return moe_cache_t(heads, D, n_pages, page, blocks, _dev_ptr(k, "k"), _dev_ptr(v, "v"), _dev_ptr(k_scale, "k_scale"),

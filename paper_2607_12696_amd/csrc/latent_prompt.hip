@@ -1,8 +1,8 @@
 // Latent attention of prompts, expanded form: per head 192-element keys (128 of its own, 64 rotary ones that all heads
 // share) and 128-element values, causal.
 //
-// 640 operations a row, key and head against 512 bytes a key and head: bound by the matrix cores.  A workgroup takes 256
-// consecutive queries of one head, one a compute unit, 32 rows each of eight wavefronts, two on a SIMD.
+// 640 operations a row, key and head against 512 bytes a key and head: bound by the matrix cores.  A workgroup takes 128
+// consecutive queries of one head, 32 rows each of four wavefronts; two workgroups a compute unit, each with its own barriers.
 //   Scores are transposed (S^T = K Q^T): a lane holds one row, its scores are the value product's operand as they stand
 //   (O^T = V^T P^T), and V^T is read with the transposing LDS load.
 //   Three tiles are under way: while the matrix cores multiply the keys of tile t + 1 and the values of tile t - 1, the
@@ -18,11 +18,12 @@ namespace {
 
 constexpr int kDn = 128, kP = 64, kDv = 128, kDq = kDn + kP;
 constexpr int kKeys = 32;
-constexpr int kRt = 1, kWaves = 8, kRows = 32 * kRt * kWaves, kThreads = 64 * kWaves;  // kRt: row tiles of a wavefront
+constexpr int kRt = 1, kWaves = 4, kRows = 32 * kRt * kWaves, kThreads = 64 * kWaves;  // kRt: row tiles of a wavefront
 constexpr int kSteps = kDq / 16;
 constexpr int kRing = 4, kAhead = 3;  // key and value operands in registers
-constexpr int kLoads = 3;             // loads of a tile by a wavefront
+constexpr int kLoads = 5;             // loads of a tile by a wavefront
 constexpr int kScore = kRt * kSteps, kProducts = kScore + kRt * 8;  // of a tile
+constexpr int kLoadFrom = kProducts - 2 * kLoads;  // a load behind every other product from here on
 constexpr int kEdge = kRows / kKeys + 1;  // most tiles that some rows of a workgroup see in part
 constexpr float kSlack = 8.f;
 
@@ -41,14 +42,15 @@ constexpr int kKeyTile = 3 * kPanel, kValueTile = kKeys * kDv * 2;
 struct Tiles {
     char k[3][kKeyTile];    // panel, row r, chunk c of 16 bytes at place c ^ (r >> 1 & 7); the last panel is the rotary part
     char v[5][kValueTile];  // panel of 32 elements, row
-    uint32_t some[kEdge][kThreads];  // which weights of a lane are not zero, in a tile with infinities or NaN
-    char nothing[1024];
+    uint16_t some[kEdge][kThreads];  // which weights of a lane are not zero, in a tile with infinities or NaN
 };
 
 union Lds {
     char q[kWaves][32 * kRt * kDq * 2];  // the queries of each wavefront, before the loop: at c ^ (r >> 1 & 7)
     Tiles t;
 };
+static_assert(kRt == 1, "16 weights of a lane");
+static_assert(2 * sizeof(Lds) <= 160 * 1024, "two workgroups a compute unit");
 
 // The score products, sums in vector registers, which the vector unit works on; a register written by the vector
 // unit needs two wait states before a product reads it.
@@ -62,7 +64,7 @@ __device__ __forceinline__ void mfma_next(f32x16 &s, const bf16x8 &k, const bf16
     asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(k), "v"(q));
 }
 
-__global__ __launch_bounds__(kThreads, kWaves / 4) void prompt_kernel(PromptArgs a, int blocks)
+__global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int blocks)
 {
     __shared__ __attribute__((aligned(16))) Lds lds;
     // A head's row blocks on one XCD; the longest of all heads first, so that no long one is left for the end.
@@ -106,40 +108,42 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void prompt_kernel(PromptArgs
     }
     __syncthreads();
 
-    // ---- loads: of the first four wavefronts, w brings rows 8 w .. 8 w + 7 of a tile's keys, a panel a load; of the others,
-    // w + 4 brings panel w of its values, 16 rows a load (and a load of nothing, so that all count alike).  Rows past the last
-    // key, and tiles past the last, become zeros.
-    const bool keys = wave < 4;
-    const uint16_t *src = keys ? a.k + h * a.k_head + k0 * a.k_stride : a.v + h * a.v_head + k0 * a.v_stride;
+    // ---- loads: wavefront w brings rows 8 w .. 8 w + 7 of a tile's keys, a panel a load, and panel w of its values, 16 rows a
+    // load.  Rows past the last key, and tiles past the last, become zeros.
+    const uint16_t *src_k = a.k + h * a.k_head + k0 * a.k_stride, *src_v = a.v + h * a.v_head + k0 * a.v_stride;
     const uint16_t *rope = a.k_rope + (long)k0 * kP;
-    const uint32_t stride2 = (uint32_t)(keys ? a.k_stride : a.v_stride) * 2;
+    const uint32_t stride_k = (uint32_t)a.k_stride * 2, stride_v = (uint32_t)a.v_stride * 2;
     const int e = 8 * wave + lane / 8, place = (lane % 8) ^ (e >> 1 & 7);
-    const uint32_t off = keys ? e * stride2 + place * 16 : lane / 4 * stride2 + (wave - 4) * 64 + lane % 4 * 16;
-    const uint32_t off1 = keys ? off + 128 : off + 16 * stride2, rope_off = (uint32_t)(e * kP * 2 + place * 16);
+    const uint32_t off_k = e * stride_k + place * 16, off_rope = (uint32_t)(e * kP * 2 + place * 16);
+    const uint32_t off_v = lane / 4 * stride_v + wave * 64 + lane % 4 * 16, off_low = off_v + 16 * stride_v;
     // The tile to load next: its place in memory and in the rings.
-    const uint32_t ring = __builtin_amdgcn_readfirstlane(keys ? lds_addr(lds.t.k) + wave * 1024 : lds_addr(lds.t.v) + (wave - 4) * 2048);
-    const uint32_t turn = keys ? kKeyTile : kValueTile, around = keys ? 3 * kKeyTile : 5 * kValueTile;
-    const uint32_t step1 = keys ? kPanel : 1024, nothing = __builtin_amdgcn_readfirstlane(lds_addr(lds.t.nothing));
+    const uint32_t ring_k = __builtin_amdgcn_readfirstlane(lds_addr(lds.t.k) + wave * 1024);
+    const uint32_t ring_v = __builtin_amdgcn_readfirstlane(lds_addr(lds.t.v) + wave * 2048);
     int left_k = tiles ? nk : 0;  // keys from the tile on
-    uint32_t to = 0;
-    u32x4 row_src, rope_src;
+    uint32_t to_k = ring_k, to_v = ring_v;
+    u32x4 k_src, rope_src, v_src;
     auto aim = [&] {
         const int rows = max(min(left_k, kKeys), 0);
-        row_src = rsrc_words(src, rows ? (uint32_t)(rows - 1) * stride2 + kDn * 2 : 0);
-        rope_src = rsrc_words(rope, keys ? (uint32_t)rows * kP * 2 : 0);
+        k_src = rsrc_words(src_k, rows ? (uint32_t)(rows - 1) * stride_k + kDn * 2 : 0);
+        rope_src = rsrc_words(rope, (uint32_t)rows * kP * 2);
+        v_src = rsrc_words(src_v, rows ? (uint32_t)(rows - 1) * stride_v + kDv * 2 : 0);
     };
     auto advance = [&] {
         left_k -= kKeys;
         if (left_k > 0) {
-            src += kKeys / 2 * stride2;
+            src_k += kKeys / 2 * stride_k;
+            src_v += kKeys / 2 * stride_v;
             rope += kKeys * kP;
         }
-        to = to + turn == around ? 0 : to + turn;
+        to_k = to_k == ring_k + 2 * kKeyTile ? ring_k : to_k + kKeyTile;
+        to_v = to_v == ring_v + 4 * kValueTile ? ring_v : to_v + kValueTile;
     };
     auto load = [&](int n) {
-        if (n == 0) load16_lds(row_src, off, ring + to);
-        else if (n == 1) load16_lds(row_src, off1, ring + to + step1);
-        else load16_lds(rope_src, rope_off, keys ? ring + to + 2 * kPanel : nothing);
+        if (n == 0) load16_lds(k_src, off_k, to_k);
+        else if (n == 1) load16_lds(k_src, off_k + 128, to_k + kPanel);
+        else if (n == 2) load16_lds(rope_src, off_rope, to_k + 2 * kPanel);
+        else if (n == 3) load16_lds(v_src, off_v, to_v);
+        else load16_lds(v_src, off_low, to_v + 1024);
     };
 #pragma unroll 1
     for (int t = 0; t < 2; ++t) {
@@ -310,7 +314,7 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void prompt_kernel(PromptArgs
         }
         products(next, [&](int c) {
             weights(s, c);
-            if (c >= kScore && c < kScore + 2 * kLoads && (c - kScore) % 2 == 0) load((c - kScore) / 2);
+            if (c >= kLoadFrom && (c - kLoadFrom) % 2 == 0) load((c - kLoadFrom) / 2);
         });
 #pragma unroll
         for (int rt = 0; rt < kRt; ++rt)
@@ -322,7 +326,7 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void prompt_kernel(PromptArgs
             uint32_t some = 0;
 #pragma unroll
             for (int i = 0; i < 16 * kRt; ++i) some |= (s[i / 16][i % 16] != 0.f ? 1u : 0u) << i;
-            lds.t.some[t - edge][threadIdx.x] = some;
+            lds.t.some[t - edge][threadIdx.x] = (uint16_t)some;
         }
     };
 
@@ -383,7 +387,7 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void prompt_kernel(PromptArgs
             for (int j = 0; j < min(limit(row) - at, kKeys); ++j) {
                 const uint16_t v = a.v[h * a.v_head + (long)(k0 + at + j) * a.v_stride + el];
                 if (!not_finite(v)) continue;
-                const uint32_t some = lds.t.some[e][wave * kWave + j / 4 % 2 * 32 + col] >> (16 * rt + j / 8 * 4 + j % 4) & 1;
+                const uint32_t some = lds.t.some[e][wave * kWave + j / 4 % 2 * 32 + col] >> (j / 8 * 4 + j % 4) & 1;
                 c = fmaf(some ? 1.f : 0.f, bf16_bits_to_f32(v), c);
             }
         }
