@@ -416,8 +416,9 @@ typedef enum {
  *   sum, y or q may be NULL (q and scales exactly when qfmt is MOE_Q_NONE),
  *   not all three.  sum may be the buffer of x or of residual, and y that of
  *   x; other overlaps are not allowed.
- * Limits: T >= 1, d % 32 == 0, d <= 16384, finite eps >= 0; all pointers 16-byte
- * aligned (scales: 4).  One kernel, deterministic.
+ * Limits: T >= 1; T <= 2^21, d % 32 == 0 and d <= 16384 (else
+ * MOE_ERR_UNSUPPORTED), finite eps >= 0; all pointers 16-byte aligned (scales:
+ * 4).  One kernel, deterministic.
  */
 moe_status_t moe_add_rmsnorm(const void *x, const void *residual, const void *weight, int T, int d, float eps,
                              int qfmt, void *sum, void *y, void *q, void *scales, void *stream);

@@ -26,6 +26,7 @@ constexpr int kMaxBatch = 1024;
 constexpr int kMaxHeads = 1024;
 constexpr long kMaxRows = 1L << 24;  // query rows (token, head) of a call
 constexpr int kMaxWidth = 16384;     // of a normalised row
+constexpr int kMaxNormRows = 1 << 21;  // by 1024 threads: a launch's 2^31
 constexpr long kMaxPromptRows = 1L << 30;
 constexpr int64_t kMaxStride = 1L << 23;  // elements between a prompt's keys
 
@@ -91,7 +92,7 @@ moe_status_t moe_add_rmsnorm(const void *x, const void *residual, const void *we
     for (const void *p : ptr)
         if (!aligned(p, 16)) return MOE_ERR_INVALID_ARG;
     if (!aligned(scales, 4)) return MOE_ERR_INVALID_ARG;
-    if (d % 32 || d > kMaxWidth) return MOE_ERR_UNSUPPORTED;
+    if (d % 32 || d > kMaxWidth || T > kMaxNormRows) return MOE_ERR_UNSUPPORTED;
     return from_hip(ecospec::launch_add_rmsnorm(
         static_cast<const uint16_t *>(x), static_cast<const uint16_t *>(residual),
         static_cast<const uint16_t *>(weight), T, d, eps, qfmt, static_cast<uint16_t *>(sum),

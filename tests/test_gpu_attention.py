@@ -349,3 +349,93 @@ def test_other_stream_and_graph():
         call()
         assert torch.equal(o, got[0]) and torch.equal(lse, got[1])
         compare(latent_rows(lc, some_rows([4, 2], 16, np.random.default_rng(step), most=12)), *got)
+
+
+# ----------------------------------------------------------------------------- each variant and plan
+
+@pytest.mark.parametrize("scale", [-0.07, 0.0])
+def test_scales_that_are_not_positive(scale):
+    for c, run, rows, n, H in ((latent_case([3, 1], [90, 33], 8, 16, seed=21), latent_run, latent_rows, [3, 1], 8),
+                               (cache_case([3, 1], [90, 33], 8, 2, 64, 16, seed=22), cache_run, cache_rows, [3, 1], 8),
+                               (prompt_case([60, 9], [70, 9], 2, seed=23), prompt_run, prompt_rows, [60, 9], 2)):
+        c["scale"] = scale
+        compare(rows(c, some_rows(n, H, np.random.default_rng(4))), *run(c))
+
+
+@pytest.mark.parametrize("counts,lens,H", [([3, 4, 2], [70, 300, 1025], 16), ([1, 2], [640, 31], 40), ([4] * 5, [2000, 0, 7, 96, 129], 12)])
+def test_latent_of_two_row_tiles(counts, lens, H):
+    """33 to 64 rows a sequence on average."""
+    assert 32 * len(counts) < sum(counts) * H <= 64 * len(counts)
+    c = latent_case(counts, lens, H, 32, seed=24, poison=True)
+    compare(latent_rows(c, some_rows(counts, H, np.random.default_rng(5), most=80)), *latent_run(c))
+
+
+def test_more_sequences_than_lanes():
+    """150 sequences, some without drafts, some without a cache."""
+    rng = np.random.default_rng(6)
+    counts = [int(n) for n in rng.integers(0, 4, 150)]
+    lens = [int(n) for n in rng.integers(0, 400, 150)]
+    c = latent_case(counts, lens, 8, 16, seed=25, poison=True)
+    compare(latent_rows(c, some_rows(counts, 8, rng)), *latent_run(c))
+    c = cache_case(counts, lens, 8, 2, 64, 16, seed=26, poison=True)
+    compare(cache_rows(c, some_rows(counts, 8, rng)), *cache_run(c))
+    c = prompt_case(counts, [n + m for n, m in zip(counts, lens)], 2, seed=27)
+    compare(prompt_rows(c, some_rows(counts, 2, rng)), *prompt_run(c, max_tokens=3))
+
+
+@pytest.mark.parametrize("B", [700, 1024])
+def test_many_row_groups(B):
+    """More row groups than run at once, cut (700) and whole (1024 latent, 4 x 1024 of four key/value heads)."""
+    rng = np.random.default_rng(7)
+    lens = [int(n) for n in rng.integers(0, 90, B)]
+    c = latent_case([1] * B, lens, 16, 16, seed=28, poison=True)
+    compare(latent_rows(c, some_rows([1] * B, 16, rng)), *latent_run(c))
+    c = cache_case([1] * B, lens, 8, 4, 128, 16, seed=29, poison=True)
+    compare(cache_rows(c, some_rows([1] * B, 8, rng)), *cache_run(c))
+
+
+@pytest.mark.parametrize("D,page", [(64, 16), (128, 64)])
+def test_cache_scales_of_any_value(D, page):
+    """Page scales that are no powers of two, over 12 orders of magnitude within a sequence."""
+    counts, lens = [3, 2], [777, 40]
+    c = cache_case(counts, lens, 16, 4, D, page, seed=30, poison=True)
+    rng = np.random.default_rng(8)
+    for x in ("ks", "vs"):
+        used = torch.isfinite(c[x])
+        c[x][used] = torch.from_numpy((0.004 * rng.lognormal(0.0, 0.8, c[x].shape)).astype(np.float32))[used]
+    c["vs"][int(c["table"][0, 1])] = 3e-14
+    compare(cache_rows(c, some_rows(counts, 16, rng)), *cache_run(c))
+
+
+def test_prompt_of_separate_strided_tensors():
+    c = prompt_case([140, 3], [150, 40], 3, seed=31)
+    k = draw.normal(31, "k", 190, 3, 144)[..., :128]  # rows of 3 * 144
+    v = draw.normal(31, "v", 3, 190, 136).transpose(0, 1)[..., :128]  # heads apart
+    c["kv"] = torch.cat([k, v], 2)
+    q, rope, qo, ko = dev(c["q"], c["rope"], c["qo"], c["ko"])
+    kd = torch.empty(190, 3, 144, dtype=torch.bfloat16, device=DEV)[..., :128]
+    vd = torch.empty(3, 190, 136, dtype=torch.bfloat16, device=DEV).transpose(0, 1)[..., :128]
+    kd.copy_(k)
+    vd.copy_(v)
+    o, lse = moe.moe_latent_prompt(q, kd, rope, vd, qo, ko, c["scale"])
+    compare(prompt_rows(c, some_rows([140, 3], 3, np.random.default_rng(9), most=80)), o, lse)
+
+
+def test_given_outputs_and_no_log_sums():
+    """Outputs in the caller's buffers, nothing past them written; and a null lse through the C interface."""
+    import ctypes as C
+    c = cache_case([3, 2], [50, 700], 16, 4, 64, 16, seed=32)
+    want, _ = cache_run(c)
+    room = torch.full((7, 16, 64), 5.0, dtype=torch.bfloat16, device=DEV)
+    lse = torch.full((7, 16), 5.0, device=DEV)
+    cache_run(c, o=room[:5], lse=lse[:5])
+    assert torch.equal(room[:5], want) and torch.all(room[5:] == 5) and torch.all(lse[5:] == 5)
+
+    p = prompt_case([40], [40], 2, seed=33)
+    q, kv, rope, qo, ko = dev(p["q"], p["kv"], p["rope"], p["qo"], p["ko"])
+    want, _ = moe.moe_latent_prompt(q, kv[..., :128], rope, kv[..., 128:], qo, ko, p["scale"])
+    o = torch.empty_like(want)
+    a = moe.moe_prompt_t(40, 40, 1, 2, 128, 64, 128, 40, qo.data_ptr(), ko.data_ptr(), q.data_ptr(), kv.data_ptr(), rope.data_ptr(),
+                         kv.data_ptr() + 256, 512, 256, 512, 256, p["scale"])
+    assert moe.lib().moe_latent_prompt(C.byref(a), o.data_ptr(), None, torch.cuda.current_stream().cuda_stream) == moe.MOE_OK
+    assert torch.equal(o, want)

@@ -98,3 +98,60 @@ def test_special_values():
     vn[6:, 1] = 2.0 ** -126  # below the smallest scale's range
     off = draw.offsets([6, 6])
     same(run(c, kn, vn, off), expect(c, kn, vn, off))
+
+
+@pytest.mark.parametrize("D,page", [(64, 16), (128, 64), (128, 128)])
+def test_scales_that_are_no_powers_of_two(D, page):
+    """A continued page whose scale the caller chose: kept where it is enough, a power of two where it grows."""
+    lens, counts = [page // 2 + 1, page - 1, 3], [4, 3, page]
+    c = empty_cache(lens, 3, D, page, page, seed=11)
+    for x in ("ks", "vs"):
+        c[x] = torch.from_numpy(np.random.default_rng(11).uniform(0.002, 0.02, c[x].shape).astype(np.float32))
+    kn, vn = draw.normal(11, "kn", sum(counts), 3, D, std=1.5), draw.normal(11, "vn", sum(counts), 3, D, std=0.7)
+    kn[:, 1] *= 9
+    off = draw.offsets(counts)
+    same(run(c, kn, vn, off), expect(c, kn, vn, off))
+
+
+def test_many_sequences_and_gathered_rows():
+    """200 sequences, some with nothing new; rows in any order, the same one more than once."""
+    rng = np.random.default_rng(12)
+    lens, counts = [int(n) for n in rng.integers(0, 100, 200)], [int(n) for n in rng.integers(0, 25, 200)]
+    c = empty_cache(lens, 2, 64, 16, 25, seed=12)
+    kn, vn = draw.normal(12, "kn", 64, 2, 64), draw.normal(12, "vn", 64, 2, 64, std=4.0)
+    rows = torch.from_numpy(rng.integers(0, 64, sum(counts)).astype(np.int32))
+    off = draw.offsets(counts)
+    w = expect(c, kn, vn, off, rows)
+    same(run(c, kn, vn, off, rows), w)
+    same(run(c, kn, vn, off, rows, max_tokens=24), w)
+
+
+def test_other_stream_and_graph():
+    """Captured once, replayed as the cache grows: the lengths are read on the device."""
+    lens, counts, D, page = [5, 30], [3, 2], 64, 16
+    c = empty_cache(lens, 2, D, page, 30, seed=13)
+    d = {x: t.to(DEV) for x, t in c.items()}
+    kn, vn = draw.normal(13, "kn", 5, 2, D).to(DEV), draw.normal(13, "vn", 5, 2, D).to(DEV)
+    off = draw.offsets(counts).to(DEV)
+
+    def call():
+        moe.moe_cache_append(kn, vn, off, d["k"], d["v"], d["ks"], d["vs"], d["table"], d["len"], max_tokens=3)
+
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        call()
+    torch.cuda.synchronize()
+    same(d, expect(c, kn.cpu(), vn.cpu(), off.cpu()))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for step in range(4):
+        d["len"] += off.diff()
+        kn.copy_(draw.normal(50 + step, "kn", 5, 2, D, std=3.0 ** step))
+        vn.copy_(draw.normal(50 + step, "vn", 5, 2, D, std=2.0 ** step))
+        torch.cuda.synchronize()
+        c = {x: t.cpu() for x, t in d.items()}
+        g.replay()
+        torch.cuda.synchronize()
+        same(d, expect(c, kn.cpu(), vn.cpu(), off.cpu()))

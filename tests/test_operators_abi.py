@@ -114,6 +114,17 @@ def test_prompt_rejects(change, status):
     assert prompt(**change) == status
 
 
+def test_launches_that_do_not_fit():
+    """Sizes past what one launch or 32-bit offsets reach are refused, not cut."""
+    assert norm(T=(1 << 21) + 1) == UNS
+    big = dict(N=1 << 30, n_rows=1 << 30, most=1 << 30)
+    assert append(cache(Hkv=256, D=128, page=16), **big) == UNS
+    assert append(cache(Hkv=256, D=64, page=128), **big) == UNS
+    assert prompt(k_stride=1 << 24) == UNS and prompt(v_stride=1 << 24) == UNS
+    assert prompt(N=1 << 29, H=8, max_tokens=1) == UNS
+    assert prompt(N=1 << 20, B=1024, H=8, max_tokens=1 << 20) == UNS
+
+
 def test_short_workspaces():
     n, c = C.c_size_t(), latent_cache()
     assert moe.lib().moe_latent_attn_workspace_size(C.byref(c), 4, 2, 16, C.byref(n)) == OK and n.value > 0
