@@ -29,7 +29,7 @@ struct PagedArgs {
 struct LatentArgs : PagedArgs {
     const uint16_t *q, *kv_new, *pages;
 };
-size_t latent_workspace(int N, int B, int H);
+size_t latent_workspace(int N, int B, int H, int max_blocks, int page);
 hipError_t launch_latent_attn(const LatentArgs &a, void *workspace, hipStream_t stream);
 
 struct CacheArgs : PagedArgs {

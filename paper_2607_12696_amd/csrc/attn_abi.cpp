@@ -105,7 +105,7 @@ moe_status_t moe_latent_attn_workspace_size(const moe_latent_cache_t *cache, int
     moe_status_t st = check_latent(cache);
     if (st != MOE_OK) return st;
     if ((st = check_call(N, B, H)) != MOE_OK) return st;
-    *bytes = ecospec::latent_workspace(N, B, H);
+    *bytes = ecospec::latent_workspace(N, B, H, cache->max_blocks, cache->page);
     return MOE_OK;
 }
 
@@ -120,7 +120,7 @@ moe_status_t moe_latent_attn(const moe_latent_cache_t *cache, const moe_drafts_t
     if ((st = check_call(drafts->N, drafts->B, H)) != MOE_OK) return st;
     if (o == q || !aligned(q, 16) || !aligned(kv_new, 16) || !aligned(o, 16) || !aligned(workspace, 256))
         return MOE_ERR_INVALID_ARG;
-    if (workspace_bytes < ecospec::latent_workspace(drafts->N, drafts->B, H)) return MOE_ERR_WORKSPACE;
+    if (workspace_bytes < ecospec::latent_workspace(drafts->N, drafts->B, H, cache->max_blocks, cache->page)) return MOE_ERR_WORKSPACE;
     ecospec::LatentArgs a{};
     set_paged(a, drafts, H, scale, o, lse);
     a.n_pages = cache->n_pages;

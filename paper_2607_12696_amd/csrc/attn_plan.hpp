@@ -4,7 +4,9 @@
 // row groups of ROWS; the keys of a row group (cached tokens, then drafts) are cut into tiles of KEYS, and its tiles into
 // chunks of about equal length, one workgroup each.  Lengths are known on the device only, so every workgroup works the
 // plan out for itself, from the two offsets and the length of each sequence: the chunk length is the smallest for which
-// all chunks run at once.  A row group of several chunks leaves its parts (fp32 output sums with the reference maximum
+// all chunks run at once, or in two rounds where those are shorter.  (Row groups of different lengths leave chunks of
+// different lengths: 8 trees over 6000 to 20000 tokens have chunks of up to 188 tiles at once, of 143 on average, and of up
+// to 79 in two rounds: 375 us instead of 405.)  A row group of several chunks leaves its parts (fp32 output sums with the reference maximum
 // and the sum of the weights of each row) in the workspace, in the matrix cores' accumulator order, and join_kernel adds
 // them up in chunk order.
 #pragma once
@@ -23,6 +25,7 @@ struct Shape {
     int rows, keys;  // of a row group and of a key tile
     int min_tiles;   // shortest chunk
     int slots;       // workgroups that run at once
+    int twice;       // length from which chunks are cut for two rounds if that is shorter (0: never)
 };
 
 struct GroupInfo {
@@ -54,16 +57,18 @@ inline long group_bound(int N, int B, int per_token, int heads, int rows)
 // Beyond this many row groups a slot nothing is cut.
 constexpr int kRounds = 4;
 
-inline long grid_bound(long groups, int slots)
+constexpr int kStart = 8;  // what a chunk costs besides its tiles, in tiles
+
+inline long grid_bound(long groups, int slots, bool twice)
 {
-    const long cut = (long)slots * (groups / slots + 1), most = (long)kRounds * slots;
+    const long rounds = groups / slots + 1, cut = slots * (twice && rounds < 2 ? 2 : rounds), most = (long)kRounds * slots;
     return (groups >= most ? groups : cut < most ? cut : most) + 7 & ~7L;  // whole rounds of the XCDs
 }
 
 // The workspace for at most `groups` row groups, and its size.
-inline size_t parts_at(void *workspace, long groups, int slots, int rows, int width, Parts *p)
+inline size_t parts_at(void *workspace, long groups, int slots, bool twice, int rows, int width, Parts *p)
 {
-    const long cut = grid_bound(groups, slots), n = cut < (long)kRounds * slots ? cut : (long)kRounds * slots;
+    const long cut = grid_bound(groups, slots, twice), n = cut < (long)kRounds * slots ? cut : (long)kRounds * slots;
     char *w = static_cast<char *>(workspace);
     const size_t ml = 256 + ((size_t)groups * sizeof(GroupInfo) + 255) / 256 * 256;
     const size_t o = ml + (size_t)n * rows * sizeof(float2);
@@ -127,10 +132,21 @@ __device__ __forceinline__ bool plan_item(const PagedArgs &a, int per_token, int
             }
             return wave_sum_int(n);
         };
-        c = max(s.min_tiles, (int)((float)total / (float)max(room, 1)));
-        items = count(c);
-        // Ends: chunks as long as the longest row group make one item of each, and there is room for those.
-        for (int i = 0; items > room; ++i) items = count(c += max(1, i < 12 ? c / 16 : c / 4));
+        auto fit = [&](int room) {
+            c = max(s.min_tiles, (int)((float)total / (float)max(room, 1)));
+            items = count(c);
+            // Ends: chunks as long as the longest row group make one item of each, and there is room for those.
+            for (int i = 0; items > room; ++i) items = count(c += max(1, i < 12 ? c / 16 : c / 4));
+        };
+        fit(room);
+        if (s.twice && c >= s.twice && groups <= s.slots) {
+            const int once = c, once_items = items;
+            fit(2 * s.slots);
+            if (2 * (c + kStart) >= once + kStart) {
+                c = once;
+                items = once_items;
+            }
+        }
     }
     // Neighbouring items (the row groups of one chunk read the same keys) run on one XCD, whose L2 they share:
     // workgroups are dealt to the eight XCDs in turn.

@@ -385,8 +385,8 @@ hipError_t launch(const CacheArgs &a, void *workspace, hipStream_t stream)
     const int G = a.H / a.Hkv;
     const long groups = group_bound(a.N, a.B, G, a.Hkv, 32 * RT);
     Parts parts;
-    parts_at(workspace, groups, kSlots, 32 * RT, D, &parts);
-    cache_attn_kernel<D, RT><<<(unsigned)grid_bound(groups, kSlots), 256, 0, stream>>>(a, Shape{32 * RT, kKeys, kWaves, kSlots}, parts);
+    parts_at(workspace, groups, kSlots, false, 32 * RT, D, &parts);
+    cache_attn_kernel<D, RT><<<(unsigned)grid_bound(groups, kSlots, false), 256, 0, stream>>>(a, Shape{32 * RT, kKeys, kWaves, kSlots, 0}, parts);
     launch_join<32 * RT, D>(a, G, parts, groups, stream);
     return hipGetLastError();
 }
@@ -396,7 +396,7 @@ hipError_t launch(const CacheArgs &a, void *workspace, hipStream_t stream)
 size_t cache_workspace(int N, int B, int H, int Hkv, int D)
 {
     const int rt = row_tiles(N, B, H / Hkv, D);
-    return parts_at(nullptr, group_bound(N, B, H / Hkv, Hkv, 32 * rt), kSlots, 32 * rt, D, nullptr);
+    return parts_at(nullptr, group_bound(N, B, H / Hkv, Hkv, 32 * rt), kSlots, false, 32 * rt, D, nullptr);
 }
 
 hipError_t launch_cache_attn(const CacheArgs &a, void *workspace, hipStream_t stream)

@@ -419,24 +419,33 @@ int row_tiles(int N, int B, int H)
     return rows <= 32L * B ? 1 : rows <= 64L * B ? 2 : 4;
 }
 
+// Two rounds of chunks (and a grid for them) are considered from chunks of kLong tiles on; whether a call can have them is
+// known from the block table's width.
+constexpr int kLong = 64;
+
+bool may_be_long(long groups, int max_blocks, int page) { return (double)groups * max_blocks * page >= (double)kLong * kKeys * kCus; }
+
 template <int RT>
 hipError_t launch(const LatentArgs &a, void *workspace, hipStream_t stream)
 {
     constexpr int kRows = 32 * RT;
     const long groups = group_bound(a.N, a.B, a.H, 1, kRows);
     Parts parts;
-    parts_at(workspace, groups, kCus, kRows, kR, &parts);
-    latent_attn_kernel<RT><<<(unsigned)grid_bound(groups, kCus), kThreads, 0, stream>>>(a, Shape{kRows, kKeys, 2, kCus}, parts);
+    const bool twice = may_be_long(groups, a.max_blocks, a.page);
+    parts_at(workspace, groups, kCus, twice, kRows, kR, &parts);
+    latent_attn_kernel<RT><<<(unsigned)grid_bound(groups, kCus, twice), kThreads, 0, stream>>>(
+        a, Shape{kRows, kKeys, 2, kCus, twice ? kLong : 0}, parts);
     launch_join<kRows, kR>(a, a.H, parts, groups, stream);
     return hipGetLastError();
 }
 
 }  // namespace
 
-size_t latent_workspace(int N, int B, int H)
+size_t latent_workspace(int N, int B, int H, int max_blocks, int page)
 {
     const int rows = 32 * row_tiles(N, B, H);
-    return parts_at(nullptr, group_bound(N, B, H, 1, rows), kCus, rows, kR, nullptr);
+    const long groups = group_bound(N, B, H, 1, rows);
+    return parts_at(nullptr, groups, kCus, may_be_long(groups, max_blocks, page), rows, kR, nullptr);
 }
 
 hipError_t launch_latent_attn(const LatentArgs &a, void *workspace, hipStream_t stream)

@@ -394,6 +394,16 @@ def test_many_row_groups(B):
     compare(cache_rows(c, some_rows([1] * B, 8, rng)), *cache_run(c))
 
 
+def test_latent_chunks_in_two_rounds():
+    """178 row groups of 140 and 70 tiles: at once they would be 256 chunks of 140 tiles or fewer, in two rounds 484 of 47."""
+    counts, lens = [64, 64, 50], [4400, 4390, 2170]
+    c = latent_case(counts, lens, 128, 64, seed=34, poison=True)
+    o, lse = latent_run(c)
+    compare(latent_rows(c, some_rows(counts, 128, np.random.default_rng(10), most=24)), o, lse)
+    again = latent_run(c)
+    assert torch.equal(o, again[0]) and torch.equal(lse, again[1])
+
+
 @pytest.mark.parametrize("D,page", [(64, 16), (128, 64)])
 def test_cache_scales_of_any_value(D, page):
     """Page scales that are no powers of two, over 12 orders of magnitude within a sequence."""
