@@ -12,6 +12,9 @@
 // one in flight), chunks of 16 bytes XORed with the row's low bits so that neither kind of read meets a bank twice.  With
 // one wavefront on a SIMD nothing else hides the softmax: it runs between the value products of the tile before.  One
 // barrier a tile.
+//   Measured: trees of 4 to 16 tokens of 8 sequences over 6000 to 20000 tokens, 128 heads, 375 us with the join (867
+// TFLOP/s; a large library product reaches 1250); 48 single tokens over 1300 to 6000 tokens 97 us, 16 of them the join
+// of 67 MB of parts; one token of 16 heads over 4097 tokens 17 us, the fixed cost of two launches.
 #include "attn_plan.hpp"
 
 namespace ecospec {
@@ -412,12 +415,19 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
     }
 }
 
-// Row tiles of a workgroup: as few as hold the average sequence's rows.
+// Row tiles of a workgroup: as few as hold the average sequence's rows.  Tiles without rows cost their products (32 tokens
+// of 16 heads over up to 9000: 56 us with one tile, 88 with four); more workgroups for the same rows read the keys again
+// (64 sequences of up to four such tokens: 106 us with two tiles, 137 with one, 140 with four; 48 tokens of 128 heads: 94
+// with four, 114 with two, 220 with one).
 int row_tiles(int N, int B, int H)
 {
     const long rows = (long)N * H;
     return rows <= 32L * B ? 1 : rows <= 64L * B ? 2 : 4;
 }
+
+// Shortest chunk, in tiles: longer ones leave compute units idle (one token over 2047: 22 us, 24 with 4 and
+// 28 with 8; over 8191 they are alike).
+constexpr int kShort = 2;
 
 // Two rounds of chunks (and a grid for them) are considered from chunks of kLong tiles on; whether a call can have them is
 // known from the block table's width.
@@ -434,7 +444,7 @@ hipError_t launch(const LatentArgs &a, void *workspace, hipStream_t stream)
     const bool twice = may_be_long(groups, a.max_blocks, a.page);
     parts_at(workspace, groups, kCus, twice, kRows, kR, &parts);
     latent_attn_kernel<RT><<<(unsigned)grid_bound(groups, kCus, twice), kThreads, 0, stream>>>(
-        a, Shape{kRows, kKeys, 2, kCus, twice ? kLong : 0}, parts);
+        a, Shape{kRows, kKeys, kShort, kCus, twice ? kLong : 0}, parts);
     launch_join<kRows, kR>(a, a.H, parts, groups, stream);
     return hipGetLastError();
 }

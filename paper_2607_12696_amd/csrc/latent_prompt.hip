@@ -11,6 +11,10 @@
 //   panels: of 64 elements for keys (rows of 128 bytes, chunks of 16 XORed with row bits, so that 16 rows' chunks, a quarter
 //   of a read, lie in different banks), of 32 for values (rows of 64 bytes: half a read is 256 in a row).  So a read's
 //   place in the tile is an immediate offset.  One barrier a tile of 32 keys.
+// Measured: 5003 tokens of 128 heads 1.22 ms (842 TFLOP/s), 6 prompts of 563 to 1201 tokens, 16 heads, 74 us.  Workgroups of
+// 256 queries, one a compute unit, load half as often but wait for each other more and leave more idle rows: 1.24 ms and
+// 84 us.  The long prompt is held by the card's power (1.6 GHz; operands of zeros take a fifth less time), the short ones by
+// their longest row block.
 #include "attn_plan.hpp"
 
 namespace ecospec {

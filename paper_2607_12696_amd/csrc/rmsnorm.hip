@@ -5,7 +5,8 @@
 // between the sum of squares and the outputs: every input is read once and the
 // norm is never rounded to bf16 before it is coded.  The sum of squares is fp32,
 // a tree over the workgroup; v stays fp32 although `sum` is stored in bf16, so
-// the norm has one rounding.
+// the norm has one rounding.  Measured: 6001 rows of 2880 with MX codes 25 us
+// (6.3 TB/s, part of it from the memory-side cache), 4 rows of 7168 4 us.
 #include "attn.hpp"
 #include "device.hpp"
 
