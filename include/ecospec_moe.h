@@ -558,8 +558,10 @@ moe_status_t moe_cache_append(const moe_cache_t *cache, const void *k_new, const
  *   q, o [N][H][D], k_new, v_new [N][Hkv][D]: bf16; lse [N][H] fp32 or NULL.
  *   workspace: device scratch of moe_cache_attn_workspace_size bytes, 256-byte
  *   aligned; its contents on entry do not matter.
- * Arithmetic: codes are exact in bf16, scales multiply the fp32 scores and the
- * fp32 softmax weights; otherwise as for moe_latent_attn.  Deterministic.
+ * Arithmetic: codes are exact in bf16; the keys' scale multiplies the fp32
+ * scores, the values' scale the bf16 codes (its power of two, exact) and the
+ * fp32 softmax weights (the rest); otherwise as for moe_latent_attn.
+ * Deterministic.
  * Limits: H % Hkv == 0, H <= 1024, 1 <= B <= 1024, N >= 1, N * H <= 2^24,
  * scale finite.
  */

@@ -22,15 +22,27 @@ constexpr int kWaves = 4;
 // fp32, far from overflow, and the bf16 weights' rounding is relative.
 constexpr float kSlack = 8.f;
 
-// bf16 operand of eight codes.
-__device__ __forceinline__ bf16x8 decode(uint32_t w0, uint32_t w1)
+// bf16 operand of eight codes, times the power of two of `scale`: exact.
+__device__ __forceinline__ bf16x8 decode(uint32_t w0, uint32_t w1, float scale)
 {
     u32x4 o;
-    o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.0f, false));
-    o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.0f, true));
-    o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.0f, false));
-    o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.0f, true));
+    o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, false));
+    o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, true));
+    o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, false));
+    o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true));
     return __builtin_bit_cast(bf16x8, o);
+}
+
+// The score products, written out so that the first needs no sums of zeros; a register written by the vector unit needs
+// two wait states before a product reads it.
+__device__ __forceinline__ void mfma_first(f32x16 &s, const bf16x8 &k, const bf16x8 &q)
+{
+    asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(k), "v"(q));
+}
+
+__device__ __forceinline__ void mfma_next(f32x16 &s, const bf16x8 &k, const bf16x8 &q)
+{
+    asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(k), "v"(q));
 }
 
 // RT: row tiles of 32 rows; D: head width.
@@ -84,8 +96,9 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
     const int lp = 31 - __builtin_clz(a.page);
     const int cached = (it.len + kKeys - 1) / kKeys;  // tiles
 
-    // Running maximum, weights and sums of one row tile's scores x, in powers of two once multiplied by `unit` > 0.
-    auto softmax = [&](int rt, f32x16 &x, float unit) {
+    // Running maximum, weights and sums of one row tile's scores x, in powers of two once multiplied by `unit` > 0.  The
+    // weights come out times 2^up, and `down_up` = 2^-up keeps that out of their sum.
+    auto softmax = [&](int rt, f32x16 &x, float unit, float up, float down_up) {
         float tops[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) tops[h] = max3(max3(x[8 * h], x[8 * h + 1], x[8 * h + 2]), max3(x[8 * h + 3], x[8 * h + 4], x[8 * h + 5]), x[8 * h + 6]);
@@ -100,14 +113,14 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[rt][d][i] *= down;
         }
-        const float base = m[rt] == -INFINITY ? 0.f : m[rt];
+        const float base = (m[rt] == -INFINITY ? 0.f : m[rt]) - up;
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], unit, -base));
             sum[i % 2] += x[i];
         }
-        l[rt] += sum[0] + sum[1];
+        l[rt] = fmaf(sum[0] + sum[1], down_up, l[rt]);
     };
     // The sums of the score products are read by an instruction that the compiler does not see: 19 wait states after them.
     auto settle = [&](f32x16 (&s)[RT]) {
@@ -156,15 +169,14 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
         const int left = it.len - t * kKeys - 16 * half;  // of this half's 16 keys
         f32x16 s[RT];
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[rt][i] = 0.f;
-#pragma unroll
         for (int st = 0; st < kSteps; ++st) {
-            const bf16x8 k = decode(kr[st / 2][st % 2 * 2], kr[st / 2][st % 2 * 2 + 1]);
+            const bf16x8 k = decode(kr[st / 2][st % 2 * 2], kr[st / 2][st % 2 * 2 + 1], 1.f);
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-                s[rt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, __builtin_bit_cast(bf16x8, q_lds[(rt * kSteps + st) * 64 + lane]), s[rt], 0, 0, 0);
+            for (int rt = 0; rt < RT; ++rt) {
+                const bf16x8 q = __builtin_bit_cast(bf16x8, q_lds[(rt * kSteps + st) * 64 + lane]);
+                if (st == 0) mfma_first(s[rt], k, q);
+                else mfma_next(s[rt], k, q);
+            }
         }
         const bool tail = (t + 1) * kKeys > it.len;
         if (tail) {
@@ -193,18 +205,22 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (i >= left) s[rt][i] = -INFINITY;
+        // The values' scale, one for a lane's 16 keys: its power of two goes into their conversion, the rest into the
+        // exponent of the weights.
+        const float rest = __uint_as_float(0x3f800000u | (__float_as_uint(vs) & 0x7fffffu));
+        const float up = __builtin_amdgcn_logf(rest), down_up = __builtin_amdgcn_rcpf(rest);
         bf16x8 p[RT][2];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            softmax(rt, s[rt], fmaxf(ks, 0x1p-126f));
+            softmax(rt, s[rt], fmaxf(ks, 0x1p-126f), up, down_up);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) p[rt][i / 8][i % 8] = static_cast<__bf16>(s[rt][i] * vs);
+            for (int i = 0; i < 16; ++i) p[rt][i / 8][i % 8] = static_cast<__bf16>(s[rt][i]);
         }
 #pragma unroll
         for (int d = 0; d < kDt; ++d)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const bf16x8 v = decode(vr[d][2 * h], vr[d][2 * h + 1]);
+                const bf16x8 v = decode(vr[d][2 * h], vr[d][2 * h + 1], vs);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) o[rt][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[rt][h], o[rt][d], 0, 0, 0);
             }
@@ -216,17 +232,16 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
     for (; t < it.last; t += kWaves) {
         const int j0 = (t - cached) * kKeys;
         f32x16 s[RT];
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[rt][i] = 0.f;
         const uint16_t *kp = a.k_new + ((long)(it.t0 + min(j0 + pi, drafts - 1)) * a.Hkv + kvh) * D + 16 * half;
 #pragma unroll
         for (int st = 0; st < kSteps; ++st) {
             const bf16x8 k = *reinterpret_cast<const bf16x8 *>(kp + 32 * (st / 2) + 8 * (st % 2));
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-                s[rt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, __builtin_bit_cast(bf16x8, q_lds[(rt * kSteps + st) * 64 + lane]), s[rt], 0, 0, 0);
+            for (int rt = 0; rt < RT; ++rt) {
+                const bf16x8 q = __builtin_bit_cast(bf16x8, q_lds[(rt * kSteps + st) * 64 + lane]);
+                if (st == 0) mfma_first(s[rt], k, q);
+                else mfma_next(s[rt], k, q);
+            }
         }
         settle(s);
         // Weights as the products' operand, and in LDS (row, draft) for drafts that are not finite.
@@ -246,7 +261,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 if (!(bits >> i & 1)) s[rt][i] = -INFINITY;
-            softmax(rt, s[rt], scale2);
+            softmax(rt, s[rt], scale2, 0.f, 1.f);
 #pragma unroll
             for (int i = 0; i < 16; ++i) p[rt][i / 8][i % 8] = static_cast<__bf16>(s[rt][i]);
 #pragma unroll
