@@ -510,7 +510,8 @@ moe_status_t moe_latent_prompt(const moe_prompt_t *a, void *o, float *lse, void 
  * values of each page and head.  Paging as in moe_latent_cache_t.  A page
  * holds, per head, its keys token by token and its values element by element
  * (each element's tokens side by side: the operand order of the value
- * product).  The scales of pages in use are positive and finite.
+ * product).  The scales of pages in use are finite and at least
+ * 2^-126.
  * Requirements: D 64 or 128 (else MOE_ERR_UNSUPPORTED); page 16, 32, 64 or
  * 128; 1 <= Hkv <= 256; max_blocks * page <= 2^30; k and v 16-byte aligned. */
 typedef struct {

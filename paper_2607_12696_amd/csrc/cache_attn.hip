@@ -132,45 +132,56 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
     // Positive and not zero: the largest product is the largest score (a negative scale turned the queries' signs), and it
     // meets infinities.
     const float scale2 = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-126f);
-    u32x4 kr[D / 32], vr[kDt];
+    struct Codes {  // of a tile: this lane's operands and scales
+        u32x4 k[D / 32], v[kDt];
+        float ks, vs;
+    } ring[2];
     const long stride = (long)a.page * D;  // of a head's page
-    // Pages of a tile are read two tiles of the wavefront ahead, its codes and scales one: this half's 16 keys for the
-    // values and the scales, the 16 of key pi for the keys.  Through vector registers: a scalar load would make every wait
-    // for LDS wait for it too.
+    // A tile's codes and scales are read two tiles of the wavefront ahead (one ahead keeps 8 MB on their way, too little for
+    // HBM's latency), its pages three: this half's 16 keys for the values and the scales, the 16 of key pi for the keys.
+    // Through vector registers: a scalar load would make every wait for LDS wait for it too.
     auto page_id = [&](int t, int group) { return table[min((t * kKeys + 16 * group) >> lp, a.max_blocks - 1)]; };
     auto head = [&](int id) { return (long)min(max(id, 0), a.n_pages - 1) * a.Hkv + kvh; };
-    auto load_k = [&](int t, int id) {
+    auto load_k = [&](Codes &c, int t, int id) {
         const uint8_t *p = a.k + head(id) * stride + ((t * kKeys + pi) & (a.page - 1)) * D + 16 * half;
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) kr[i] = *reinterpret_cast<const u32x4 *>(p + 32 * i);
+        for (int i = 0; i < D / 32; ++i) c.k[i] = *reinterpret_cast<const u32x4 *>(p + 32 * i);
     };
-    auto load_v = [&](int t, int id) {
+    auto load_v = [&](Codes &c, int t, int id) {
         const uint8_t *p = a.v + head(id) * stride + ((t * kKeys + 16 * half) & (a.page - 1)) + (long)col * a.page;
 #pragma unroll
-        for (int d = 0; d < kDt; ++d) vr[d] = *reinterpret_cast<const u32x4 *>(p + (long)(32 * d) * a.page);
+        for (int d = 0; d < kDt; ++d) c.v[d] = *reinterpret_cast<const u32x4 *>(p + (long)(32 * d) * a.page);
     };
     const int end = min(it.last, cached);
     int t = it.first + wave, k_id = 0, v_id = 0;
-    float ks_next = 0.f, vs_next = 0.f;
+    auto load_scales = [&](Codes &c, int id) {
+        c.ks = a.k_scale[head(id)];
+        c.vs = a.v_scale[head(id)];
+    };
+    auto load_ids = [&](int t) {
+        k_id = page_id(min(t, end - 1), pi >> 4);
+        v_id = page_id(min(t, end - 1), half);
+    };
     if (t < end) {
-        k_id = page_id(t, pi >> 4);
-        v_id = page_id(t, half);
-        load_k(t, k_id);
-        load_v(t, v_id);
-        ks_next = a.k_scale[head(v_id)];
-        vs_next = a.v_scale[head(v_id)];
-        k_id = page_id(min(t + kWaves, end - 1), pi >> 4);
-        v_id = page_id(min(t + kWaves, end - 1), half);
+        load_ids(t);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int k_of = k_id, v_of = v_id, at = min(t + n * kWaves, end - 1);
+            load_ids(t + (n + 1) * kWaves);
+            load_k(ring[n], at, k_of);
+            load_v(ring[n], at, v_of);
+            load_scales(ring[n], v_of);
+        }
     }
-    for (; t < end; t += kWaves) {
-        const float ks = ks_next * scale2;
-        float vs = vs_next;
-        const int next = t + kWaves;
+    auto tile = [&](int t, Codes &c) {
+        const float ks = c.ks * scale2;
+        float vs = c.vs;
+        const int next = t + 2 * kWaves;
         const int left = it.len - t * kKeys - 16 * half;  // of this half's 16 keys
         f32x16 s[RT];
 #pragma unroll
         for (int st = 0; st < kSteps; ++st) {
-            const bf16x8 k = decode(kr[st / 2][st % 2 * 2], kr[st / 2][st % 2 * 2 + 1], 1.f);
+            const bf16x8 k = decode(c.k[st / 2][st % 2 * 2], c.k[st / 2][st % 2 * 2 + 1], 1.f);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 const bf16x8 q = __builtin_bit_cast(bf16x8, q_lds[(rt * kSteps + st) * 64 + lane]);
@@ -187,16 +198,14 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     const int n = left - 4 * w;
-                    vr[d][w] &= n >= 4 ? ~0u : n <= 0 ? 0u : (1u << 8 * n) - 1;
+                    c.v[d][w] &= n >= 4 ? ~0u : n <= 0 ? 0u : (1u << 8 * n) - 1;
                 }
         }
         const int id = v_id;
         if (next < end) {
-            load_k(next, k_id);
-            ks_next = a.k_scale[head(id)];
-            vs_next = a.v_scale[head(id)];
-            k_id = page_id(min(next + kWaves, end - 1), pi >> 4);
-            v_id = page_id(min(next + kWaves, end - 1), half);
+            load_k(c, next, k_id);
+            load_scales(c, id);
+            load_ids(next + kWaves);
         }
         settle(s);
         if (tail)
@@ -220,15 +229,21 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
         for (int d = 0; d < kDt; ++d)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const bf16x8 v = decode(vr[d][2 * h], vr[d][2 * h + 1], vs);
+                const bf16x8 v = decode(c.v[d][2 * h], c.v[d][2 * h + 1], vs);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) o[rt][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[rt][h], o[rt][d], 0, 0, 0);
             }
-        if (next < end) load_v(next, id);
+        if (next < end) load_v(c, next, id);
+    };
+    for (; t < end; t += 2 * kWaves) {
+        tile(t, ring[0]);
+        if (t + kWaves < end) tile(t + kWaves, ring[1]);
     }
 
     // ---- drafts
     const int drafts = min(it.n_tok, kMaxDrafts);
+    t = it.first + wave;
+    if (t < end) t += (end - t + kWaves - 1) / kWaves * kWaves;
     for (; t < it.last; t += kWaves) {
         const int j0 = (t - cached) * kKeys;
         f32x16 s[RT];
