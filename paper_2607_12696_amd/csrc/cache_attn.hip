@@ -9,8 +9,10 @@
 //
 // Bound by HBM (2 bytes a cached token, head and element) up to some 64 rows a key/value head.  Four wavefronts take the
 // tiles of a workgroup's chunk in turn, each with its own running maximum and sums, joined at the end through LDS.
-//   Measured: trees of up to 8 tokens of 16 sequences over 15000 to 60000 tokens, 64 heads of 64 on 8, 147 us (3.9 TB/s of
-// cache); four tokens over 16383, 64 heads of 128 on 4, 22 us, most of it the fixed cost of two launches and of 344 parts.  With 64 rows the vector unit is the limit (conversions, exponentials and packing: it is busy two thirds of the cycles).
+//   Measured: trees of up to 8 tokens of 16 sequences over 15000 to 60000 tokens, 64 heads of 64 on 8, 143 us (4.05 TB/s of
+// cache); four tokens over 16383, 64 heads of 128 on 4, 22 us, most of it the fixed cost of two launches and of 344 parts.
+// Wavefronts are alive for three quarters of the former (chunks of 69 to 81 rounds), and the vector unit (conversions,
+// exponentials and packing) is busy three quarters of that.
 #include "attn_plan.hpp"
 
 namespace ecospec {
@@ -137,8 +139,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
         float ks, vs;
     } ring[2];
     const long stride = (long)a.page * D;  // of a head's page
-    // A tile's codes and scales are read two tiles of the wavefront ahead (one ahead keeps 8 MB on their way, too little for
-    // HBM's latency), its pages three: this half's 16 keys for the values and the scales, the 16 of key pi for the keys.
+    // A tile's codes and scales are read two tiles of the wavefront ahead (one ahead: 2047 tokens 22 us instead of 20, long caches
+    // alike), its pages three: this half's 16 keys for the values and the scales, the 16 of key pi for the keys.
     // Through vector registers: a scalar load would make every wait for LDS wait for it too.
     auto page_id = [&](int t, int group) { return table[min((t * kKeys + 16 * group) >> lp, a.max_blocks - 1)]; };
     auto head = [&](int id) { return (long)min(max(id, 0), a.n_pages - 1) * a.Hkv + kvh; };
@@ -410,7 +412,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
 int row_tiles(int N, int B, int per_token, int D) { return D == 64 && (long)N * per_token > 32L * B ? 2 : 1; }
 
 // Workgroups at once: two on a compute unit hide each other's waits (trees of 16 sequences: 148 us, with one 203, with three
-// 161; one sequence of four tokens: 23, 22 and 29).
+// 161, all before the codes were read two tiles ahead; one sequence of four tokens: 23, 22 and 29).
 constexpr int kSlots = 2 * kCus;
 
 template <int D, int RT>
