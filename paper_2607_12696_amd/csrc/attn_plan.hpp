@@ -6,9 +6,9 @@
 // plan out for itself, from the two offsets and the length of each sequence: the chunk length is the smallest for which
 // all chunks run at once, or in two rounds where those are shorter.  (Row groups of different lengths leave chunks of
 // different lengths: 8 trees over 6000 to 20000 tokens have chunks of up to 188 tiles at once, of 143 on average, and of up
-// to 79 in two rounds: 375 us instead of 405.)  A row group of several chunks leaves its parts (fp32 output sums with the reference maximum
-// and the sum of the weights of each row) in the workspace, in the matrix cores' accumulator order, and join_kernel adds
-// them up in chunk order.
+// to 79 in two rounds: 375 us instead of 405.)  A row group of several chunks leaves its parts (fp32 output sums with the
+// reference maximum and the sum of the weights of each row) in the workspace, in the matrix cores' accumulator order, and
+// join_kernel adds them up in chunk order.
 #pragma once
 
 #include "attn.hpp"
@@ -286,19 +286,6 @@ __device__ __forceinline__ float halves_max(float v)
 __device__ __forceinline__ float halves_sum(float v)
 {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// The same over the two rows of 16 lanes of each half (lanes l and l ^ 16).
-__device__ __forceinline__ float quads_max(float v)
-{
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-
-__device__ __forceinline__ float quads_sum(float v)
-{
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 

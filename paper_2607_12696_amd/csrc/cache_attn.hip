@@ -103,7 +103,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
     auto softmax = [&](int rt, f32x16 &x, float unit, float up, float down_up) {
         float tops[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) tops[h] = max3(max3(x[8 * h], x[8 * h + 1], x[8 * h + 2]), max3(x[8 * h + 3], x[8 * h + 4], x[8 * h + 5]), x[8 * h + 6]);
+        for (int h = 0; h < 2; ++h)
+            tops[h] = max3(max3(x[8 * h], x[8 * h + 1], x[8 * h + 2]), max3(x[8 * h + 3], x[8 * h + 4], x[8 * h + 5]), x[8 * h + 6]);
         const float top = halves_max(max3(tops[0], tops[1], fmaxf(x[7], x[15])) * unit);
         if (__any(top > m[rt] + kSlack)) {
             const float now = fmaxf(m[rt], top);
@@ -139,8 +140,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
         float ks, vs;
     } ring[2];
     const long stride = (long)a.page * D;  // of a head's page
-    // A tile's codes and scales are read two tiles of the wavefront ahead (one ahead: 2047 tokens 22 us instead of 20, long caches
-    // alike), its pages three: this half's 16 keys for the values and the scales, the 16 of key pi for the keys.
+    // A tile's codes and scales are read two tiles of the wavefront ahead (one ahead: 2047 tokens 22 us instead of 20, long
+    // caches alike), its pages three: this half's 16 keys for the values and the scales, the 16 of key pi for the keys.
     // Through vector registers: a scalar load would make every wait for LDS wait for it too.
     auto page_id = [&](int t, int group) { return table[min((t * kKeys + 16 * group) >> lp, a.max_blocks - 1)]; };
     auto head = [&](int id) { return (long)min(max(id, 0), a.n_pages - 1) * a.Hkv + kvh; };
@@ -385,7 +386,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
                 for (int i = 0; i < 4; ++i)
                     out[(rt * kDt + d) * 256 + i * 64 + lane] =
                         f32x4{o[rt][d][4 * i], o[rt][d][4 * i + 1], o[rt][d][4 * i + 2], o[rt][d][4 * i + 3]};
-            if (half == 0) parts.ml[(long)it.slot * kRows + rt * 32 + col] = make_float2(total[rt] == 0.f ? -INFINITY : base[rt], total[rt]);
+            if (half == 0)
+                parts.ml[(long)it.slot * kRows + rt * 32 + col] = make_float2(total[rt] == 0.f ? -INFINITY : base[rt], total[rt]);
         }
         return;
     }
@@ -422,7 +424,8 @@ hipError_t launch(const CacheArgs &a, void *workspace, hipStream_t stream)
     const long groups = group_bound(a.N, a.B, G, a.Hkv, 32 * RT);
     Parts parts;
     parts_at(workspace, groups, kSlots, false, 32 * RT, D, &parts);
-    cache_attn_kernel<D, RT><<<(unsigned)grid_bound(groups, kSlots, false), 256, 0, stream>>>(a, Shape{32 * RT, kKeys, kWaves, kSlots, 0}, parts);
+    cache_attn_kernel<D, RT><<<(unsigned)grid_bound(groups, kSlots, false), 256, 0, stream>>>(
+        a, Shape{32 * RT, kKeys, kWaves, kSlots, 0}, parts);
     launch_join<32 * RT, D>(a, G, parts, groups, stream);
     return hipGetLastError();
 }

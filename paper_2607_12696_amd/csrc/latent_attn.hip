@@ -136,7 +136,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
         const int i = lane % 16, key = 4 * half + i / 4;
 #pragma unroll
         for (int d = 0; d < 2; ++d)
-            v_at[d] = (uint32_t)(key * kRowBytes + ((((4 * d + lane / 16 % 2 * 2 + i % 4 / 2) ^ twist(key)) + 16 * wave) * 16) + i % 2 * 8);
+            v_at[d] = (uint32_t)(key * kRowBytes + (((4 * d + lane / 16 % 2 * 2 + i % 4 / 2) ^ twist(key)) + 16 * wave) * 16 + i % 2 * 8);
     }
 
     // ---- queries of the wavefront's 32 rows, consecutive in memory, through LDS
@@ -433,7 +433,10 @@ constexpr int kShort = 2;
 // known from the block table's width.
 constexpr int kLong = 64;
 
-bool may_be_long(long groups, int max_blocks, int page) { return (double)groups * max_blocks * page >= (double)kLong * kKeys * kCus; }
+bool may_be_long(long groups, int max_blocks, int page)
+{
+    return (double)groups * max_blocks * page >= (double)kLong * kKeys * kCus;
+}
 
 template <int RT>
 hipError_t launch(const LatentArgs &a, void *workspace, hipStream_t stream)

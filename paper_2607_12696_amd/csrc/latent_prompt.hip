@@ -72,10 +72,12 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int b
 {
     __shared__ __attribute__((aligned(16))) Lds lds;
     // A head's row blocks on one XCD; the longest of all heads first, so that no long one is left for the end.
-    const int pairs = (a.B * a.H + 7) / 8, pair = blockIdx.x % 8 + 8 * (int)(blockIdx.x / 8 % pairs), block = blocks - 1 - (int)(blockIdx.x / 8 / pairs);
+    const int pairs = (a.B * a.H + 7) / 8, pair = blockIdx.x % 8 + 8 * (int)(blockIdx.x / 8 % pairs);
+    const int block = blocks - 1 - (int)(blockIdx.x / 8 / pairs);
     if (pair >= a.B * a.H) return;
     const int b = pair / a.H, h = pair % a.H;
-    const int q0 = __builtin_amdgcn_readfirstlane(min(max(a.q_offsets[b], 0), a.N)), nq = __builtin_amdgcn_readfirstlane(min(max(a.q_offsets[b + 1], q0), a.N)) - q0;
+    const int q0 = __builtin_amdgcn_readfirstlane(min(max(a.q_offsets[b], 0), a.N));
+    const int nq = __builtin_amdgcn_readfirstlane(min(max(a.q_offsets[b + 1], q0), a.N)) - q0;
     const int k0 = __builtin_amdgcn_readfirstlane(min(max(a.kv_offsets[b], 0), a.M));
     const int nk = __builtin_amdgcn_readfirstlane(min(max(a.kv_offsets[b + 1], k0), a.M)) - k0;
     const int row0 = block * kRows;
@@ -105,8 +107,10 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int b
         for (int rt = 0; rt < kRt; ++rt)
 #pragma unroll
             for (int st = 0; st < kSteps; ++st) {
-                u32x4 w = *reinterpret_cast<const u32x4 *>(lds.q[wave] + (32 * rt + col) * kDq * 2 + ((2 * st + half) ^ (col >> 1 & 7)) * 16);
-                if (a.scale < 0.f) w ^= 0x80008000u;  // the scale is positive from here on: the largest product is the largest score
+                const char *at = lds.q[wave] + (32 * rt + col) * kDq * 2 + ((2 * st + half) ^ (col >> 1 & 7)) * 16;
+                u32x4 w = *reinterpret_cast<const u32x4 *>(at);
+                // The scale is positive from here on: the largest product is the largest score.
+                if (a.scale < 0.f) w ^= 0x80008000u;
                 q[rt][st] = __builtin_bit_cast(bf16x8, w);
             }
     }
@@ -192,8 +196,8 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int b
     auto weights = [&](f32x16 (&s)[kRt], int c) {
         if (c < kRt) {
             f32x16 &x = s[c];
-            top[c] = max3(max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), x[6]), max3(max3(x[7], x[8], x[9]), max3(x[10], x[11], x[12]), x[13]),
-                          fmaxf(x[14], x[15]));
+            top[c] = max3(max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), x[6]),
+                          max3(max3(x[7], x[8], x[9]), max3(x[10], x[11], x[12]), x[13]), fmaxf(x[14], x[15]));
         } else if (c < 2 * kRt) {
             top[c - kRt] = halves_max(top[c - kRt]) * scale2;
         } else if (c < 3 * kRt) {
