@@ -466,7 +466,8 @@ typedef struct {
  * Arithmetic: bf16 products summed in fp32, softmax in fp32, the weights
  * exp(s - max) rounded to bf16 for the value product, fp32 sums, one rounding
  * to bf16 at the end.  Deterministic.
- * Limits: 1 <= H <= 1024, 1 <= B <= 1024, N >= 1, N * H <= 2^24, scale finite.
+ * Limits: 1 <= H <= 1024, 1 <= B <= 1024, 1 <= N <= 64 * B, N * H <= 2^24,
+ * scale finite.
  */
 moe_status_t moe_latent_attn_workspace_size(const moe_latent_cache_t *cache, int N, int B, int H, size_t *bytes);
 moe_status_t moe_latent_attn(const moe_latent_cache_t *cache, const moe_drafts_t *drafts, const void *q,
@@ -563,8 +564,8 @@ moe_status_t moe_cache_append(const moe_cache_t *cache, const void *k_new, const
  * scores, the values' scale the bf16 codes (its power of two, exact) and the
  * fp32 softmax weights (the rest); otherwise as for moe_latent_attn.
  * Deterministic.
- * Limits: H % Hkv == 0, H <= 1024, 1 <= B <= 1024, N >= 1, N * H <= 2^24,
- * scale finite.
+ * Limits: H % Hkv == 0, H <= 1024, 1 <= B <= 1024, 1 <= N <= 64 * B,
+ * N * H <= 2^24, scale finite.
  */
 moe_status_t moe_cache_attn_workspace_size(const moe_cache_t *cache, int N, int B, int H, size_t *bytes);
 moe_status_t moe_cache_attn(const moe_cache_t *cache, const moe_drafts_t *drafts, const void *q, const void *k_new,

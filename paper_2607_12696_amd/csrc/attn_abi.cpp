@@ -59,6 +59,7 @@ moe_status_t check_cache(const moe_cache_t *c)
 moe_status_t check_call(int N, int B, int H)
 {
     if (N < 1 || B < 1 || B > kMaxBatch || H < 1 || H > kMaxHeads || (long)N * H > kMaxRows) return MOE_ERR_INVALID_ARG;
+    if (N > (long)ecospec::kMaxDrafts * B) return MOE_ERR_INVALID_ARG;  // some sequence has more than a mask names
     return MOE_OK;
 }
 
