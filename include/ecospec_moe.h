@@ -462,7 +462,8 @@ typedef struct {
  *   q [N][H][r+p], kv_new [N][r+p] (the drafts' rows), o [N][H][r]: bf16;
  *   lse [N][H] fp32 or NULL.
  *   workspace: device scratch of moe_latent_attn_workspace_size bytes, 256-byte
- *   aligned; its contents on entry do not matter.
+ *   aligned; its contents on entry do not matter.  The size for N and B is
+ *   enough for every call of no more tokens and sequences (same cache, same H).
  * Arithmetic: bf16 products summed in fp32, softmax in fp32, the weights
  * exp(s - max) rounded to bf16 for the value product, fp32 sums, one rounding
  * to bf16 at the end.  Deterministic.
@@ -559,7 +560,8 @@ moe_status_t moe_cache_append(const moe_cache_t *cache, const void *k_new, const
  *   its page's scale) and the drafts that t attends to (k_new, v_new).
  *   q, o [N][H][D], k_new, v_new [N][Hkv][D]: bf16; lse [N][H] fp32 or NULL.
  *   workspace: device scratch of moe_cache_attn_workspace_size bytes, 256-byte
- *   aligned; its contents on entry do not matter.
+ *   aligned; its contents on entry do not matter.  The size for N and B is
+ *   enough for every call of no more tokens and sequences (same cache, same H).
  * Arithmetic: codes are exact in bf16; the keys' scale multiplies the fp32
  * scores, the values' scale the bf16 codes (its power of two, exact) and the
  * fp32 softmax weights (the rest); otherwise as for moe_latent_attn.

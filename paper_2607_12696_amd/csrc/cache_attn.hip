@@ -410,8 +410,9 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a, Shape s
 
 // Row tiles of a workgroup: two for heads of 64 elements where the average row group has more than 32 rows (37 drafts over
 // 130001 tokens: 142 us against 170 us with one); one for heads of 128, whose sums of two leave the loads no registers
-// (16 sequences of four drafts over 16383 tokens: 49 us, 58 us with two).
-int row_tiles(int N, int B, int per_token, int D) { return D == 64 && (long)N * per_token > 32L * B ? 2 : 1; }
+// (16 sequences of four drafts over 16383 tokens: 49 us, 58 us with two).  The average is over the sequences that can have
+// tokens at all.
+int row_tiles(int N, int B, int per_token, int D) { return D == 64 && (long)N * per_token > 32L * (N < B ? N : B) ? 2 : 1; }
 
 // Workgroups at once: two on a compute unit hide each other's waits (trees of 16 sequences: 148 us, with one 203, with three
 // 161, all before the codes were read two tiles ahead; one sequence of four tokens: 23, 22 and 29).
@@ -432,10 +433,17 @@ hipError_t launch(const CacheArgs &a, void *workspace, hipStream_t stream)
 
 }  // namespace
 
+// Enough for every call of at most N tokens and B sequences: of both counts of row tiles where such a call can have either,
+// from a token a sequence to one sequence with all tokens; each one's need grows with N and B.
 size_t cache_workspace(int N, int B, int H, int Hkv, int D)
 {
-    const int rt = row_tiles(N, B, H / Hkv, D);
-    return parts_at(nullptr, group_bound(N, B, H / Hkv, Hkv, 32 * rt), kSlots, false, 32 * rt, D, nullptr);
+    const int G = H / Hkv;
+    size_t most = 0;
+    for (int rt = row_tiles(1, 1, G, D); rt <= row_tiles(N < kMaxDrafts ? N : kMaxDrafts, 1, G, D); ++rt) {
+        const size_t need = parts_at(nullptr, group_bound(N, B, G, Hkv, 32 * rt), kSlots, false, 32 * rt, D, nullptr);
+        most = need > most ? need : most;
+    }
+    return most;
 }
 
 hipError_t launch_cache_attn(const CacheArgs &a, void *workspace, hipStream_t stream)

@@ -415,14 +415,14 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentArgs a, 
     }
 }
 
-// Row tiles of a workgroup: as few as hold the average sequence's rows.  Tiles without rows cost their products (32 tokens
-// of 16 heads over up to 9000: 56 us with one tile, 88 with four); more workgroups for the same rows read the keys again
-// (64 sequences of up to four such tokens: 106 us with two tiles, 137 with one, 140 with four; 48 tokens of 128 heads: 94
-// with four, 114 with two, 220 with one).
+// Row tiles of a workgroup: as few as hold the rows of an average sequence (of those that can have tokens at all).  Tiles
+// without rows cost their products (32 tokens of 16 heads over up to 9000: 56 us with one tile, 88 with four); more
+// workgroups for the same rows read the keys again (64 sequences of up to four such tokens: 106 us with two tiles, 137 with
+// one, 140 with four; 48 tokens of 128 heads: 94 with four, 114 with two, 220 with one).
 int row_tiles(int N, int B, int H)
 {
-    const long rows = (long)N * H;
-    return rows <= 32L * B ? 1 : rows <= 64L * B ? 2 : 4;
+    const long rows = (long)N * H, sequences = N < B ? N : B;
+    return rows <= 32 * sequences ? 1 : rows <= 64 * sequences ? 2 : 4;
 }
 
 // Shortest chunk, in tiles: longer ones leave compute units idle (one token over 2047: 22 us, 24 with 4 and
@@ -454,11 +454,17 @@ hipError_t launch(const LatentArgs &a, void *workspace, hipStream_t stream)
 
 }  // namespace
 
+// Enough for every call of at most N tokens and B sequences: of all the row tiles that such a call can have, from those of
+// a token a sequence to those of one sequence with all tokens; each one's need grows with N and B.
 size_t latent_workspace(int N, int B, int H, int max_blocks, int page)
 {
-    const int rows = 32 * row_tiles(N, B, H);
-    const long groups = group_bound(N, B, H, 1, rows);
-    return parts_at(nullptr, groups, kCus, may_be_long(groups, max_blocks, page), rows, kR, nullptr);
+    size_t most = 0;
+    for (int rt = row_tiles(1, 1, H); rt <= row_tiles(N < kMaxDrafts ? N : kMaxDrafts, 1, H); rt *= 2) {
+        const long groups = group_bound(N, B, H, 1, 32 * rt);
+        const size_t need = parts_at(nullptr, groups, kCus, may_be_long(groups, max_blocks, page), 32 * rt, kR, nullptr);
+        most = need > most ? need : most;
+    }
+    return most;
 }
 
 hipError_t launch_latent_attn(const LatentArgs &a, void *workspace, hipStream_t stream)

@@ -33,3 +33,24 @@ def test_more_tokens_than_masks_have_bits(kind, N, B):
     assert size(kind, N, B)[0] == BAD
     assert attend(kind, N, B) == BAD
     assert size(kind, 64 * B, B)[0] == OK
+
+
+@pytest.mark.parametrize("H", [1, 5, 16, 33, 64, 128])
+@pytest.mark.parametrize("kind,shape", [("latent", 4), ("latent", 4000), ("grouped", 64), ("grouped", 128)])
+def test_workspace_of_the_largest_call_is_enough_for_smaller_ones(kind, shape, H):
+    """The size asked for the most tokens and sequences bounds that of every call with no more of either."""
+    if kind == "latent":
+        c = moe.moe_latent_cache_t(512, 64, 8, 64, shape, FAKE, FAKE, FAKE)
+    else:
+        c = moe.moe_cache_t(1, shape, 8, 64, 4, FAKE, FAKE + 1024, FAKE, FAKE, FAKE, FAKE)
+    steps = [1, 2, 3, 4, 7, 8, 16, 31, 32, 33, 64, 100, 150, 300, 600, 1000]
+    sizes = {}
+    for N in steps:
+        for B in steps:
+            if N > 64 * B:
+                continue
+            status, sizes[N, B] = size(kind, N, B, H, c)
+            assert status == OK
+    for (N, B), n in sizes.items():
+        for (N2, B2), m in sizes.items():
+            assert N2 > N or B2 > B or m <= n, ((N2, B2, m), (N, B, n))
