@@ -412,6 +412,7 @@ typedef enum {
  *   q = the 8-bit form of u: fp32 scale = max(max |u|, 2^-100) / 448 over the
  *   group, code = e4m3fn(u / scale), magnitudes from 448 up saturating; or MX.
  * v and u are not rounded on the way: y and q come from the unrounded sum.
+ * The mean is right for rows of any size, also where v^2 is past fp32's range.
  *   x, residual, sum, y [T][d] bf16, weight [d] bf16; q, scales by qfmt.
  *   sum, y or q may be NULL (q and scales exactly when qfmt is MOE_Q_NONE),
  *   not all three.  sum may be the buffer of x or of residual, and y that of

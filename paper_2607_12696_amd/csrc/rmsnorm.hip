@@ -50,8 +50,13 @@ __device__ __forceinline__ float saturate(float v)
 }
 
 // Squares are summed of v / 128, so that the sum over the widest row (16384 elements) overflows no sooner than their
-// mean does.
+// mean does.  Where the mean does, or is so small that squares may have lost bits below fp32's smallest normal number, the
+// row is summed again times a power of two that brings it back.  (Rows like that need an epsilon of nearly nothing, or
+// elements past 2^64: others go on with the sum they have.)
 constexpr float kDown = 0x1p-7f;
+constexpr float kLeast = 0x1p-80f;  // an element of the root mean square adds 2^-14 of this, 32 bits above the smallest normal
+constexpr float kUp = 0x1p100f;     // a row below kLeast has elements below 2^-33: 2^67, their squares / 128^2 sum to 2^120
+constexpr float kBack = 0x1p-70f;   // elements below 2^128: 2^58
 
 template <int STEP>
 __device__ __forceinline__ float lanes_max(float m)
@@ -96,7 +101,28 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(NormArgs a)
     ss = 0.f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) ss += part[0][w];
-    const float rinv = 1.f / sqrtf(ss / ((float)a.d * kDown * kDown) + a.eps);
+    float mean = ss / ((float)a.d * kDown * kDown) + a.eps, by = 1.f;
+    if (!(mean >= kLeast && mean < INFINITY)) {
+        by = mean < kLeast ? kUp : kBack;
+        ss = 0.f;
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+            if (i * THREADS + threadIdx.x < vecs)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float t = v[i][j] * (by * kDown);
+                    ss = fmaf(t, t, ss);
+                }
+        ss = wave_sum(ss);
+        if (lane_id() == 0) part[1][threadIdx.x / kWave] = ss;
+        __syncthreads();
+        ss = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) ss += part[1][w];
+        mean = ss / ((float)a.d * kDown * kDown) + a.eps * by * by;
+        __syncthreads();
+    }
+    const float rinv = 1.f / sqrtf(mean);
     float top = 0.f;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
@@ -107,6 +133,7 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(NormArgs a)
             unpack8(reinterpret_cast<const u32x4 *>(a.weight)[at], w);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
+                v[i][j] *= by;
                 v[i][j] *= rinv * w[j];
                 top = fmaxf(top, fabsf(v[i][j]));
             }
