@@ -49,6 +49,14 @@ __device__ __forceinline__ float saturate(float v)
     return v;
 }
 
+// The quotient f / scale by its rounded reciprocal and one correction, which brings it to the nearest fp32 number: a product
+// with the reciprocal alone can leave a tie between two codes.  An infinite scale (inv 0) is passed as 0: quotients 0 and NaN.
+__device__ __forceinline__ float quotient(float f, float scale, float inv)
+{
+    const float q = f * inv;
+    return saturate(fmaf(fmaf(-q, scale, f), inv, q));
+}
+
 // Squares are summed of v / 128, so that the sum over the widest row (16384 elements) overflows no sooner than their
 // mean does.  Where the mean does, or is so small that squares may have lost bits below fp32's smallest normal number, the
 // row is summed again times a power of two that brings it back.  (Rows like that need an epsilon of nearly nothing, or
@@ -157,17 +165,19 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(NormArgs a)
         if (in)
 #pragma unroll
             for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(v[i][j]));
-        float inv;
+        float inv, scale = 0.f;
         if (a.qfmt == Q_MX) {
             m = lanes_max<4>(m);  // 32 elements
             int e = (int)(__float_as_uint(m) >> 23) - 127 - 8;
             if (e < -127) e = -127;
             inv = ldexpf(1.f, -e);
+            scale = ldexpf(1.f, e);
             if (in && (at & 3) == 0) static_cast<uint8_t *>(a.scales)[row * (a.d / 32) + at / 4] = (uint8_t)(e + 127);
         } else {
             m = a.qfmt == Q_ROW ? top : lanes_max<16>(m);  // 128 elements
             const float s = fmaxf(m, 0x1p-100f) / 448.f;
             inv = 1.f / s;
+            if (s < INFINITY) scale = s;
             if (a.qfmt == Q_GROUP && in && (at & 15) == 0)
                 static_cast<float *>(a.scales)[row * ((a.d + 127) / 128) + at / 16] = s;
         }
@@ -176,8 +186,8 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(NormArgs a)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const float *f = v[i] + 4 * h;
-            int w = __builtin_amdgcn_cvt_pk_fp8_f32(saturate(f[0] * inv), saturate(f[1] * inv), 0, false);
-            c[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(saturate(f[2] * inv), saturate(f[3] * inv), w, true);
+            int w = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(f[0], scale, inv), quotient(f[1], scale, inv), 0, false);
+            c[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(quotient(f[2], scale, inv), quotient(f[3], scale, inv), w, true);
         }
         reinterpret_cast<u32x2 *>(a.q + row * a.d)[at] = c;
     }
