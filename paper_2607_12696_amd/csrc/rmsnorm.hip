@@ -51,10 +51,11 @@ __device__ __forceinline__ float saturate(float v)
 
 // The quotient f / scale by its rounded reciprocal and one correction, which brings it to the nearest fp32 number: a product
 // with the reciprocal alone can leave a tie between two codes.  An infinite scale (inv 0) is passed as 0: quotients 0 and NaN.
+// Zeros keep their sign.
 __device__ __forceinline__ float quotient(float f, float scale, float inv)
 {
     const float q = f * inv;
-    return saturate(fmaf(fmaf(-q, scale, f), inv, q));
+    return fmaf(fmaf(q, scale, -f), -inv, q);
 }
 
 // Squares are summed of v / 128, so that the sum over the widest row (16384 elements) overflows no sooner than their
@@ -170,8 +171,7 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(NormArgs a)
             m = lanes_max<4>(m);  // 32 elements
             int e = (int)(__float_as_uint(m) >> 23) - 127 - 8;
             if (e < -127) e = -127;
-            inv = ldexpf(1.f, -e);
-            scale = ldexpf(1.f, e);
+            inv = ldexpf(1.f, -e);  // the product is the quotient
             if (in && (at & 3) == 0) static_cast<uint8_t *>(a.scales)[row * (a.d / 32) + at / 4] = (uint8_t)(e + 127);
         } else {
             m = a.qfmt == Q_ROW ? top : lanes_max<16>(m);  // 128 elements
@@ -182,12 +182,19 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(NormArgs a)
                 static_cast<float *>(a.scales)[row * ((a.d + 127) / 128) + at / 16] = s;
         }
         if (!in) continue;
+        float f[8];
+        if (a.qfmt == Q_MX) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = saturate(v[i][j] * inv);
+        } else {  // at most 448 but for a rounding, and what is below 464 becomes 448
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = quotient(v[i][j], scale, inv);
+        }
         u32x2 c;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const float *f = v[i] + 4 * h;
-            int w = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(f[0], scale, inv), quotient(f[1], scale, inv), 0, false);
-            c[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(quotient(f[2], scale, inv), quotient(f[3], scale, inv), w, true);
+            const int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * h], f[4 * h + 1], 0, false);
+            c[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[4 * h + 2], f[4 * h + 3], w, true);
         }
         reinterpret_cast<u32x2 *>(a.q + row * a.d)[at] = c;
     }

@@ -42,3 +42,22 @@ def test_codes_are_those_of_the_quotient(top, fmt):
     got = q.numpy()
     bad = np.argwhere(got != want)
     assert not len(bad), (top, [(float(u[i, j]), hex(got[i, j]), hex(want[i, j])) for i, j in bad[:5]])
+
+
+@pytest.mark.parametrize("fmt", [moe.MOE_Q_FP8_GROUP, moe.MOE_Q_FP8_ROW, moe.MOE_Q_MXFP8])
+def test_zeros_and_infinities(fmt):
+    """Zeros keep their sign.  An infinite norm (a weight too large for it) saturates in MX, whose scale stays finite; the
+    other formats' scale is infinite then, and the quotients are zeros and a NaN."""
+    x = torch.ones(2, 256).to(torch.bfloat16)
+    x[:, 3], x[:, 4], x[1, 7] = 0.0, -0.0, -255.0  # row 1: 7 has 15.6 times the root mean square
+    w = torch.ones(256, dtype=torch.bfloat16)
+    w[7] = 3.2e38
+    _, y, q, s = (t.cpu() for t in moe.moe_add_rmsnorm(x.to(DEV), w.to(DEV), 0.0, qfmt=fmt))
+    assert y[1, 7] == -float("inf") and torch.isfinite(y[0]).all()
+    assert (q[:, 3] == 0).all() and (q[:, 4] == 0x80).all()
+    if fmt == moe.MOE_Q_MXFP8:
+        assert s[1, 0] == 247 and q[1, 7] == 0xFE  # 2^120, -448
+        assert (q[1, 32:] != 0).all()
+    else:
+        assert s[1, 0] == float("inf") and q[1, 7] & 0x7F == 0x7F
+        assert (q[1, 8:128] & 0x7F == 0).all()
