@@ -330,7 +330,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int b
             for (int st = 0; st < 2; ++st) p[rt][st] = __builtin_bit_cast(bf16x8, packed[rt][st]);
         advance();
         turn_rings();
-        if (odd_tiles >> (t - edge) & (t >= edge ? 1 : 0)) {
+        if (odd_tiles >> max(t - edge, 0) & 1) {  // no bit is set before tile `edge`
             uint32_t some = 0;
 #pragma unroll
             for (int i = 0; i < 16 * kRt; ++i) some |= (s[i / 16][i % 16] != 0.f ? 1u : 0u) << i;
