@@ -22,11 +22,11 @@ namespace {
 
 constexpr int kDn = 128, kP = 64, kDv = 128, kDq = kDn + kP;
 constexpr int kKeys = 32;
-constexpr int kRt = 1, kWaves = 4, kRows = 32 * kRt * kWaves, kThreads = 64 * kWaves;  // kRt: row tiles of a wavefront
+constexpr int kWaves = 4, kRows = 32 * kWaves, kThreads = 64 * kWaves;
 constexpr int kSteps = kDq / 16;
 constexpr int kRing = 4, kAhead = 3;  // key and value operands in registers
 constexpr int kLoads = 5;             // loads of a tile by a wavefront
-constexpr int kScore = kRt * kSteps, kProducts = kScore + kRt * 8;  // of a tile
+constexpr int kProducts = kSteps + 8;  // of a tile: scores, values
 constexpr int kLoadFrom = kProducts - 2 * kLoads;  // a load behind every other product from here on
 constexpr int kEdge = kRows / kKeys + 1;  // most tiles that some rows of a workgroup see in part
 constexpr float kSlack = 8.f;
@@ -50,10 +50,9 @@ struct Tiles {
 };
 
 union Lds {
-    char q[kWaves][32 * kRt * kDq * 2];  // the queries of each wavefront, before the loop: at c ^ (r >> 1 & 7)
+    char q[kWaves][32 * kDq * 2];  // the queries of each wavefront, before the loop: at c ^ (r >> 1 & 7)
     Tiles t;
 };
-static_assert(kRt == 1, "16 weights of a lane");
 static_assert(2 * sizeof(Lds) <= 160 * 1024, "two workgroups a compute unit");
 
 // The score products, sums in vector registers, which the vector unit works on; a register written by the vector
@@ -87,32 +86,29 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int b
     auto limit = [&](int row) { return min(max(row + 1 + nk - nq, 0), nk); };  // keys that a query sees
     const int tiles = (limit(min(row0 + kRows, nq) - 1) + kKeys - 1) / kKeys;
     const int edge = limit(row0) / kKeys;  // first tile that some row of the workgroup does not see to its end
-    const int first = row0 + 32 * kRt * wave;
+    const int first = row0 + 32 * wave;
     const int all_see = limit(first);      // keys that all rows of the wavefront see
 
     // ---- queries through LDS
-    bf16x8 q[kRt][kSteps];
+    bf16x8 q[kSteps];
     {
-        const int rows = max(min(nq - first, 32 * kRt), 0), stride = a.H * kDq * 2;
+        const int rows = max(min(nq - first, 32), 0), stride = a.H * kDq * 2;
         const u32x4 from = rsrc_words(a.q + ((long)(q0 + min(first, nq - 1)) * a.H + h) * kDq,
                                       rows ? (uint32_t)((rows - 1) * stride + kDq * 2) : 0);
         const uint32_t to = __builtin_amdgcn_readfirstlane(lds_addr(lds.q[wave]));
 #pragma unroll
-        for (int n = 0; n < 12 * kRt; ++n) {
+        for (int n = 0; n < 12; ++n) {
             const int i = n * 64 + lane, r = i / 24, c = i % 24;
             load16_lds(from, (uint32_t)(r * stride + (c ^ (r >> 1 & 7)) * 16), to + n * 1024);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-        for (int rt = 0; rt < kRt; ++rt)
-#pragma unroll
-            for (int st = 0; st < kSteps; ++st) {
-                const char *at = lds.q[wave] + (32 * rt + col) * kDq * 2 + ((2 * st + half) ^ (col >> 1 & 7)) * 16;
-                u32x4 w = *reinterpret_cast<const u32x4 *>(at);
-                // The scale is positive from here on: the largest product is the largest score.
-                if (a.scale < 0.f) w ^= 0x80008000u;
-                q[rt][st] = __builtin_bit_cast(bf16x8, w);
-            }
+        for (int st = 0; st < kSteps; ++st) {
+            u32x4 w = *reinterpret_cast<const u32x4 *>(lds.q[wave] + col * kDq * 2 + ((2 * st + half) ^ (col >> 1 & 7)) * 16);
+            // The scale is positive from here on: the largest product is the largest score.
+            if (a.scale < 0.f) w ^= 0x80008000u;
+            q[st] = __builtin_bit_cast(bf16x8, w);
+        }
     }
     __syncthreads();
 
@@ -163,23 +159,14 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int b
     // The values of tile -1, whose weights are zeros.
     for (int i = threadIdx.x; i < kKeys * kDv * 2 / 16; i += kThreads) reinterpret_cast<u32x4 *>(lds.t.v[4])[i] = u32x4{0, 0, 0, 0};
 
-    f32x16 o[kRt][kDv / 32];
+    f32x16 o[kDv / 32];
 #pragma unroll
-    for (int rt = 0; rt < kRt; ++rt)
+    for (int d = 0; d < kDv / 32; ++d)
 #pragma unroll
-        for (int d = 0; d < kDv / 32; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[rt][d][i] = 0.f;
-    float m[kRt], l[kRt], down[kRt];
-    int scaled[kRt];
-#pragma unroll
-    for (int rt = 0; rt < kRt; ++rt) {
-        m[rt] = -INFINITY;
-        l[rt] = 0.f;
-        down[rt] = 1.f;
-        scaled[rt] = 0;
-    }
-    bf16x8 p[kRt][2] = {};  // weights of the tile before: row tile, 16 keys
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+    float m = -INFINITY, l = 0.f, down = 1.f;
+    int scaled = 0;
+    bf16x8 p[2] = {};  // weights of the tile before: 16 keys each
     uint32_t odd_tiles = 0;  // edge tiles with infinities or NaN among the values
     const float scale2 = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-126f);  // not zero: it meets infinities
 
@@ -189,45 +176,42 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int b
     const int i16 = lane % 16;
     const uint32_t v_at = (uint32_t)((4 * half + i16 / 4) * 64 + lane / 16 % 2 * 32 + i16 % 4 * 8);
 
-    // Behind product c, a piece of the weights of the scores s of a tile.  Register i of a row tile is key
-    // 8 (i / 4) + 4 half + i % 4.
-    float top[kRt], base[kRt], sum[kRt];
-    u32x4 packed[kRt][2];
-    auto weights = [&](f32x16 (&s)[kRt], int c) {
-        if (c < kRt) {
-            f32x16 &x = s[c];
-            top[c] = max3(max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), x[6]),
-                          max3(max3(x[7], x[8], x[9]), max3(x[10], x[11], x[12]), x[13]), fmaxf(x[14], x[15]));
-        } else if (c < 2 * kRt) {
-            top[c - kRt] = halves_max(top[c - kRt]) * scale2;
-        } else if (c < 3 * kRt) {
-            const int rt = c - 2 * kRt;
-            int move = __any(top[rt] > m[rt] + kSlack);
-            scaled[rt] = move & __any(m[rt] != -INFINITY);
+    // Behind product c, a piece of the weights of the scores s of a tile.  Register i is key 8 (i / 4) + 4 half + i % 4.
+    float top, base, sum;
+    u32x4 packed[2];
+    auto weights = [&](f32x16 &s, int c) {
+        if (c == 0) {
+            top = max3(max3(max3(s[0], s[1], s[2]), max3(s[3], s[4], s[5]), s[6]),
+                       max3(max3(s[7], s[8], s[9]), max3(s[10], s[11], s[12]), s[13]), fmaxf(s[14], s[15]));
+        } else if (c == 1) {
+            top = halves_max(top) * scale2;
+        } else if (c == 2) {
+            int move = __any(top > m + kSlack);
+            scaled = move & __any(m != -INFINITY);
             asm("" : "+v"(move));  // a select, not a branch
-            const float now = move ? fmaxf(m[rt], top[rt]) : m[rt];
-            base[rt] = now == -INFINITY ? 0.f : now;
-            down[rt] = __builtin_amdgcn_exp2f((m[rt] == -INFINITY ? base[rt] : m[rt]) - base[rt]);
-            m[rt] = now;
-            sum[rt] = 0.f;
+            const float now = move ? fmaxf(m, top) : m;
+            base = now == -INFINITY ? 0.f : now;
+            down = __builtin_amdgcn_exp2f((m == -INFINITY ? base : m) - base);
+            m = now;
+            sum = 0.f;
         } else {
-            const int e = c - 3 * kRt;  // of 16 kRt elements
-            if (e < 16 * kRt) s[e / 16][e % 16] = __builtin_amdgcn_exp2f(fmaf(s[e / 16][e % 16], scale2, -base[e / 16]));
+            const int e = c - 3;  // of 16 elements
+            if (e < 16) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], scale2, -base));
             // The element before: its sum, and pairs to bf16.  Written out to stay here, where the compiler would sink them
             // behind all products; a piece later, because the result of an exp2 needs a wait state.
-            if (e > 0 && e <= 16 * kRt) {
-                const int rt = (e - 1) / 16, i = (e - 1) % 16;
-                asm volatile("v_add_f32 %0, %0, %1" : "+v"(sum[rt]) : "v"(s[rt][i]));
+            if (e > 0 && e <= 16) {
+                const int i = e - 1;
+                asm volatile("v_add_f32 %0, %0, %1" : "+v"(sum) : "v"(s[i]));
                 if (i % 2) {
                     uint32_t w;
-                    asm volatile("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(w) : "v"(s[rt][i - 1]), "v"(s[rt][i]));
-                    packed[rt][i / 8][i % 8 / 2] = w;
+                    asm volatile("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(w) : "v"(s[i - 1]), "v"(s[i]));
+                    packed[i / 8][i % 8 / 2] = w;
                 }
-                if (i == 15) l[rt] = fmaf(l[rt], down[rt], sum[rt]);
+                if (i == 15) l = fmaf(l, down, sum);
             }
         }
     };
-    static_assert(kProducts >= 19 * kRt + 1, "all pieces");
+    static_assert(kProducts >= 20, "all pieces");
     // Operands of the tiles at these ring offsets.
     uint32_t key_at[4], value_at = v_at + 4 * kValueTile;
     auto k_frag = [&](int st) { return *reinterpret_cast<const bf16x8 *>(lds.t.k[0] + key_at[st % 4] + st / 4 * kPanel); };
@@ -242,28 +226,22 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int b
         for (int st = 0; st < kRing - 1; ++st) k[st] = k_frag(st);
     };
     // Products of a tile's keys (the first ones fetched) into s, then of a tile's values, `between(c)` behind product c.
-    auto products = [&](f32x16 (&s)[kRt], auto between) {
+    auto products = [&](f32x16 &s, auto between) {
 #pragma unroll
         for (int st = 0; st < kSteps; ++st) {
             if (st + kRing - 1 < kSteps) k[(st + kRing - 1) % kRing] = k_frag(st + kRing - 1);
             else v[st + kRing - 1 - kSteps] = v_frag(st + kRing - 1 - kSteps);
-#pragma unroll
-            for (int rt = 0; rt < kRt; ++rt) {
-                __builtin_amdgcn_sched_barrier(0);
-                if (st == 0) mfma_first(s[rt], k[0], q[rt][0]);
-                else mfma_next(s[rt], k[st % kRing], q[rt][st]);
-                between(kRt * st + rt);
-            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (st == 0) mfma_first(s, k[0], q[0]);
+            else mfma_next(s, k[st % kRing], q[st]);
+            between(st);
         }
         static_assert(kRing - 1 == kAhead, "the last steps fetch the first value operands");
 #pragma unroll
         for (int n = 0; n < 8; ++n) {
-#pragma unroll
-            for (int rt = 0; rt < kRt; ++rt) {
-                __builtin_amdgcn_sched_barrier(0);
-                o[rt][n % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[n % kAhead], p[rt][n / 4], o[rt][n % 4], 0, 0, 0);
-                between(kScore + kRt * n + rt);
-            }
+            __builtin_amdgcn_sched_barrier(0);
+            o[n % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[n % kAhead], p[n / 4], o[n % 4], 0, 0, 0);
+            between(kSteps + n);
             if (n + kAhead < 8) v[n % kAhead] = v_frag(n + kAhead);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -279,7 +257,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int b
     };
 
     // One tile: s its scores, next the scores of the tile after.
-    auto tile = [&](int t, f32x16 (&s)[kRt], f32x16 (&next)[kRt]) {
+    auto tile = [&](int t, f32x16 &s, f32x16 &next) {
         // Tile t + 1 has landed; every wavefront is past the scores of tile t and the values of tile t - 2.
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads) : "memory");
         first_keys();
@@ -304,36 +282,29 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int b
             if (__syncthreads_or(odd)) odd_tiles |= 1u << (t - edge);
         }
         // The sums so far, for the reference maximum that the weights of tile t - 1 have.
+        if (scaled) {
 #pragma unroll
-        for (int rt = 0; rt < kRt; ++rt)
-            if (scaled[rt]) {
-#pragma unroll
-                for (int d = 0; d < kDv / 32; ++d) acc_scale(o[rt][d], down[rt]);
-                scaled[rt] = 0;
-            }
+            for (int d = 0; d < kDv / 32; ++d) acc_scale(o[d], down);
+            scaled = 0;
+        }
         if ((t + 1) * kKeys > all_see) {
+            const int left = limit(first + col) - t * kKeys - 4 * half;
 #pragma unroll
-            for (int rt = 0; rt < kRt; ++rt) {
-                const int left = limit(first + 32 * rt + col) - t * kKeys - 4 * half;
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (i / 4 * 8 + i % 4 >= left) s[rt][i] = -INFINITY;
-            }
+            for (int i = 0; i < 16; ++i)
+                if (i / 4 * 8 + i % 4 >= left) s[i] = -INFINITY;
         }
         products(next, [&](int c) {
             weights(s, c);
             if (c >= kLoadFrom && (c - kLoadFrom) % 2 == 0) load((c - kLoadFrom) / 2);
         });
 #pragma unroll
-        for (int rt = 0; rt < kRt; ++rt)
-#pragma unroll
-            for (int st = 0; st < 2; ++st) p[rt][st] = __builtin_bit_cast(bf16x8, packed[rt][st]);
+        for (int st = 0; st < 2; ++st) p[st] = __builtin_bit_cast(bf16x8, packed[st]);
         advance();
         turn_rings();
         if (odd_tiles >> max(t - edge, 0) & 1) {  // no bit is set before tile `edge`
             uint32_t some = 0;
 #pragma unroll
-            for (int i = 0; i < 16 * kRt; ++i) some |= (s[i / 16][i % 16] != 0.f ? 1u : 0u) << i;
+            for (int i = 0; i < 16; ++i) some |= (s[i] != 0.f ? 1u : 0u) << i;
             lds.t.some[t - edge][threadIdx.x] = (uint16_t)some;
         }
     };
@@ -343,19 +314,16 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int b
 #pragma unroll
     for (int n = 0; n < kLoads; ++n) load(n);
     advance();
-    f32x16 s0[kRt], s1[kRt];
+    f32x16 s0, s1;
     {
 #pragma unroll
         for (int i = 0; i < 4; ++i) key_at[i] = k_at[i];
 #pragma unroll
-        for (int st = 0; st < kSteps; ++st)
-#pragma unroll
-            for (int rt = 0; rt < kRt; ++rt) {
-                if (st == 0) mfma_first(s0[rt], k_frag(0), q[rt][0]);
-                else mfma_next(s0[rt], k_frag(st), q[rt][st]);
-            }
-#pragma unroll
-        for (int rt = 0; rt < kRt; ++rt) asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s0[rt]));
+        for (int st = 0; st < kSteps; ++st) {
+            if (st == 0) mfma_first(s0, k_frag(0), q[0]);
+            else mfma_next(s0, k_frag(st), q[st]);
+        }
+        asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s0));
     }
     key_to = kKeyTile;
 #pragma unroll
@@ -368,26 +336,23 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int b
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing is on its way to LDS when the workgroup ends
 
-#pragma unroll
-    for (int rt = 0; rt < kRt; ++rt) {
-        const int row = first + 32 * rt + col;
-        l[rt] = halves_sum(l[rt]);
-        if (row >= nq) continue;
-        const float inv = l[rt] == 0.f ? 0.f : 1.f / l[rt];
+    const int row = first + col;
+    l = halves_sum(l);
+    if (row < nq) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
         const long at = (long)(q0 + row) * a.H + h;
 #pragma unroll
         for (int d = 0; d < kDv / 32; ++d)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 *reinterpret_cast<u32x2 *>(a.o + at * kDv + 32 * d + 8 * i + 4 * half) =
-                    u32x2{pack_bf16x2(o[rt][d][4 * i] * inv, o[rt][d][4 * i + 1] * inv),
-                          pack_bf16x2(o[rt][d][4 * i + 2] * inv, o[rt][d][4 * i + 3] * inv)};
-        if (a.lse && half == 0) a.lse[at] = l[rt] == 0.f ? -INFINITY : (m[rt] + __builtin_amdgcn_logf(l[rt])) / kLog2e;
+                    u32x2{pack_bf16x2(o[d][4 * i] * inv, o[d][4 * i + 1] * inv),
+                          pack_bf16x2(o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv)};
+        if (a.lse && half == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) / kLog2e;
     }
-    if (!odd_tiles) return;
-    for (int n = 0; n < 64 * kRt; ++n) {  // the lane's own elements, as above
-        const int rt = n / 64, row = first + 32 * rt + col, el = n % 64 / 16 * 32 + n % 16 / 4 * 8 + 4 * half + n % 4;
-        if (row >= nq) continue;
+    if (!odd_tiles || row >= nq) return;
+    for (int n = 0; n < 64; ++n) {  // the lane's own elements, as above
+        const int el = n / 16 * 32 + n % 16 / 4 * 8 + 4 * half + n % 4;
         float c = 0.f;
         for (int e = 0; e < kEdge; ++e) {
             if (!(odd_tiles >> e & 1)) continue;
