@@ -3,7 +3,7 @@
 Plain numpy on float64 values of the inputs, one query row at a time; shares no code with the product library.
 
 rmsnorm(x, residual, weight, eps)        -> (v, u): the residual sum and the norm
-quantise(u, fmt)                         -> (codes, scales, values) by format: "group", "mx", "row"
+group_scales(u, fmt)                     -> (scales, width of a group) of the 8-bit forms: "group", "mx", "row"
 attend(q, k, v, scale)                   -> Attended of one query row over keys k [n, dk], values v [n, dv]
 append(...)                              -> the 8-bit cache after new tokens, in place
 E4M3                                     float64 value of every e4m3fn code
