@@ -9,10 +9,14 @@
 //
 // Bound by HBM (2 bytes a cached token, head and element) up to some 64 rows a key/value head.  Four wavefronts take the
 // tiles of a workgroup's chunk in turn, each with its own running maximum and sums, joined at the end through LDS.
-//   Measured: trees of up to 8 tokens of 16 sequences over 15000 to 60000 tokens, 64 heads of 64 on 8, 143 us (4.05 TB/s of
-// cache); four tokens over 16383, 64 heads of 128 on 4, 22 us, most of it the fixed cost of two launches and of 344 parts.
-// Wavefronts are alive for three quarters of the former (chunks of 69 to 81 rounds), and the vector unit (conversions,
-// exponentials and packing) is busy three quarters of that.
+// The weights are rounded to bf16 for the value product, whose operands are of that type; their sum keeps fp32.  A weight is
+// off by at most 2^-9 of itself, which takes the error of o against 64 bits from 1.7e-3 (its own rounding to bf16) to 2.2e-3
+// and 2.4e-3 (root mean square, both cases below); weights in two parts would double the value products.
+//   Measured: trees of up to 8 tokens of 16 sequences over 15000 to 60000 tokens, 64 heads of 64 on 8, 143 and 150 us on two
+// cards (4.05 and 3.9 TB/s of cache); four tokens over 16383, 64 heads of 128 on 4, 23 us, most of it the fixed cost of two
+// launches and of 456 parts.  Wavefronts are alive for three quarters of the former (chunks of 82 rounds at most, 75 on
+// average), and the vector unit (conversions, exponentials and packing) is busy three quarters of that.  64 tokens of one
+// sequence over 16383: 64 us with those heads of 128, 39 with those of 64; every 32 (64) rows read and convert the codes.
 #include "attn_plan.hpp"
 
 namespace ecospec {

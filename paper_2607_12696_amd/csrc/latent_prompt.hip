@@ -11,10 +11,14 @@
 //   panels: of 64 elements for keys (rows of 128 bytes, chunks of 16 XORed with row bits, so that 16 rows' chunks, a quarter
 //   of a read, lie in different banks), of 32 for values (rows of 64 bytes: half a read is 256 in a row).  So a read's
 //   place in the tile is an immediate offset.  One barrier a tile of 32 keys.
-// Measured: 5003 tokens of 128 heads 1.22 ms (842 TFLOP/s), 6 prompts of 563 to 1201 tokens, 16 heads, 74 us.  Workgroups of
+//   The weights are rounded to bf16, the type of the value product's operands; their sum keeps fp32.  A weight is off by at
+// most 2^-9 of itself, which takes the error of o against 64 bits from 1.6e-3 (its own rounding to bf16) to 2.2e-3 (root mean
+// square); weights in two parts would double the value products.
+// Measured: 5003 tokens of 128 heads 1.22 ms (842 TFLOP/s), 6 prompts of 563 to 1201 tokens, 16 heads, 75 us.  Workgroups of
 // 256 queries, one a compute unit, load half as often but wait for each other more and leave more idle rows: 1.24 ms and
-// 84 us.  The long prompt is held by the card's power (1.6 GHz; operands of zeros take a fifth less time), the short ones by
-// their longest row block.
+// 84 us.  In the long prompt the matrix cores are busy for half of the cycles and wavefronts wait for a quarter of theirs;
+// power counts too (operands of zeros take a fifth less time).  The short ones are held by their longest row block: 47 tiles
+// in series at 1.5 us, two workgroups sharing a compute unit.
 #include "attn_plan.hpp"
 
 namespace ecospec {

@@ -6,7 +6,9 @@
 // norm is never rounded to bf16 before it is coded.  The sum of squares is fp32,
 // a tree over the workgroup; v stays fp32 although `sum` is stored in bf16, so
 // the norm has one rounding.  Measured: 6001 rows of 2880 with MX codes 25 us
-// (6.3 TB/s, part of it from the memory-side cache), 4 rows of 7168 4 us.
+// (6.3 TB/s, part of it from the memory-side cache), 4 rows of 7168 4 us; 6001
+// rows of 7168 74 us with codes by row and 61 without codes.  Narrow rows leave
+// threads idle: 20000 of 512 19 us, 60000 of 128 44 us (1.4 TB/s).
 #include "attn.hpp"
 #include "device.hpp"
 
@@ -210,7 +212,7 @@ hipError_t launch_add_rmsnorm(const uint16_t *x, const uint16_t *residual, const
     // As many threads as the row has vectors of 8, up to the largest workgroup.  One vector a thread beats fewer threads
     // with more: 4 rows of 7168 take 3.9 us in the kernel, 4.4 us with two a thread and 6.2 us with four; 6001 rows 72 us
     // against 76 and 83.  Threads without one cost: 6001 rows of 2880 take 26 us, 32 us with 1024 threads; 20000 rows of
-    // 1536 take 46 us, 73 us with 512 threads.
+    // 1536 take 47 us, 73 us with 512 threads.
     if (d <= 2048)
         rmsnorm_kernel<256, 1><<<T, 256, 0, stream>>>(a);
     else if (d <= 4096)
