@@ -6,9 +6,9 @@
 // plan out for itself, from the two offsets and the length of each sequence: the chunk length is the smallest for which
 // all chunks run at once, or in two rounds where those are shorter.  (Row groups of different lengths leave chunks of
 // different lengths: 8 trees over 6000 to 20000 tokens have chunks of up to 188 tiles at once, of 143 on average, and of up
-// to 79 in two rounds: 375 us instead of 405 where a pass stands among others, 359 instead of 357 back to back.)  A row group of several chunks leaves its parts (fp32 output sums with the
-// reference maximum and the sum of the weights of each row) in the workspace, in the matrix cores' accumulator order, and
-// join_kernel adds them up in chunk order.
+// to 79 in two rounds: 375 us instead of 405 where a pass stands among others, 359 instead of 357 back to back.)  A row
+// group of several chunks leaves its parts (fp32 output sums with the reference maximum and the sum of the weights of each
+// row) in the workspace, in the matrix cores' accumulator order, and join_kernel adds them up in chunk order.
 #pragma once
 
 #include "attn.hpp"
