@@ -575,6 +575,146 @@ moe_status_t moe_cache_attn(const moe_cache_t *cache, const moe_drafts_t *drafts
                             const void *v_new, int H, float scale, void *o, float *lse, void *workspace,
                             size_t workspace_bytes, void *stream);
 
+/*
+ * The two ends of a decoding step: pages and prompts in, log probabilities
+ * out.
+ */
+
+/* Pages of B sequences, for caches paged as in moe_latent_cache_t (one update
+ * serves the caches of all layers that share the table).  Sequence b has
+ * cache_len[b] tokens in the first ceil(cache_len[b] / page) pages of its row
+ * of block_table; free_pages[0 .. n_free - 1] are the pages that nobody has.
+ * No page is in two places.  page 16, 32, 64 or 128; n_pages, max_blocks >= 1;
+ * max_blocks * page <= 2^30; 1 <= B <= 1024. */
+typedef struct {
+    int B, n_pages, page, max_blocks;
+    int32_t *block_table;     /* [B][max_blocks] */
+    const int32_t *cache_len; /* [B] */
+    int32_t *free_pages;      /* [n_pages] */
+    const int32_t *n_free;    /* [1] */
+} moe_page_pool_t;
+
+/*
+ * Pages for what a step changes: sequence b keeps its first keep_len[b] tokens
+ * (keep_len NULL: all; more than cache_len[b] means all) and gets n_b =
+ * token_offsets[b+1] - token_offsets[b] new ones behind them.  A request that
+ * ended keeps none and gets none; one that takes its place keeps none and gets
+ * its prompt.
+ *   have = ceil(cache_len[b] / page), want = ceil((keep + n_b) / page);
+ *   where want < have, pages want .. have - 1 of the sequence are returned:
+ *     the returned pages of all sequences, in order, go behind the free ones;
+ *   where want > have, the sequence takes want - have pages, from the end of
+ *     that list, in order of the sequences;
+ *   a sequence of want > max_blocks takes nothing, and so does one whose last
+ *     page, counted with all that the sequences before it ask for, is past
+ *     what the list holds: it is refused and stays as it was, none of its
+ *     tokens kept back or added.
+ *   token_offsets [B+1]: from 0 to at most N, none decreasing.
+ *   block_table, free_pages: updated in place (what free_pages holds from
+ *   *n_free_out on is left over and means nothing).
+ *   new_len [B] out: keep + n_b, cache_len[b] where refused.  n_free_out,
+ *   refused [1] out: the free pages left, and the refused sequences.
+ *   slots [N] (int64), positions [N] out: token t of sequence b, the i-th new
+ *   one, is at position keep + i, row `slots[t]` of the pages taken as one
+ *   array of n_pages * page rows.  Both are -1 for tokens of a refused
+ *   sequence and for entries from token_offsets[B] on.  Each may be NULL.
+ * new_len and n_free_out are buffers of their own (not cache_len, keep_len or
+ * n_free): the update reads the old counts throughout, and so do the calls that
+ * append the new tokens.  The same call again, on the same counts, gives the
+ * same results.  1 <= N <= 2^30.  One kernel, deterministic.
+ */
+moe_status_t moe_pages_update(const moe_page_pool_t *pool, const int32_t *keep_len, const int32_t *token_offsets, int N,
+                              int32_t *new_len, int32_t *n_free_out, int32_t *refused, int64_t *slots,
+                              int32_t *positions, void *stream);
+
+/*
+ * Rows of new tokens into the latent cache: row slots[i] of the pages, taken as
+ * one array of n_pages * page rows, becomes row rows[i] (rows NULL: i) of
+ * kv_new [n_rows][r+p] bf16.  A slot outside [0, n_pages * page) drops its
+ * entry; no slot within is given twice.  pages [n_pages][page][r+p] bf16, as in
+ * moe_latent_cache_t; slots [N] int64 (moe_pages_update's), rows [N].
+ * Requirements: r = 512, p = 64 (else MOE_ERR_UNSUPPORTED); page 16, 32, 64 or
+ * 128; pages and kv_new 16-byte aligned; N, n_rows >= 1, N <= 2^24 (else
+ * MOE_ERR_UNSUPPORTED).  One kernel.
+ */
+moe_status_t moe_latent_append(void *pages, int n_pages, int page, int r, int p, const void *kv_new, int n_rows,
+                               const int32_t *rows, int N, const int64_t *slots, void *stream);
+
+/*
+ * Grouped-query attention of whole prompts.  Sequence b has queries
+ * q_offsets[b] .. q_offsets[b+1] - 1 and keys kv_offsets[b] .. kv_offsets[b+1] - 1
+ * (both from 0 to at most N and M, none decreasing); its i-th query of n attends
+ * to the first i + 1 + (m - n) of its m keys (the queries are the last n of m
+ * tokens).  A query that attends to nothing gets zeros, and -inf as its
+ * log-sum; keys past a query's have no effect on it, infinities and NaN among
+ * them.  Query head h uses key/value head h / (H / Hkv).
+ *   s_j = scale * q[t][h] . k_j,  o[t][h] = sum_j softmax(s)_j v_j,
+ *   lse[t][h] = log sum_j exp(s_j)
+ *   q: head h of query t is the D elements from q + t * q_stride + h * q_head
+ *   on (strides in elements), k and v likewise by key and key/value head: parts
+ *   of one projection's output may be passed as they lie.
+ *   o [N][H][D] bf16; lse [N][H] fp32 or NULL.  Rows from q_offsets[B] on are
+ *   left as they were.
+ *   max_tokens: at least the most queries of a sequence.
+ *   workspace: device scratch of moe_grouped_prompt_workspace_size bytes, 256-byte
+ *   aligned; its contents on entry do not matter.  The size depends on D alone.
+ * Arithmetic as for moe_latent_attn.  Deterministic.
+ * Limits: D 64 or 128 (else MOE_ERR_UNSUPPORTED); 1 <= Hkv <= 256, H % Hkv == 0,
+ * H <= 1024, 1 <= B <= 1024, N, M >= 1, scale finite; strides >= 0 and multiples
+ * of 8, 16-byte aligned pointers; k_stride, v_stride <= 2^23, N * H <= 2^30 and
+ * B * H * max_tokens <= 2^30 (else MOE_ERR_UNSUPPORTED).
+ */
+typedef struct {
+    int N, M, B, H, Hkv, D, max_tokens;
+    const int32_t *q_offsets, *kv_offsets; /* [B+1] each */
+    const void *q, *k, *v;
+    int64_t q_stride, q_head, k_stride, k_head, v_stride, v_head;
+    float scale;
+} moe_grouped_prompt_t;
+
+moe_status_t moe_grouped_prompt_workspace_size(int D, size_t *bytes);
+moe_status_t moe_grouped_prompt(const moe_grouped_prompt_t *a, void *o, float *lse, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
+/* Type of the logits. */
+typedef enum {
+    MOE_F32 = 0,
+    MOE_BF16 = 1
+} moe_dtype_t;
+
+/*
+ * Log probabilities from logits: what a verification accepts drafts by, and
+ * what an answer reports.  Per row of V logits l, with s = scale * l (scale: the
+ * inverse temperature):
+ *   lse = log sum_j exp(s_j),  p_j = exp(s_j - lse),
+ *   logprob[m] = s_t - lse for each given token t = tokens[m] (-inf for a t
+ *     outside [0, V): a place that is not used),
+ *   entropy = -sum_j p_j log p_j,
+ *   top_idx, top_logprob: the k tokens of largest logit, larger first, equal
+ *     ones (-0 == +0) by lower index, NaN after every number.
+ * A logit of -inf has probability 0.  A row of nothing else has lse and all log
+ * probabilities -inf, and entropy 0.  A NaN among the logits, or a scaled one of
+ * +inf, makes the row's lse, entropy and log probabilities NaN (those of unused
+ * places stay -inf).
+ *   logits: row n is the V elements from logits + n * stride on (stride in
+ *   elements, >= V; any alignment of the type); dtype: moe_dtype_t.
+ *   tokens [N][M], logprob [N][M] (both NULL exactly when M is 0), lse and
+ *   entropy [N], each or NULL, top_idx [N][k], top_logprob [N][k] (top_idx NULL
+ *   exactly when k is 0; top_logprob may be NULL).
+ *   workspace: device scratch of moe_token_logprobs_workspace_size bytes,
+ *   256-byte aligned; its contents on entry do not matter.  The size for N rows
+ *   is enough for every call of no more rows.
+ * Arithmetic: fp32, the exponentials and their sums relative to the largest
+ * logits so far; the logits are read once.  Deterministic.
+ * Limits: 1 <= N <= 2^22, 1 <= V <= 2^24, 0 <= k <= min(V, 64), 0 <= M <= 65536,
+ * N * M <= 2^30, scale finite and > 0.  Two kernels.
+ */
+moe_status_t moe_token_logprobs_workspace_size(int N, size_t *bytes);
+moe_status_t moe_token_logprobs(const void *logits, int dtype, int64_t stride, int N, int V, float scale,
+                                const int32_t *tokens, int M, int k, float *logprob, float *lse, float *entropy,
+                                int32_t *top_idx, float *top_logprob, void *workspace, size_t workspace_bytes,
+                                void *stream);
+
 /* Static description of a status code. */
 const char *moe_status_string(moe_status_t status);
 

@@ -26,6 +26,13 @@ and the rest of a layer's verification step:
     moe_latent_prompt(q, k, k_rope, v, q_offsets, kv_offsets, scale)   -> (o, lse)
     moe_cache_append(k_new, v_new, token_offsets, k, v, k_scale, v_scale, block_table, cache_len)
     moe_cache_attn(q, k_new, v_new, token_offsets, k, v, k_scale, v_scale, block_table, cache_len, scale, mask) -> (o, lse)
+
+and the two ends of a decoding step:
+
+    moe_pages_update(cache_len, token_offsets, block_table, free_pages, n_free, page, N, keep_len) -> PageUpdate
+    moe_latent_append(kv_new, pages, slots, rows)
+    moe_grouped_prompt(q, k, v, q_offsets, kv_offsets, scale)           -> (o, lse)
+    moe_token_logprobs(logits, tokens, k, scale)                        -> TokenLogprobs
 """
 from __future__ import annotations
 
@@ -46,12 +53,15 @@ MOE_SEL_COST_RATIO, MOE_SEL_CONFIDENCE, MOE_SEL_GLOBAL_COST, MOE_SEL_COST_DIFF =
 MOE_ACT_SWIGLU, MOE_ACT_SWIGLU_OAI = 0, 1
 MOE_ACTQ_BF16, MOE_ACTQ_MXFP8 = 0, 1
 MOE_Q_NONE, MOE_Q_FP8_GROUP, MOE_Q_MXFP8, MOE_Q_FP8_ROW = 0, 1, 2, 3
+MOE_F32, MOE_BF16 = 0, 1
 
 EXPORTED = ("moe_route_topk", "moe_route_union", "moe_route_topk_grouped", "moe_router_workspace_size", "moe_route_topk_hidden", "moe_expert_union", "moe_verify_workspace_size", "moe_verify_layer",
             "moe_verify_layer_timed", "moe_packed_size", "moe_pack_weights", "moe_pack_gate_up", "moe_pack_down",
             "moe_select_tree", "moe_status_string", "moe_last_error", "moe_verify_layer_noalloc",
             "moe_add_rmsnorm", "moe_latent_attn_workspace_size", "moe_latent_attn", "moe_latent_prompt",
-            "moe_cache_append", "moe_cache_attn_workspace_size", "moe_cache_attn")
+            "moe_cache_append", "moe_cache_attn_workspace_size", "moe_cache_attn",
+            "moe_pages_update", "moe_latent_append", "moe_grouped_prompt_workspace_size", "moe_grouped_prompt",
+            "moe_token_logprobs_workspace_size", "moe_token_logprobs")
 
 
 class MoeError(RuntimeError):
@@ -94,6 +104,17 @@ class moe_cache_t(C.Structure):
         (n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "block_table", "cache_len")]
 
 
+class moe_page_pool_t(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("B", "n_pages", "page", "max_blocks")] + [
+        (n, C.c_void_p) for n in ("block_table", "cache_len", "free_pages", "n_free")]
+
+
+class moe_grouped_prompt_t(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("N", "M", "B", "H", "Hkv", "D", "max_tokens")] + [
+        (n, C.c_void_p) for n in ("q_offsets", "kv_offsets", "q", "k", "v")] + [
+        (n, C.c_int64) for n in ("q_stride", "q_head", "k_stride", "k_head", "v_stride", "v_head")] + [("scale", C.c_float)]
+
+
 _lock = threading.Lock()
 _lib = None
 
@@ -134,6 +155,12 @@ def lib() -> C.CDLL:
             L.moe_cache_append.argtypes = [st(moe_cache_t), p, p, i, p, i, i, p, i, p]
             L.moe_cache_attn_workspace_size.argtypes = [st(moe_cache_t), i, i, i, st(C.c_size_t)]
             L.moe_cache_attn.argtypes = [st(moe_cache_t), st(moe_drafts_t), p, p, p, i, C.c_float, p, p, p, C.c_size_t, p]
+            L.moe_pages_update.argtypes = [st(moe_page_pool_t), p, p, i, p, p, p, p, p, p]
+            L.moe_latent_append.argtypes = [p, i, i, i, i, p, i, p, i, p, p]
+            L.moe_grouped_prompt_workspace_size.argtypes = [i, st(C.c_size_t)]
+            L.moe_grouped_prompt.argtypes = [st(moe_grouped_prompt_t), p, p, p, C.c_size_t, p]
+            L.moe_token_logprobs_workspace_size.argtypes = [i, st(C.c_size_t)]
+            L.moe_token_logprobs.argtypes = [p, i, C.c_int64, i, i, C.c_float, p, i, i, p, p, p, p, p, p, C.c_size_t, p]
             L.moe_status_string.argtypes = [i]
             L.moe_status_string.restype = C.c_char_p
             L.moe_last_error.restype = C.c_char_p
@@ -141,7 +168,8 @@ def lib() -> C.CDLL:
                       "moe_verify_layer_noalloc", "moe_verify_layer_timed", "moe_packed_size", "moe_pack_weights", "moe_pack_gate_up",
                       "moe_pack_down", "moe_select_tree", "moe_add_rmsnorm", "moe_latent_attn_workspace_size",
                       "moe_latent_attn", "moe_latent_prompt", "moe_cache_append", "moe_cache_attn_workspace_size",
-                      "moe_cache_attn"):
+                      "moe_cache_attn", "moe_pages_update", "moe_latent_append", "moe_grouped_prompt_workspace_size",
+                      "moe_grouped_prompt", "moe_token_logprobs_workspace_size", "moe_token_logprobs"):
                 getattr(L, f).restype = i
             _lib = L
     return _lib
@@ -703,6 +731,151 @@ def moe_cache_attn(q, k_new, v_new, token_offsets, k, v, k_scale, v_scale, block
         C.byref(c), C.byref(d), _bf16_ptr(q, "q", N, H, c.D), _bf16_ptr(k_new, "k_new", N, c.Hkv, c.D),
         _bf16_ptr(v_new, "v_new", N, c.Hkv, c.D), H, scale, op, lp, _dev_ptr(workspace, "workspace"), nbytes, _stream(q)))
     return o, lse
+
+
+# --------------------------------------------------------------------------- the two ends of a decoding step
+
+@dataclass
+class PageUpdate:
+    """Counts after a moe_pages_update, and where the new tokens go."""
+    new_len: object    # int32 [B]
+    n_free: object     # int32 [1]
+    refused: object    # int32 [1]: sequences that got nothing
+    slots: object      # int64 [N]: row among all pages' rows, -1: none
+    positions: object  # int32 [N], -1: none
+
+
+def moe_pages_update(cache_len, token_offsets, block_table, free_pages, n_free, page: int, N: int, keep_len=None,
+                     out: PageUpdate | None = None) -> PageUpdate:
+    """Pages for what a step changes: sequence b keeps its first keep_len[b] tokens (None: all) and gets
+    token_offsets[b + 1] - token_offsets[b] new ones; pages that it no longer needs go to the free ones, those that it needs
+    are taken from there.
+
+    cache_len, keep_len [B], token_offsets [B + 1], n_free [1] int32; block_table [B, blocks] and free_pages [n_pages] int32
+    are updated in place.  N: entries of slots and positions, at least the new tokens.  The counts are not changed: the new
+    ones are new_len and n_free of the result, whose tensors are those of `out` where it is given."""
+    torch = _torch()
+    B, blocks = block_table.shape
+    n_pages, dev = free_pages.shape[0], block_table.device
+    if out is None:
+        ints = torch.empty(B + 2 + N, dtype=torch.int32, device=dev).split((B, 1, 1, N))
+        out = PageUpdate(*ints[:3], torch.empty(N, dtype=torch.int64, device=dev), ints[3])
+    if out.slots.dtype != torch.int64 or out.slots.shape != (N,):
+        raise ValueError("slots must be int64 [N]")
+    pool = moe_page_pool_t(B, n_pages, page, blocks, _int32_ptr(block_table, "block_table", B, blocks),
+                           _int32_ptr(cache_len, "cache_len", B), _int32_ptr(free_pages, "free_pages", n_pages),
+                           _int32_ptr(n_free, "n_free", 1))
+    _check("moe_pages_update", lib().moe_pages_update(
+        C.byref(pool), None if keep_len is None else _int32_ptr(keep_len, "keep_len", B),
+        _int32_ptr(token_offsets, "token_offsets", B + 1), N, _int32_ptr(out.new_len, "new_len", B),
+        _int32_ptr(out.n_free, "n_free", 1), _int32_ptr(out.refused, "refused", 1), _dev_ptr(out.slots, "slots"),
+        _int32_ptr(out.positions, "positions", N), _stream(block_table)))
+    return out
+
+
+def moe_latent_append(kv_new, pages, slots, rows=None) -> None:
+    """New rows into the latent cache, in place: row slots[i] of the pages becomes row rows[i] (None: i) of kv_new
+    [n_rows, r + p] bf16; slots int64 [N] (entries outside the pages, as -1, are dropped), rows int32 [N]; pages
+    [n_pages, page, r + p] bf16."""
+    torch = _torch()
+    n_pages, page, width = pages.shape
+    n_rows = kv_new.shape[0]
+    N = slots.shape[0]
+    if slots.dtype != torch.int64 or slots.dim() != 1:
+        raise ValueError("slots must be int64 [N]")
+    _check("moe_latent_append", lib().moe_latent_append(
+        _bf16_ptr(pages, "pages", n_pages, page, width), n_pages, page, width - 64, 64, _bf16_ptr(kv_new, "kv_new", n_rows, width),
+        n_rows, None if rows is None else _int32_ptr(rows, "rows", N), N, _dev_ptr(slots, "slots"), _stream(pages)))
+
+
+def moe_grouped_prompt_workspace_size(D: int) -> int:
+    n = C.c_size_t()
+    _check("moe_grouped_prompt_workspace_size", lib().moe_grouped_prompt_workspace_size(D, C.byref(n)))
+    return n.value
+
+
+def moe_grouped_prompt(q, k, v, q_offsets, kv_offsets, scale: float, max_tokens: int | None = None, o=None, lse=None,
+                       workspace=None):
+    """Grouped-query attention, causal, of the prompts of B sequences -> (o [N, H, D] bf16, lse [N, H] fp32).
+
+    q [N, H, D], k, v [M, Hkv, D] bf16 (strided views of a projection's output, contiguous along D); q_offsets, kv_offsets
+    [B + 1] int32.  A sequence's queries are the last of its keys' tokens.  max_tokens: at least the most queries of a
+    sequence (None: N)."""
+    N, H = q.shape[:2]
+    M, Hkv = k.shape[:2]
+    B = q_offsets.shape[0] - 1
+    qp, D, qs, qh = _strided_ptr(q, "q", N, H)
+    kp, dk, ks, kh = _strided_ptr(k, "k", M, Hkv)
+    vp, dv, vs, vh = _strided_ptr(v, "v", M, Hkv)
+    if dk != D or dv != D:
+        raise ValueError("q, k and v must have heads of one width")
+    o, lse, op, lp = _attn_outputs(q, D, o, lse)
+    if workspace is None:
+        workspace = _torch().empty(moe_grouped_prompt_workspace_size(D), dtype=_torch().uint8, device=q.device)
+    a = moe_grouped_prompt_t(N, M, B, H, Hkv, D, N if max_tokens is None else max_tokens,
+                             _int32_ptr(q_offsets, "q_offsets", B + 1), _int32_ptr(kv_offsets, "kv_offsets", B + 1), qp, kp, vp,
+                             qs, qh, ks, kh, vs, vh, scale)
+    _check("moe_grouped_prompt", lib().moe_grouped_prompt(C.byref(a), op, lp, _dev_ptr(workspace, "workspace"),
+                                                          workspace.numel() * workspace.element_size(), _stream(q)))
+    return o, lse
+
+
+@dataclass
+class TokenLogprobs:
+    """What moe_token_logprobs gives; what was not asked for is None."""
+    logprob: object      # fp32 [N, M] (or [N], as the tokens)
+    lse: object          # fp32 [N]
+    entropy: object      # fp32 [N]
+    top_idx: object      # int32 [N, k]
+    top_logprob: object  # fp32 [N, k]
+
+
+def moe_token_logprobs_workspace_size(N: int) -> int:
+    n = C.c_size_t()
+    _check("moe_token_logprobs_workspace_size", lib().moe_token_logprobs_workspace_size(N, C.byref(n)))
+    return n.value
+
+
+def moe_token_logprobs(logits, tokens=None, k: int = 0, scale: float = 1.0, out: TokenLogprobs | None = None,
+                       workspace=None) -> TokenLogprobs:
+    """Log probabilities of given tokens, log-sum, entropy and the k best alternatives of rows of logits [N, V].
+
+    logits bf16 or fp32, contiguous along V (rows may be strided); tokens int32 [N, M] or [N], entries outside [0, V) unused
+    (-inf), or None; k: alternatives, largest logit first, equal ones by lower index; scale: the inverse temperature.
+    out: tensors to write to (those that are None are not computed, but for what tokens and k ask for)."""
+    torch = _torch()
+    if logits.dim() != 2 or logits.stride(1) != 1 and logits.shape[1] != 1:
+        raise ValueError("logits must be [N, V], contiguous along V")
+    N, V = logits.shape
+    if not logits.is_cuda or logits.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("logits must be bfloat16 or float32, on the device")
+    M = 0
+    if tokens is not None:
+        if tokens.dim() not in (1, 2) or tokens.shape[0] != N:
+            raise ValueError("tokens must be int32 [N] or [N, M]")
+        M = tokens.numel() // max(N, 1)
+        if not M:
+            tokens = None
+    dev, f32 = logits.device, torch.float32
+    if out is None:
+        rows = torch.empty(N * (2 + M + k), dtype=f32, device=dev).split((N * M, N, N, N * k))
+        out = TokenLogprobs(rows[0].view(tokens.shape) if M else None, rows[1], rows[2],
+                            torch.empty(N, k, dtype=torch.int32, device=dev) if k else None, rows[3].view(N, k) if k else None)
+    if (out.logprob is None) != (not M) or (out.top_idx is None) != (not k):
+        raise ValueError("out.logprob goes with tokens, out.top_idx with k")
+    for t, what, shape in ((out.logprob, "logprob", tokens.shape if M else None), (out.lse, "lse", (N,)),
+                           (out.entropy, "entropy", (N,)), (out.top_logprob, "top_logprob", (N, k))):
+        if t is not None and (t.dtype != f32 or tuple(t.shape) != tuple(shape)):
+            raise ValueError(f"{what} must be float32 {list(shape)}")
+    if workspace is None:
+        workspace = torch.empty(moe_token_logprobs_workspace_size(N), dtype=torch.uint8, device=dev)
+    _check("moe_token_logprobs", lib().moe_token_logprobs(
+        logits.data_ptr(), MOE_BF16 if logits.dtype == torch.bfloat16 else MOE_F32, logits.stride(0) if N > 1 else max(V, logits.stride(0)), N, V, scale,
+        _int32_ptr(tokens, "tokens", *tokens.shape) if M else None, M, k, _dev_ptr(out.logprob, "logprob"), _dev_ptr(out.lse, "lse"),
+        _dev_ptr(out.entropy, "entropy"), _int32_ptr(out.top_idx, "top_idx", N, k) if k else None,
+        _dev_ptr(out.top_logprob, "top_logprob"), _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(),
+        _stream(logits)))
+    return out
 
 
 # --------------------------------------------------------------------------- selector (host)

@@ -21,8 +21,8 @@ LIB = os.path.join(PKG, "libecospec_moe.so")
 BUILD = os.path.join(ROOT, "_build")
 
 SOURCES = ["route_topk.hip", "expert_union.hip", "expert_ffn.hip", "expert_small.hip", "pack.hip", "router.hip", "noalloc.hip",
-           "rmsnorm.hip", "latent_attn.hip", "latent_prompt.hip", "cache_append.hip", "cache_attn.hip", "abi.cpp",
-           "attn_abi.cpp", "selector.cpp"]
+           "rmsnorm.hip", "latent_attn.hip", "latent_prompt.hip", "cache_append.hip", "cache_attn.hip", "pages.hip",
+           "grouped_prompt.hip", "token_logprobs.hip", "abi.cpp", "attn_abi.cpp", "step_abi.cpp", "selector.cpp"]
 ARCH = "gfx950"
 DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 COMMON = ["-O3", "-std=c++17", "-fPIC", f"-I{INCLUDE}", f"-I{CSRC}", "-Wall", "-Wno-unused-function"]
