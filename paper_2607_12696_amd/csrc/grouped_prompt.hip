@@ -7,9 +7,10 @@
 //   (O^T = V^T P^T), and V^T is read with the transposing LDS load.
 //   Three tiles of 32 keys are under way: while the matrix cores multiply the keys of tile t + 1 and the values of tile
 //   t - 1, the vector unit works out the weights of tile t, a piece behind each product.
-//   Keys and values go from memory straight to LDS, two tiles ahead (rings of three tiles of keys, five of values), in
+//   Keys and values go from memory straight to LDS, two tiles before their products (rings of four tiles each), in
 //   panels: of 64 elements for keys (rows of 128 bytes, chunks of 16 XORed with row bits, so that 16 rows' chunks, a quarter
-//   of a read, lie in different banks), of 32 for values (rows of 64 bytes: half a read is 256 in a row).  One barrier a tile.
+//   of a read, lie in different banks), of 32 for values (rows of 64 bytes: half a read is 256 in a row).  One barrier a
+//   tile, and operands are read seven products ahead, past it: keys land a tile earlier than that needs.
 #include "attn_plan.hpp"
 #include "step.hpp"
 
@@ -42,16 +43,18 @@ __device__ __forceinline__ void mfma_next(f32x16 &s, const bf16x8 &k, const bf16
 
 // D: width of a head; R: row tiles of a wavefront.
 template <int D, int R>
-__global__ __launch_bounds__(kPromptThreads, R == 1 || D == 64 ? 2 : 1) void prompt_kernel(GroupedPromptArgs a, int blocks)
+__global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(GroupedPromptArgs a, int blocks)
 {
     constexpr int kRows = 32 * R * kPromptWaves, kSteps = D / 16, kPanels = D / 64, kTiles = D / 32;
     constexpr int kTile = kKeys * D * 2, kLoads = 2 * kPanels;  // bytes of a tile; loads of a tile by a wavefront
     constexpr int kEdge = kRows / kKeys + 1;                    // most tiles that some rows of a workgroup see in part
-    constexpr int kRing = 4, kAhead = 3;                        // key and value operands in registers
-    constexpr int kProducts = (kSteps + 2 * kTiles) * R, kPieces = 20 * R;  // of a tile
+    constexpr int kOperands = kSteps + 2 * kTiles;              // key and value operands of a tile
+    constexpr int kRing = 8, kAhead = kRing - 1;                // of them in registers
+    static_assert(kOperands % kRing == 0, "a tile's first operand has a fixed place");
+    constexpr int kProducts = kOperands * R, kPieces = 20 * R;  // of a tile
     struct Tiles {
-        char k[3][kTile];  // panel, row r, chunk c of 16 bytes at place c ^ (r >> 1 & 7)
-        char v[5][kTile];  // panel of 32 elements, row
+        char k[4][kTile];  // panel, row r, chunk c of 16 bytes at place c ^ (r >> 1 & 7)
+        char v[4][kTile];  // panel of 32 elements, row
         uint16_t some[kEdge][R][kPromptThreads];  // which weights of a lane are not zero, in a tile with infinities or NaN
     };
     __shared__ __attribute__((aligned(16))) Tiles lds;
@@ -103,42 +106,54 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 || D == 64 ? 2 : 1) void pro
     const uint32_t off_v = (v_row + lane / 4) * stride_v + v_panel * 64 + lane % 4 * 16, off_low = off_v + 16 * stride_v;
     const uint32_t ring_k = __builtin_amdgcn_readfirstlane(lds_addr(lds.k) + wave * 1024);
     const uint32_t ring_v = __builtin_amdgcn_readfirstlane(lds_addr(lds.v) + v_panel * 2048 + v_row * 64);
-    int left_k = tiles ? nk : 0;  // keys from the tile to load next on
+    int left_k = nk, left_v = nk;  // keys from the tile to load next on
     uint32_t to_k = ring_k, to_v = ring_v;
-    u32x4 k_src, v_src;
-    auto aim = [&] {
+    u32x4 key_src, value_src;
+    auto aim_keys = [&] {
         const int n = max(min(left_k, kKeys), 0);
-        k_src = rsrc_words(src_k, n ? (uint32_t)(n - 1) * stride_k + D * 2 : 0);
-        v_src = rsrc_words(src_v, n ? (uint32_t)(n - 1) * stride_v + D * 2 : 0);
+        key_src = rsrc_words(src_k, n ? (uint32_t)(n - 1) * stride_k + D * 2 : 0);
     };
-    auto advance = [&] {
+    auto aim_values = [&] {
+        const int n = max(min(left_v, kKeys), 0);
+        value_src = rsrc_words(src_v, n ? (uint32_t)(n - 1) * stride_v + D * 2 : 0);
+    };
+    auto keys_done = [&] {
         left_k -= kKeys;
-        if (left_k > 0) {
-            src_k += kKeys / 2 * stride_k;
-            src_v += kKeys / 2 * stride_v;
-        }
-        to_k = to_k == ring_k + 2 * kTile ? ring_k : to_k + kTile;
-        to_v = to_v == ring_v + 4 * kTile ? ring_v : to_v + kTile;
+        if (left_k > 0) src_k += kKeys / 2 * stride_k;
+        to_k = to_k == ring_k + 3 * kTile ? ring_k : to_k + kTile;
+    };
+    auto values_done = [&] {
+        left_v -= kKeys;
+        if (left_v > 0) src_v += kKeys / 2 * stride_v;
+        to_v = to_v == ring_v + 3 * kTile ? ring_v : to_v + kTile;
     };
     auto load = [&](int n) {
-        if (n < kPanels) load16_lds(k_src, off_k + n * 128, to_k + n * (kKeys * 128));
-        else if (n == kPanels) load16_lds(v_src, off_v, to_v);
-        else load16_lds(v_src, off_low, to_v + 1024);
+        if (n < kPanels) load16_lds(key_src, off_k + n * 128, to_k + n * (kKeys * 128));
+        else if (n == kPanels) load16_lds(value_src, off_v, to_v);
+        else load16_lds(value_src, off_low, to_v + 1024);
+    };
+    auto load_keys = [&] {
+        aim_keys();
+#pragma unroll
+        for (int n = 0; n < kPanels; ++n) load(n);
+        keys_done();
+    };
+    auto load_values = [&] {
+        aim_values();
+#pragma unroll
+        for (int n = kPanels; n < kLoads; ++n) load(n);
+        values_done();
     };
 #pragma unroll 1
-    for (int t = 0; t < 2; ++t) {
-        aim();
-#pragma unroll
-        for (int n = 0; n < kLoads; ++n) load(n);
-        advance();
-    }
+    for (int t = 0; t < 3; ++t) load_keys();
+    load_values();
     // The values of tile -1, whose weights are zeros.
-    for (int i = threadIdx.x; i < kTile / 16; i += kPromptThreads) reinterpret_cast<u32x4 *>(lds.v[4])[i] = u32x4{0, 0, 0, 0};
+    for (int i = threadIdx.x; i < kTile / 16; i += kPromptThreads) reinterpret_cast<u32x4 *>(lds.v[3])[i] = u32x4{0, 0, 0, 0};
 
     f32x16 o[R][kTiles];
     float m[R], l[R], down[R];
     int scaled[R];
-    bf16x8 p[R][2] = {};  // weights of the tile before: 16 keys each
+    u32x4 p0[R][2] = {}, p1[R][2];  // weights of the tile before and of this one, in turn: 16 keys each
 #pragma unroll
     for (int r = 0; r < R; ++r) {
 #pragma unroll
@@ -161,8 +176,7 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 || D == 64 ? 2 : 1) void pro
 
     // Piece c of the weights of row tile r with scores s.  Register i is key 8 (i / 4) + 4 half + i % 4.
     float top[R], base[R], sum[R];
-    u32x4 packed[R][2];
-    auto weights = [&](f32x16 &s, int r, int c) {
+    auto weights = [&](f32x16 &s, u32x4 (&p)[2], int r, int c) {
         if (c == 0) {
             top[r] = max3(max3(max3(s[0], s[1], s[2]), max3(s[3], s[4], s[5]), s[6]),
                           max3(max3(s[7], s[8], s[9]), max3(s[10], s[11], s[12]), s[13]), fmaxf(s[14], s[15]));
@@ -179,78 +193,77 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 || D == 64 ? 2 : 1) void pro
             sum[r] = 0.f;
         } else {
             const int e = c - 3;  // of 16 elements
-            if (e < 16) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], scale2, -base[r]));
-            // The element before: its sum, and pairs to bf16.  Written out to stay here, where the compiler would sink them
-            // behind all products; a piece later, because the result of an exp2 needs a wait state.
+            // Written out to stay here, where the compiler would sink it behind all products, and in this order: the result of
+            // an exponential needs a wait state, which the instructions of the element before are.
+            if (e < 16) {
+                const float x = fmaf(s[e], scale2, -base[r]);
+                asm volatile("v_exp_f32 %0, %1" : "=v"(s[e]) : "v"(x));
+            }
+            // The element before: its sum, and pairs to bf16.
             if (e > 0 && e <= 16) {
                 const int i = e - 1;
                 asm volatile("v_add_f32 %0, %0, %1" : "+v"(sum[r]) : "v"(s[i]));
                 if (i % 2) {
                     uint32_t w;
                     asm volatile("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(w) : "v"(s[i - 1]), "v"(s[i]));
-                    packed[r][i / 8][i % 8 / 2] = w;
+                    p[i / 8][i % 8 / 2] = w;
                 }
                 if (i == 15) l[r] = fmaf(l[r], down[r], sum[r]);
             }
         }
     };
-    // Operands of the tiles at these ring offsets.
-    uint32_t key_at[4], value_at = v_at + 4 * kTile;
-    auto k_frag = [&](int st) { return *reinterpret_cast<const bf16x8 *>(lds.k[0] + key_at[st % 4] + st / 4 * (kKeys * 128)); };
-    auto v_frag = [&](int n) {  // n: kTiles * (16 keys) + element tile
-        const char *w = lds.v[0] + value_at + n % kTiles * (kKeys * 64) + n / kTiles * 16 * 64;
-        const u32x2 lo = read_tr(w), hi = read_tr(w + 8 * 64);
-        return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
-    };
-    bf16x8 k[kRing], v[kAhead];
-    // Products of a tile's keys (the first ones fetched) into s, then of a tile's values, `between(c)` behind product c.
-    auto products = [&](f32x16 (&s)[R], auto between) {
+    // Operand f of a tile: its keys' steps, then its values' (16 keys, element tile).  From kOperands on the next tile's.
+    uint32_t key_to = 0, value_to = 2 * kTile, key_at[4], value_at;
+    bf16x8 ring[kRing];
+    auto fetch = [&](int f) {
+        const int x = f % kOperands;
+        if (x == 0) {
+            key_to = key_to == 3 * kTile ? 0 : key_to + kTile;
 #pragma unroll
-        for (int st = 0; st < kSteps; ++st) {
-            if (st + kRing - 1 < kSteps) k[(st + kRing - 1) % kRing] = k_frag(st + kRing - 1);
-            else v[st + kRing - 1 - kSteps] = v_frag(st + kRing - 1 - kSteps);
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                __builtin_amdgcn_sched_barrier(0);
-                if (st == 0) mfma_first(s[r], k[0], q[r][0]);
-                else mfma_next(s[r], k[st % kRing], q[r][st]);
-                between(st * R + r);
-            }
+            for (int i = 0; i < 4; ++i) key_at[i] = k_at[i] + key_to;
         }
-        static_assert(kRing - 1 == kAhead, "the last steps fetch the first value operands");
+        if (x == kSteps) {
+            value_to = value_to == 3 * kTile ? 0 : value_to + kTile;
+            value_at = v_at + value_to;
+        }
+        if (x < kSteps) {
+            ring[f % kRing] = *reinterpret_cast<const bf16x8 *>(lds.k[0] + key_at[x % 4] + x / 4 * (kKeys * 128));
+        } else {
+            const char *w = lds.v[0] + value_at + (x - kSteps) % kTiles * (kKeys * 64) + (x - kSteps) / kTiles * 16 * 64;
+            const u32x2 lo = read_tr(w), hi = read_tr(w + 8 * 64);
+            ring[f % kRing] = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+        }
+    };
+    // Products of a tile's keys into s, then of a tile's values by p, `between(c)` behind product c.
+    auto products = [&](f32x16 (&s)[R], u32x4 (&p)[R][2], auto between) {
 #pragma unroll
-        for (int n = 0; n < 2 * kTiles; ++n) {
+        for (int f = 0; f < kOperands; ++f) {
+            fetch(f + kAhead);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 __builtin_amdgcn_sched_barrier(0);
-                o[r][n % kTiles] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[n % kAhead], p[r][n / kTiles], o[r][n % kTiles], 0, 0, 0);
-                between((kSteps + n) * R + r);
+                const int n = f - kSteps;
+                if (f == 0) mfma_first(s[r], ring[0], q[r][0]);
+                else if (f < kSteps) mfma_next(s[r], ring[f % kRing], q[r][f]);
+                else o[r][n % kTiles] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    ring[f % kRing], __builtin_bit_cast(bf16x8, p[r][n / kTiles]), o[r][n % kTiles], 0, 0, 0);
+                between(f * R + r);
             }
-            if (n + kAhead < 2 * kTiles) v[n % kAhead] = v_frag(n + kAhead);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
 
-    uint32_t key_to = 0, value_to = 4 * kTile;
-    auto turn_rings = [&] {  // to the keys and the values after
-        key_to = key_to == 2 * kTile ? 0 : key_to + kTile;
-        value_to = value_to == 4 * kTile ? 0 : value_to + kTile;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) key_at[i] = k_at[i] + key_to;
-        value_at = v_at + value_to;
-    };
-
-    // One tile: s its scores, next the scores of the tile after.
-    auto tile = [&](int t, f32x16 (&s)[R], f32x16 (&next)[R]) {
-        // Tile t + 1 has landed; every wavefront is past the scores of tile t and the values of tile t - 2.
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads) : "memory");
-#pragma unroll
-        for (int st = 0; st < kRing - 1; ++st) k[st] = k_frag(st);
-        aim();
+    // One tile: s its scores, p its weights, next the scores of the tile after, was the weights of the tile before.
+    auto tile = [&](int t, f32x16 (&s)[R], f32x16 (&next)[R], u32x4 (&p)[R][2], u32x4 (&was)[R][2]) {
+        // The keys of tile t + 2 and the values of tile t have landed; every wavefront is past the scores of tile t and the
+        // values of tile t - 2.
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLoads) : "memory");
+        aim_keys();
+        aim_values();
         if (t >= edge && t < tiles) {
             // A weight of zero must not meet an infinity or NaN: where a tile that not all rows see to its end has one,
             // zeros take its place, and what it gives the rows that see it is added at the end.
-            u32x4 *all = reinterpret_cast<u32x4 *>(lds.v[t % 5]);
+            u32x4 *all = reinterpret_cast<u32x4 *>(lds.v[t % 4]);
             bool odd = false;
             for (int i = threadIdx.x; i < kTile / 16; i += kPromptThreads) {
                 u32x4 x = all[i];
@@ -283,57 +296,52 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 || D == 64 ? 2 : 1) void pro
                     if (i / 4 * 8 + i % 4 >= left) s[r][i] = -INFINITY;
             }
         }
-        products(next, [&](int c) {
+        products(next, was, [&](int c) {
 #pragma unroll
-            for (int j = c * kPieces / kProducts; j < (c + 1) * kPieces / kProducts; ++j) weights(s[j % R], j % R, j / R);
+            for (int j = c * kPieces / kProducts; j < (c + 1) * kPieces / kProducts; ++j) weights(s[j % R], p[j % R], j % R, j / R);
             // The loads behind the last products but one, every other.
             const int n = (c - (kProducts - 2 * kLoads)) / 2;
             if (c >= kProducts - 2 * kLoads && (c - kProducts) % 2 == 0) load(n);
         });
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int st = 0; st < 2; ++st) p[r][st] = __builtin_bit_cast(bf16x8, packed[r][st]);
-        advance();
-        turn_rings();
+        keys_done();
+        values_done();
         if (odd_tiles >> max(t - edge, 0) & 1) {  // no bit is set before tile `edge`
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 uint32_t some = 0;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) some |= (s[r][i] != 0.f ? 1u : 0u) << i;
+                for (int i = 0; i < 16; ++i) {
+                    float w = s[r][i];
+                    asm volatile("" : "+v"(w));  // here, not ahead of the branch in every tile
+                    some |= (w != 0.f ? 1u : 0u) << i;
+                }
                 if (t < tiles) lds.some[t - edge][r][threadIdx.x] = (uint16_t)some;
             }
         }
     };
 
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    aim();
-#pragma unroll
-    for (int n = 0; n < kLoads; ++n) load(n);
-    advance();
+    load_keys();
+    load_values();
     f32x16 s0[R], s1[R];
-    {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) key_at[i] = k_at[i];
+    for (int st = 0; st < kSteps; ++st) {
+        const bf16x8 k = *reinterpret_cast<const bf16x8 *>(lds.k[0] + k_at[st % 4] + st / 4 * (kKeys * 128));
 #pragma unroll
-        for (int st = 0; st < kSteps; ++st)
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                if (st == 0) mfma_first(s0[r], k_frag(0), q[r][0]);
-                else mfma_next(s0[r], k_frag(st), q[r][st]);
-            }
-#pragma unroll
-        for (int r = 0; r < R; ++r) asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s0[r]));
+        for (int r = 0; r < R; ++r) {
+            if (st == 0) mfma_first(s0[r], k, q[r][0]);
+            else mfma_next(s0[r], k, q[r][st]);
+        }
     }
-    key_to = kTile;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) key_at[i] = k_at[i] + kTile;
+    for (int r = 0; r < R; ++r) asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s0[r]));
+#pragma unroll
+    for (int f = 0; f < kAhead; ++f) fetch(f);
     // Tiles 0 .. tiles: the last adds the values of the last but one.
 #pragma unroll 1
     for (int t = 0; t <= tiles; t += 2) {
-        tile(t, s0, s1);
-        if (t + 1 <= tiles) tile(t + 1, s1, s0);
+        tile(t, s0, s1, p1, p0);
+        if (t + 1 <= tiles) tile(t + 1, s1, s0, p0, p1);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing is on its way to LDS when the workgroup ends
 
@@ -387,7 +395,7 @@ size_t grouped_prompt_workspace(int D) { return 256; }
 hipError_t launch_grouped_prompt(const GroupedPromptArgs &a, int D, void *workspace, hipStream_t stream)
 {
 #ifndef ECOSPEC_GP_R
-#define ECOSPEC_GP_R 2
+#define ECOSPEC_GP_R 1
 #endif
     if (D == 64) launch<64, ECOSPEC_GP_R>(a, stream);
     else launch<128, ECOSPEC_GP_R>(a, stream);
