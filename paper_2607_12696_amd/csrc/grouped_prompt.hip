@@ -7,10 +7,12 @@
 //   (O^T = V^T P^T), and V^T is read with the transposing LDS load.
 //   Three tiles of 32 keys are under way: while the matrix cores multiply the keys of tile t + 1 and the values of tile
 //   t - 1, the vector unit works out the weights of tile t, a piece behind each product.
-//   Keys and values go from memory straight to LDS, two tiles before their products (rings of four tiles each), in
-//   panels: of 64 elements for keys (rows of 128 bytes, chunks of 16 XORed with row bits, so that 16 rows' chunks, a quarter
-//   of a read, lie in different banks), of 32 for values (rows of 64 bytes: half a read is 256 in a row).  One barrier a
-//   tile, and operands are read seven products ahead, past it: keys land a tile earlier than that needs.
+//   Keys and values go from memory straight to LDS, two steps (of KT tiles) before their products, in panels: of 64 elements
+//   for keys (rows of 128 bytes, chunks of 16 XORed with row bits, so that 16 rows' chunks, a quarter of a read, lie in
+//   different banks), of 32 for values (rows of 64 bytes: half a read is 256 in a row).  One barrier a step, and operands are
+//   read seven products ahead, past it: keys land a tile earlier than that needs.
+//   Where there are few row blocks, each one's keys are cut into chunks, a workgroup each, whose sums join_prompt_kernel
+//   adds up in order.
 #include "attn_plan.hpp"
 #include "step.hpp"
 
@@ -18,6 +20,9 @@ namespace ecospec {
 namespace {
 
 constexpr int kKeys = 32, kPromptWaves = 4, kPromptThreads = kPromptWaves * kWave;
+constexpr int kSplitRows = 32 * kPromptWaves;  // rows of a workgroup where keys are cut
+constexpr int kSlots = 2 * kCus;               // workgroups of such a call
+constexpr int kMinTiles = 4;                   // of a chunk
 constexpr float kSlack = 8.f;  // powers of two that weights may pass 1 by before their reference maximum moves
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
@@ -29,53 +34,96 @@ __device__ __forceinline__ u32x2 read_tr(const char *p)
 
 __device__ __forceinline__ bool not_finite(uint32_t bf16) { return (bf16 & 0x7f80u) == 0x7f80u; }
 
-// The score products, sums in vector registers, which the vector unit works on; a register written by the vector
-// unit needs two wait states before a product reads it.
+__device__ __forceinline__ float max2(float a, float b)  // without the copies that make signalling NaN quiet
+{
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+
+// The score products, sums in vector registers, which the vector unit works on, queries in accumulation registers.  A sum is
+// added to again two wait states later at the earliest: with one row tile (WAIT) they are written out.
 __device__ __forceinline__ void mfma_first(f32x16 &s, const bf16x8 &k, const bf16x8 &q)
 {
-    asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(k), "v"(q));
+    asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(k), "a"(q));
 }
 
+template <bool WAIT>
 __device__ __forceinline__ void mfma_next(f32x16 &s, const bf16x8 &k, const bf16x8 &q)
 {
-    asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(k), "v"(q));
+    if (WAIT) asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(k), "a"(q));
+    else asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(k), "a"(q));
 }
 
-// D: width of a head; R: row tiles of a wavefront.
-template <int D, int R>
-__global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(GroupedPromptArgs a, int blocks)
+// The chunks of a row block of `tiles` tiles.
+__device__ __forceinline__ int chunks_of(int tiles, int most) { return min(most, max(tiles / kMinTiles, 1)); }
+
+// A workgroup's row block: its sequence and key/value head, and what its rows see.
+struct Block {
+    int q0, nq, k0, nk, hk, rows, row0, tiles, G;
+
+    __device__ __forceinline__ int limit(int row) const { return min(max(row / G + 1 + nk - nq, 0), nk); }  // keys of a query row
+
+    __device__ __forceinline__ Block(const GroupedPromptArgs &a, int pair, int block, int block_rows)
+    {
+        const int b = pair / a.Hkv;
+        hk = pair % a.Hkv;
+        G = a.H / a.Hkv;
+        q0 = __builtin_amdgcn_readfirstlane(min(max(a.q_offsets[b], 0), a.N));
+        nq = __builtin_amdgcn_readfirstlane(min(max(a.q_offsets[b + 1], q0), a.N)) - q0;
+        k0 = __builtin_amdgcn_readfirstlane(min(max(a.kv_offsets[b], 0), a.M));
+        nk = __builtin_amdgcn_readfirstlane(min(max(a.kv_offsets[b + 1], k0), a.M)) - k0;
+        rows = nq * G;
+        row0 = block * block_rows;
+        tiles = row0 < rows ? (limit(min(row0 + block_rows, rows) - 1) + kKeys - 1) / kKeys : 0;
+    }
+};
+
+// Sums of a chunk: for each row the reference maximum and the weights' sum, and the output sums in accumulator order.
+struct PromptParts {
+    float2 *ml;  // [slot][kSplitRows]
+    float *o;    // [slot][wavefront][D / 32][4][lane][4]
+};
+
+// D: width of a head; R: row tiles of a wavefront; KT: key tiles a barrier; SPLIT: keys are cut into chunks.
+template <int D, int R, int KT, bool SPLIT>
+__global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(GroupedPromptArgs a, int blocks, int most_chunks,
+                                                                                PromptParts parts)
 {
     constexpr int kRows = 32 * R * kPromptWaves, kSteps = D / 16, kPanels = D / 64, kTiles = D / 32;
     constexpr int kTile = kKeys * D * 2, kLoads = 2 * kPanels;  // bytes of a tile; loads of a tile by a wavefront
     constexpr int kEdge = kRows / kKeys + 1;                    // most tiles that some rows of a workgroup see in part
     constexpr int kOperands = kSteps + 2 * kTiles;              // key and value operands of a tile
     constexpr int kRing = 8, kAhead = kRing - 1;                // of them in registers
+    constexpr int kHeld = 4 * KT;                               // tiles of keys, and of values, in LDS
     static_assert(kOperands % kRing == 0, "a tile's first operand has a fixed place");
+    static_assert(!SPLIT || kRows == kSplitRows, "parts");
     constexpr int kProducts = kOperands * R, kPieces = 20 * R;  // of a tile
     struct Tiles {
-        char k[4][kTile];  // panel, row r, chunk c of 16 bytes at place c ^ (r >> 1 & 7)
-        char v[4][kTile];  // panel of 32 elements, row
+        char k[kHeld][kTile];  // panel, row r, chunk c of 16 bytes at place c ^ (r >> 1 & 7)
+        char v[kHeld][kTile];  // panel of 32 elements, row
         uint16_t some[kEdge][R][kPromptThreads];  // which weights of a lane are not zero, in a tile with infinities or NaN
     };
     __shared__ __attribute__((aligned(16))) Tiles lds;
 
-    const int G = a.H / a.Hkv, pairs = a.B * a.Hkv;
+    const int pairs = a.B * a.Hkv;
     // Workgroups are dealt to the eight XCDs in turn: with pairs innermost a head's row blocks meet on few of them.  The
     // longest row blocks first, so that no long one is left for the end.
-    const int pair = blockIdx.x % pairs, block = blocks - 1 - (int)(blockIdx.x / pairs);
-    const int b = pair / a.Hkv, hk = pair % a.Hkv;
-    const int q0 = __builtin_amdgcn_readfirstlane(min(max(a.q_offsets[b], 0), a.N));
-    const int nq = __builtin_amdgcn_readfirstlane(min(max(a.q_offsets[b + 1], q0), a.N)) - q0;
-    const int k0 = __builtin_amdgcn_readfirstlane(min(max(a.kv_offsets[b], 0), a.M));
-    const int nk = __builtin_amdgcn_readfirstlane(min(max(a.kv_offsets[b + 1], k0), a.M)) - k0;
-    const int rows = nq * G, row0 = block * kRows;
-    if (row0 >= rows) return;
+    const int pair = blockIdx.x % pairs, item = blockIdx.x / pairs;
+    const int block = blocks - 1 - (SPLIT ? item / most_chunks : item), chunk = SPLIT ? item % most_chunks : 0;
+    const Block blk(a, pair, block, kRows);
+    if (blk.row0 >= blk.rows) return;
+    const int chunks = SPLIT ? chunks_of(blk.tiles, most_chunks) : 1;
+    if (SPLIT && chunk >= chunks) return;
+    // From here on keys and tiles are counted from the chunk's first.
+    const int from = SPLIT ? (int)((long)blk.tiles * chunk / chunks) : 0;
+    const int tiles = SPLIT ? (int)((long)blk.tiles * (chunk + 1) / chunks) - from : blk.tiles;
+    auto limit = [&](int row) { return min(max(blk.limit(row) - from * kKeys, 0), tiles * kKeys); };
+    const int k0 = blk.k0 + from * kKeys, nk = min(blk.nk - from * kKeys, tiles * kKeys), rows = blk.rows, G = blk.G;
 
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 32, half = lane / 32;
-    auto limit = [&](int row) { return min(max(row / G + 1 + nk - nq, 0), nk); };  // keys that a query row sees
-    const int tiles = (limit(min(row0 + kRows, rows) - 1) + kKeys - 1) / kKeys;
-    const int edge = limit(row0) / kKeys;  // first tile that some row of the workgroup does not see to its end
-    const int first = row0 + 32 * R * wave;
+    const int edge = limit(blk.row0) / kKeys;  // first tile that some row of the workgroup does not see to its end
+    const int first = blk.row0 + 32 * R * wave;
     const int all_see = __builtin_amdgcn_readfirstlane(limit(min(first, rows - 1)));  // keys that all rows of the wavefront see
 
     // ---- queries
@@ -85,74 +133,79 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
     for (int r = 0; r < R; ++r) {
         const int row = min(first + 32 * r + col, rows - 1), token = row / G;
         mine[r] = limit(row);
-        const uint16_t *from = a.q + (long)(q0 + token) * a.q_stride + (hk * G + row - token * G) * a.q_head + half * 8;
+        const uint16_t *src = a.q + (long)(blk.q0 + token) * a.q_stride + (blk.hk * G + row - token * G) * a.q_head + half * 8;
 #pragma unroll
         for (int st = 0; st < kSteps; ++st) {
-            u32x4 w = *reinterpret_cast<const u32x4 *>(from + st * 16);
+            u32x4 w = *reinterpret_cast<const u32x4 *>(src + st * 16);
             // The scale is positive from here on: the largest product is the largest score.
             if (a.scale < 0.f) w ^= 0x80008000u;
             q[r][st] = __builtin_bit_cast(bf16x8, w);
+            asm volatile("" : "+a"(q[r][st]));
         }
     }
 
     // ---- loads: wavefront w brings rows 8 w .. 8 w + 7 of each panel of a tile's keys, and 16 rows of panels of its values
     // a load.  Rows past the last key, and tiles past the last, become zeros.
-    const uint16_t *src_k = a.k + hk * a.k_head + k0 * a.k_stride, *src_v = a.v + hk * a.v_head + k0 * a.v_stride;
+    const uint16_t *src_k = a.k + blk.hk * a.k_head + k0 * a.k_stride, *src_v = a.v + blk.hk * a.v_head + k0 * a.v_stride;
     const uint32_t stride_k = (uint32_t)a.k_stride * 2, stride_v = (uint32_t)a.v_stride * 2;
     const int e = 8 * wave + lane / 8, place = (lane % 8) ^ (e >> 1 & 7);
-    const uint32_t off_k = e * stride_k + place * 16;
-    // Values: load n of wavefront w brings 16 rows (the upper ones for odd n) of a panel.
     const int v_panel = D == 128 ? wave : wave / 2, v_row = D == 128 ? 0 : wave % 2 * 16;
-    const uint32_t off_v = (v_row + lane / 4) * stride_v + v_panel * 64 + lane % 4 * 16, off_low = off_v + 16 * stride_v;
+    uint32_t off_k[KT], off_v[KT];
+#pragma unroll
+    for (int i = 0; i < KT; ++i) {
+        off_k[i] = (e + i * kKeys) * stride_k + place * 16;
+        off_v[i] = (v_row + i * kKeys + lane / 4) * stride_v + v_panel * 64 + lane % 4 * 16;
+    }
+    const uint32_t low = 16 * stride_v;  // the lower half of a panel of values, for heads of 128
     const uint32_t ring_k = __builtin_amdgcn_readfirstlane(lds_addr(lds.k) + wave * 1024);
     const uint32_t ring_v = __builtin_amdgcn_readfirstlane(lds_addr(lds.v) + v_panel * 2048 + v_row * 64);
-    int left_k = nk, left_v = nk;  // keys from the tile to load next on
+    int left_k = nk, left_v = nk;  // keys from the step to load next on
     uint32_t to_k = ring_k, to_v = ring_v;
     u32x4 key_src, value_src;
     auto aim_keys = [&] {
-        const int n = max(min(left_k, kKeys), 0);
+        const int n = max(min(left_k, KT * kKeys), 0);
         key_src = rsrc_words(src_k, n ? (uint32_t)(n - 1) * stride_k + D * 2 : 0);
     };
     auto aim_values = [&] {
-        const int n = max(min(left_v, kKeys), 0);
+        const int n = max(min(left_v, KT * kKeys), 0);
         value_src = rsrc_words(src_v, n ? (uint32_t)(n - 1) * stride_v + D * 2 : 0);
     };
     auto keys_done = [&] {
-        left_k -= kKeys;
-        if (left_k > 0) src_k += kKeys / 2 * stride_k;
-        to_k = to_k == ring_k + 3 * kTile ? ring_k : to_k + kTile;
+        left_k -= KT * kKeys;
+        if (left_k > 0) src_k += KT * kKeys / 2 * stride_k;
+        to_k = to_k == ring_k + (kHeld - KT) * kTile ? ring_k : to_k + KT * kTile;
     };
     auto values_done = [&] {
-        left_v -= kKeys;
-        if (left_v > 0) src_v += kKeys / 2 * stride_v;
-        to_v = to_v == ring_v + 3 * kTile ? ring_v : to_v + kTile;
+        left_v -= KT * kKeys;
+        if (left_v > 0) src_v += KT * kKeys / 2 * stride_v;
+        to_v = to_v == ring_v + (kHeld - KT) * kTile ? ring_v : to_v + KT * kTile;
     };
-    auto load = [&](int n) {
-        if (n < kPanels) load16_lds(key_src, off_k + n * 128, to_k + n * (kKeys * 128));
-        else if (n == kPanels) load16_lds(value_src, off_v, to_v);
-        else load16_lds(value_src, off_low, to_v + 1024);
+    auto load = [&](int i, int n) {  // load n of tile i of a step
+        if (n < kPanels) load16_lds(key_src, off_k[i] + n * 128, to_k + i * kTile + n * (kKeys * 128));
+        else if (n == kPanels) load16_lds(value_src, off_v[i], to_v + i * kTile);
+        else load16_lds(value_src, off_v[i] + low, to_v + i * kTile + 1024);
     };
     auto load_keys = [&] {
         aim_keys();
 #pragma unroll
-        for (int n = 0; n < kPanels; ++n) load(n);
+        for (int i = 0; i < KT * kPanels; ++i) load(i / kPanels, i % kPanels);
         keys_done();
     };
     auto load_values = [&] {
         aim_values();
 #pragma unroll
-        for (int n = kPanels; n < kLoads; ++n) load(n);
+        for (int i = 0; i < KT * kPanels; ++i) load(i / kPanels, kPanels + i % kPanels);
         values_done();
     };
 #pragma unroll 1
-    for (int t = 0; t < 3; ++t) load_keys();
+    for (int t = 0; t < KT + 2; t += KT) load_keys();
     load_values();
     // The values of tile -1, whose weights are zeros.
-    for (int i = threadIdx.x; i < kTile / 16; i += kPromptThreads) reinterpret_cast<u32x4 *>(lds.v[3])[i] = u32x4{0, 0, 0, 0};
+    for (int i = threadIdx.x; i < kTile / 16; i += kPromptThreads) reinterpret_cast<u32x4 *>(lds.v[kHeld - 1])[i] = u32x4{0, 0, 0, 0};
 
     f32x16 o[R][kTiles];
-    float m[R], l[R], down[R];
-    int scaled[R];
+    float m[R], l[R], base[R], down[R], bound[R];
+    int scaled = 0;
     u32x4 p0[R][2] = {}, p1[R][2];  // weights of the tile before and of this one, in turn: 16 keys each
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -160,13 +213,13 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
         for (int d = 0; d < kTiles; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[r][d][i] = 0.f;
-        m[r] = -INFINITY;
-        l[r] = 0.f;
+        m[r] = bound[r] = -INFINITY;
+        l[r] = base[r] = 0.f;
         down[r] = 1.f;
-        scaled[r] = 0;
     }
     uint32_t odd_tiles = 0;  // edge tiles with infinities or NaN among the values
     const float scale2 = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-126f);  // not zero: it meets infinities
+    const float slack = kSlack / scale2;
 
     uint32_t k_at[4];
 #pragma unroll
@@ -175,55 +228,65 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
     const uint32_t v_at = (uint32_t)((4 * half + i16 / 4) * 64 + lane / 16 % 2 * 32 + i16 % 4 * 8);
 
     // Piece c of the weights of row tile r with scores s.  Register i is key 8 (i / 4) + 4 half + i % 4.
-    float top[R], base[R], sum[R];
-    auto weights = [&](f32x16 &s, u32x4 (&p)[2], int r, int c) {
+    float top[R], sum[R];
+    auto weights = [&](f32x16 (&s)[R], u32x4 (&p)[R][2], int r, int c) {
+        f32x16 &x = s[r];
         if (c == 0) {
-            top[r] = max3(max3(max3(s[0], s[1], s[2]), max3(s[3], s[4], s[5]), s[6]),
-                          max3(max3(s[7], s[8], s[9]), max3(s[10], s[11], s[12]), s[13]), fmaxf(s[14], s[15]));
+            top[r] = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), x[6]);
         } else if (c == 1) {
-            top[r] = halves_max(top[r]) * scale2;
+            top[r] = max3(top[r], max3(max3(x[7], x[8], x[9]), max3(x[10], x[11], x[12]), x[13]), max2(x[14], x[15]));
         } else if (c == 2) {
-            int move = __any(top[r] > m[r] + kSlack);
-            scaled[r] = move & __any(m[r] != -INFINITY);
-            asm("" : "+v"(move));  // a select, not a branch
-            const float now = move ? fmaxf(m[r], top[r]) : m[r];
-            base[r] = now == -INFINITY ? 0.f : now;
-            down[r] = __builtin_amdgcn_exp2f((m[r] == -INFINITY ? base[r] : m[r]) - base[r]);
-            m[r] = now;
-            sum[r] = 0.f;
+            if (r < R - 1) return;
+            bool past = false;
+#pragma unroll
+            for (int i = 0; i < R; ++i) past |= top[i] > bound[i];
+            if (__builtin_expect(__any(past), 0)) {
+                // New reference maxima.  The output sums follow when the products under way are in them.
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    const float now = fmaxf(m[i], halves_max(top[i]) * scale2);
+                    scaled |= __any(m[i] != -INFINITY);
+                    base[i] = now == -INFINITY ? 0.f : now;
+                    down[i] = __builtin_amdgcn_exp2f((m[i] == -INFINITY ? base[i] : m[i]) - base[i]);
+                    l[i] *= down[i];
+                    m[i] = now;
+                    bound[i] = now == -INFINITY ? now : now / scale2 + slack;
+                }
+            }
         } else {
             const int e = c - 3;  // of 16 elements
             // Written out to stay here, where the compiler would sink it behind all products, and in this order: the result of
             // an exponential needs a wait state, which the instructions of the element before are.
             if (e < 16) {
-                const float x = fmaf(s[e], scale2, -base[r]);
-                asm volatile("v_exp_f32 %0, %1" : "=v"(s[e]) : "v"(x));
+                const float y = fmaf(x[e], scale2, -base[r]);
+                asm volatile("v_exp_f32 %0, %1" : "=v"(x[e]) : "v"(y));
             }
             // The element before: its sum, and pairs to bf16.
             if (e > 0 && e <= 16) {
                 const int i = e - 1;
-                asm volatile("v_add_f32 %0, %0, %1" : "+v"(sum[r]) : "v"(s[i]));
+                if (i == 1) asm volatile("v_add_f32 %0, %1, %2" : "=v"(sum[r]) : "v"(x[0]), "v"(x[1]));
+                if (i > 1) asm volatile("v_add_f32 %0, %0, %1" : "+v"(sum[r]) : "v"(x[i]));
                 if (i % 2) {
                     uint32_t w;
-                    asm volatile("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(w) : "v"(s[i - 1]), "v"(s[i]));
-                    p[i / 8][i % 8 / 2] = w;
+                    asm volatile("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(w) : "v"(x[i - 1]), "v"(x[i]));
+                    p[r][i / 8][i % 8 / 2] = w;
                 }
-                if (i == 15) l[r] = fmaf(l[r], down[r], sum[r]);
+                if (i == 15) asm volatile("v_add_f32 %0, %0, %1" : "+v"(l[r]) : "v"(sum[r]));
             }
         }
     };
     // Operand f of a tile: its keys' steps, then its values' (16 keys, element tile).  From kOperands on the next tile's.
-    uint32_t key_to = 0, value_to = 2 * kTile, key_at[4], value_at;
+    uint32_t key_to = 0, value_to = (kHeld - 2) * kTile, key_at[4], value_at;
     bf16x8 ring[kRing];
     auto fetch = [&](int f) {
         const int x = f % kOperands;
         if (x == 0) {
-            key_to = key_to == 3 * kTile ? 0 : key_to + kTile;
+            key_to = key_to == (kHeld - 1) * kTile ? 0 : key_to + kTile;
 #pragma unroll
             for (int i = 0; i < 4; ++i) key_at[i] = k_at[i] + key_to;
         }
         if (x == kSteps) {
-            value_to = value_to == 3 * kTile ? 0 : value_to + kTile;
+            value_to = value_to == (kHeld - 1) * kTile ? 0 : value_to + kTile;
             value_at = v_at + value_to;
         }
         if (x < kSteps) {
@@ -244,7 +307,7 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
                 __builtin_amdgcn_sched_barrier(0);
                 const int n = f - kSteps;
                 if (f == 0) mfma_first(s[r], ring[0], q[r][0]);
-                else if (f < kSteps) mfma_next(s[r], ring[f % kRing], q[r][f]);
+                else if (f < kSteps) mfma_next<R == 1>(s[r], ring[f % kRing], q[r][f]);
                 else o[r][n % kTiles] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                     ring[f % kRing], __builtin_bit_cast(bf16x8, p[r][n / kTiles]), o[r][n % kTiles], 0, 0, 0);
                 between(f * R + r);
@@ -253,17 +316,18 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
         __builtin_amdgcn_sched_barrier(0);
     };
 
-    // One tile: s its scores, p its weights, next the scores of the tile after, was the weights of the tile before.
-    auto tile = [&](int t, f32x16 (&s)[R], f32x16 (&next)[R], u32x4 (&p)[R][2], u32x4 (&was)[R][2]) {
-        // The keys of tile t + 2 and the values of tile t have landed; every wavefront is past the scores of tile t and the
-        // values of tile t - 2.
-        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLoads) : "memory");
+    // A step: tiles t .. t + KT - 1 follow.
+    auto begin = [&](int t) {
+        // The keys up to tile t + KT + 1 and the values up to tile t + KT - 1 have landed; every wavefront is past the scores of
+        // tile t and the values of tile t - 2.
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(KT * kLoads) : "memory");
         aim_keys();
         aim_values();
-        if (t >= edge && t < tiles) {
+#pragma unroll 1
+        for (int u = max(t, edge); u < min(t + KT, tiles); ++u) {
             // A weight of zero must not meet an infinity or NaN: where a tile that not all rows see to its end has one,
             // zeros take its place, and what it gives the rows that see it is added at the end.
-            u32x4 *all = reinterpret_cast<u32x4 *>(lds.v[t % 4]);
+            u32x4 *all = reinterpret_cast<u32x4 *>(lds.v[u % kHeld]);
             bool odd = false;
             for (int i = threadIdx.x; i < kTile / 16; i += kPromptThreads) {
                 u32x4 x = all[i];
@@ -277,16 +341,20 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
                 if (any) all[i] = x;
                 odd |= any;
             }
-            if (__syncthreads_or(odd)) odd_tiles |= 1u << (t - edge);
+            if (__syncthreads_or(odd)) odd_tiles |= 1u << (u - edge);
         }
+    };
+    // One tile, the i-th of its step: s its scores, p its weights, next the scores of the tile after, was the weights of the
+    // tile before.
+    auto tile = [&](int t, int i, f32x16 (&s)[R], f32x16 (&next)[R], u32x4 (&p)[R][2], u32x4 (&was)[R][2]) {
         // The sums so far, for the reference maximum that the weights of tile t - 1 have.
+        if (scaled) {
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (scaled[r]) {
+            for (int r = 0; r < R; ++r)
 #pragma unroll
                 for (int d = 0; d < kTiles; ++d) acc_scale(o[r][d], down[r]);
-                scaled[r] = 0;
-            }
+            scaled = 0;
+        }
         if ((t + 1) * kKeys > all_see) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
@@ -298,13 +366,14 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
         }
         products(next, was, [&](int c) {
 #pragma unroll
-            for (int j = c * kPieces / kProducts; j < (c + 1) * kPieces / kProducts; ++j) weights(s[j % R], p[j % R], j % R, j / R);
-            // The loads behind the last products but one, every other.
-            const int n = (c - (kProducts - 2 * kLoads)) / 2;
-            if (c >= kProducts - 2 * kLoads && (c - kProducts) % 2 == 0) load(n);
+            for (int j = c * kPieces / kProducts; j < (c + 1) * kPieces / kProducts; ++j) weights(s, p, j % R, j / R);
+            // The loads behind the last products, every other.
+            if (c >= kProducts - 2 * kLoads && (kProducts - c) % 2 == 0) load(i, (c - (kProducts - 2 * kLoads)) / 2);
         });
-        keys_done();
-        values_done();
+        if (i == KT - 1) {
+            keys_done();
+            values_done();
+        }
         if (odd_tiles >> max(t - edge, 0) & 1) {  // no bit is set before tile `edge`
 #pragma unroll
             for (int r = 0; r < R; ++r) {
@@ -329,19 +398,25 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
         const bf16x8 k = *reinterpret_cast<const bf16x8 *>(lds.k[0] + k_at[st % 4] + st / 4 * (kKeys * 128));
 #pragma unroll
         for (int r = 0; r < R; ++r) {
+            asm volatile("s_nop 1");  // behind the queries' way to their registers
             if (st == 0) mfma_first(s0[r], k, q[r][0]);
-            else mfma_next(s0[r], k, q[r][st]);
+            else mfma_next<true>(s0[r], k, q[r][st]);
         }
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s0[r]));
 #pragma unroll
     for (int f = 0; f < kAhead; ++f) fetch(f);
-    // Tiles 0 .. tiles: the last adds the values of the last but one.
+    // Tiles 0 .. tiles: the last adds the values of the last but one.  (With two a step perhaps one more, of zeros.)
 #pragma unroll 1
     for (int t = 0; t <= tiles; t += 2) {
-        tile(t, s0, s1, p1, p0);
-        if (t + 1 <= tiles) tile(t + 1, s1, s0, p0, p1);
+        begin(t);
+        tile(t, 0, s0, s1, p1, p0);
+        if (KT == 1) {
+            if (t == tiles) break;
+            begin(t + 1);
+        }
+        tile(t + 1, KT - 1, s1, s0, p0, p1);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing is on its way to LDS when the workgroup ends
 
@@ -349,57 +424,127 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
     for (int r = 0; r < R; ++r) {
         const int row = first + 32 * r + col;
         l[r] = halves_sum(l[r]);
+        const bool whole = !SPLIT || chunks == 1;
+        const float inv = !whole ? 1.f : l[r] == 0.f ? 0.f : 1.f / l[r];
+        const long slot = ((long)pair * blocks + block) * most_chunks + chunk;
         if (row >= rows) continue;
-        const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
-        const long at = (long)(q0 + row / G) * a.H + hk * G + row % G;
+        const long at = (long)(blk.q0 + row / G) * a.H + blk.hk * G + row % G;
 #pragma unroll
         for (int d = 0; d < kTiles; ++d)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *reinterpret_cast<u32x2 *>(a.o + at * D + 32 * d + 8 * i + 4 * half) =
-                    u32x2{pack_bf16x2(o[r][d][4 * i] * inv, o[r][d][4 * i + 1] * inv),
-                          pack_bf16x2(o[r][d][4 * i + 2] * inv, o[r][d][4 * i + 3] * inv)};
-        if (a.lse && half == 0) a.lse[at] = l[r] == 0.f ? -INFINITY : (m[r] + __builtin_amdgcn_logf(l[r])) / kLog2e;
-        if (!odd_tiles) continue;
-        for (int n = 0; n < D / 2; ++n) {  // the lane's own elements, as above
-            const int el = n / 16 * 32 + n % 16 / 4 * 8 + 4 * half + n % 4;
-            float c = 0.f;
-            for (int x = 0; x < kEdge; ++x) {
-                if (!(odd_tiles >> x & 1)) continue;
-                const int from = (edge + x) * kKeys;
-                for (int j = 0; j < min(mine[r] - from, kKeys); ++j) {
-                    const uint16_t w = a.v[hk * a.v_head + (long)(k0 + from + j) * a.v_stride + el];
-                    if (!not_finite(w)) continue;
-                    const uint32_t is = lds.some[x][r][wave * kWave + j / 4 % 2 * 32 + col] >> (j / 8 * 4 + j % 4) & 1;
-                    c = fmaf(is ? 1.f : 0.f, bf16_bits_to_f32(w), c);
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 x = {o[r][d][4 * i] * inv, o[r][d][4 * i + 1] * inv, o[r][d][4 * i + 2] * inv, o[r][d][4 * i + 3] * inv};
+                if (whole)
+                    *reinterpret_cast<u32x2 *>(a.o + at * D + 32 * d + 8 * i + 4 * half) =
+                        u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+                else
+                    reinterpret_cast<f32x4 *>(parts.o)[(((slot * kPromptWaves + wave) * kTiles + d) * 4 + i) * kWave + lane] = x;
+            }
+        if (odd_tiles) {
+            for (int n = 0; n < D / 2; ++n) {  // the lane's own elements, as above
+                const int el = n / 16 * 32 + n % 16 / 4 * 8 + 4 * half + n % 4;
+                float c = 0.f;
+                for (int b = 0; b < kEdge; ++b) {
+                    if (!(odd_tiles >> b & 1)) continue;
+                    const int begin = (edge + b) * kKeys;
+                    for (int j = 0; j < min(mine[r] - begin, kKeys); ++j) {
+                        const uint16_t w = a.v[blk.hk * a.v_head + (long)(k0 + begin + j) * a.v_stride + el];
+                        if (!not_finite(w)) continue;
+                        const uint32_t is = lds.some[b][r][wave * kWave + j / 4 % 2 * 32 + col] >> (j / 8 * 4 + j % 4) & 1;
+                        c = fmaf(is ? 1.f : 0.f, bf16_bits_to_f32(w), c);
+                    }
+                }
+                if (c == 0.f) continue;
+                if (whole) {
+                    uint16_t *to = a.o + at * D + el;
+                    *to = f32_to_bf16_bits(bf16_bits_to_f32(*to) + c);
+                } else {
+                    parts.o[((((slot * kPromptWaves + wave) * kTiles + n / 16) * 4 + n % 16 / 4) * kWave + lane) * 4 + n % 4] += c;
                 }
             }
-            if (c == 0.f) continue;
-            uint16_t *to = a.o + at * D + el;
-            *to = f32_to_bf16_bits(bf16_bits_to_f32(*to) + c);
         }
+        if (half) continue;
+        if (!whole) parts.ml[slot * kSplitRows + wave * 32 + col] = float2{m[r], l[r]};
+        else if (a.lse) a.lse[at] = l[r] == 0.f ? -INFINITY : (m[r] + __builtin_amdgcn_logf(l[r])) / kLog2e;
     }
 }
 
-template <int D, int R>
-void launch(const GroupedPromptArgs &a, hipStream_t stream)
+// Adds up the chunks of a row block: a workgroup has 32 rows, a lane of a wavefront the four elements that registers 4 i .. of
+// that lane of the accumulators hold.
+template <int D>
+__global__ __launch_bounds__(kPromptThreads) void join_prompt_kernel(GroupedPromptArgs a, int blocks, int most_chunks, PromptParts parts)
 {
-    const int blocks = (int)(((long)a.max_tokens * (a.H / a.Hkv) + 128 * R - 1) / (128 * R));
-    prompt_kernel<D, R><<<(unsigned)(a.B * a.Hkv * blocks), kPromptThreads, 0, stream>>>(a, blocks);
+    constexpr int kTiles = D / 32;
+    const int of = blockIdx.x % kPromptWaves, pb = blockIdx.x / kPromptWaves, pair = pb / blocks;
+    const Block blk(a, pair, pb % blocks, kSplitRows);
+    const int chunks = chunks_of(blk.tiles, most_chunks), lane = lane_id(), i = threadIdx.x / kWave;
+    const int row = blk.row0 + of * 32 + lane % 32;
+    if (chunks == 1 || row >= blk.rows) return;
+    const float2 *ml = parts.ml + (long)pb * most_chunks * kSplitRows + of * 32 + lane % 32;
+    float top = -INFINITY;
+#pragma unroll 8
+    for (int c = 0; c < chunks; ++c) top = fmaxf(top, ml[c * kSplitRows].x);
+    const float base = top == -INFINITY ? 0.f : top;
+    float total = 0.f;
+    f32x4 sum[kTiles] = {};
+    const f32x4 *o = reinterpret_cast<const f32x4 *>(parts.o) + (((long)pb * most_chunks * kPromptWaves + of) * kTiles * 4 + i) * kWave + lane;
+#pragma unroll 4
+    for (int c = 0; c < chunks; ++c) {
+        const float2 part = ml[c * kSplitRows];
+        const float f = __builtin_amdgcn_exp2f(part.x - base);
+        total = fmaf(part.y, f, total);
+#pragma unroll
+        for (int d = 0; d < kTiles; ++d) {
+            const f32x4 v = o[((long)c * kPromptWaves * kTiles + d) * 4 * kWave];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) sum[d][n] = fmaf(v[n], f, sum[d][n]);
+        }
+    }
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    const long at = (long)(blk.q0 + row / blk.G) * a.H + blk.hk * blk.G + row % blk.G;
+#pragma unroll
+    for (int d = 0; d < kTiles; ++d)
+        *reinterpret_cast<u32x2 *>(a.o + at * D + 32 * d + 8 * i + lane / 32 * 4) =
+            u32x2{pack_bf16x2(sum[d][0] * inv, sum[d][1] * inv), pack_bf16x2(sum[d][2] * inv, sum[d][3] * inv)};
+    if (a.lse && i == 0 && lane < 32) a.lse[at] = total == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(total)) / kLog2e;
+}
+
+#ifndef ECOSPEC_GP_R
+#define ECOSPEC_GP_R 1
+#endif
+#ifndef ECOSPEC_GP_KT
+#define ECOSPEC_GP_KT 1
+#endif
+
+template <int D>
+hipError_t launch(const GroupedPromptArgs &a, void *workspace, hipStream_t stream)
+{
+    const long rows = (long)a.max_tokens * (a.H / a.Hkv);
+    const int pairs = a.B * a.Hkv, few = (int)((rows + kSplitRows - 1) / kSplitRows);
+    char *w = static_cast<char *>(workspace);
+    const PromptParts parts{reinterpret_cast<float2 *>(w), reinterpret_cast<float *>(w + kSlots * kSplitRows * sizeof(float2))};
+    const long room = kSlots / ((long)pairs * few), cut = (a.M + kKeys - 1) / kKeys / kMinTiles;
+    const int chunks = (int)(room < cut ? room : cut);
+    if (chunks > 1) {
+        prompt_kernel<D, 1, 1, true><<<(unsigned)(pairs * few * chunks), kPromptThreads, 0, stream>>>(a, few, chunks, parts);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        join_prompt_kernel<D><<<(unsigned)(pairs * few * kPromptWaves), kPromptThreads, 0, stream>>>(a, few, chunks, parts);
+        return hipGetLastError();
+    }
+    constexpr int R = ECOSPEC_GP_R, KT = ECOSPEC_GP_KT;
+    const int blocks = (int)((rows + 128 * R - 1) / (128 * R));
+    prompt_kernel<D, R, KT, false><<<(unsigned)((long)pairs * blocks), kPromptThreads, 0, stream>>>(a, blocks, 1, parts);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-size_t grouped_prompt_workspace(int D) { return 256; }
+size_t grouped_prompt_workspace(int D) { return (size_t)kSlots * kSplitRows * (sizeof(float2) + D * sizeof(float)); }
 
 hipError_t launch_grouped_prompt(const GroupedPromptArgs &a, int D, void *workspace, hipStream_t stream)
 {
-#ifndef ECOSPEC_GP_R
-#define ECOSPEC_GP_R 1
-#endif
-    if (D == 64) launch<64, ECOSPEC_GP_R>(a, stream);
-    else launch<128, ECOSPEC_GP_R>(a, stream);
-    return hipGetLastError();
+    return D == 64 ? launch<64>(a, workspace, stream) : launch<128>(a, workspace, stream);
 }
 
 }  // namespace ecospec
