@@ -1,7 +1,7 @@
 // Attention of whole prompts with grouped heads: causal, sequences of different lengths side by side.
 //
 // The query rows of a sequence that read the same keys are its tokens times the heads of one key/value head, token by
-// token: a workgroup takes consecutive ones, 32 R of each of four wavefronts.  So short sequences fill its rows too, and
+// token: a workgroup takes consecutive ones, 32 R of each of W wavefronts.  So short sequences fill its rows too, and
 // long ones have few keys that only some of the rows see.
 //   Scores are transposed (S^T = K Q^T): a lane holds one row, its scores are the value product's operand as they stand
 //   (O^T = V^T P^T), and V^T is read with the transposing LDS load.
@@ -19,8 +19,8 @@
 namespace ecospec {
 namespace {
 
-constexpr int kKeys = 32, kPromptWaves = 4, kPromptThreads = kPromptWaves * kWave;
-constexpr int kSplitRows = 32 * kPromptWaves;  // rows of a workgroup where keys are cut
+constexpr int kKeys = 32, kSplitWaves = 4;
+constexpr int kSplitRows = 32 * kSplitWaves;   // rows of a workgroup where keys are cut
 constexpr int kSlots = 2 * kCus;               // workgroups of such a call
 constexpr int kMinTiles = 4;                   // of a chunk
 constexpr float kSlack = 8.f;  // powers of two that weights may pass 1 by before their reference maximum moves
@@ -85,24 +85,29 @@ struct PromptParts {
     float *o;    // [slot][wavefront][D / 32][4][lane][4]
 };
 
-// D: width of a head; R: row tiles of a wavefront; KT: key tiles a barrier; SPLIT: keys are cut into chunks.
-template <int D, int R, int KT, bool SPLIT>
-__global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(GroupedPromptArgs a, int blocks, int most_chunks,
+#ifndef ECOSPEC_GP_OCC
+#define ECOSPEC_GP_OCC 3
+#endif
+// D: width of a head; W: wavefronts; R: row tiles of each; KT: key tiles a barrier; SPLIT: keys are cut into chunks.
+template <int D, int W, int R, int KT, bool SPLIT>
+__global__ __launch_bounds__(W * kWave, D == 64 ? ECOSPEC_GP_OCC : R == 1 ? 2 : 1) void prompt_kernel(GroupedPromptArgs a, int blocks, int most_chunks,
                                                                                 PromptParts parts)
 {
-    constexpr int kRows = 32 * R * kPromptWaves, kSteps = D / 16, kPanels = D / 64, kTiles = D / 32;
+    constexpr int kThreads = W * kWave, kRows = 32 * R * W, kSteps = D / 16, kPanels = D / 64, kTiles = D / 32;
     constexpr int kTile = kKeys * D * 2, kLoads = 2 * kPanels;  // bytes of a tile; loads of a tile by a wavefront
     constexpr int kEdge = kRows / kKeys + 1;                    // most tiles that some rows of a workgroup see in part
     constexpr int kOperands = kSteps + 2 * kTiles;              // key and value operands of a tile
     constexpr int kRing = 8, kAhead = kRing - 1;                // of them in registers
     constexpr int kHeld = 4 * KT;                               // tiles of keys, and of values, in LDS
+    constexpr int kBrings = KT * 4 / W;                         // tiles of a step that a wavefront loads a quarter of
+    static_assert(kBrings * W == KT * 4, "every quarter is loaded");
     static_assert(kOperands % kRing == 0, "a tile's first operand has a fixed place");
-    static_assert(!SPLIT || kRows == kSplitRows, "parts");
+    static_assert(!SPLIT || (R == 1 && W == kSplitWaves), "parts");
     constexpr int kProducts = kOperands * R, kPieces = 20 * R;  // of a tile
     struct Tiles {
         char k[kHeld][kTile];  // panel, row r, chunk c of 16 bytes at place c ^ (r >> 1 & 7)
         char v[kHeld][kTile];  // panel of 32 elements, row
-        uint16_t some[kEdge][R][kPromptThreads];  // which weights of a lane are not zero, in a tile with infinities or NaN
+        uint16_t some[kEdge][R][kThreads];  // which weights of a lane are not zero, in a tile with infinities or NaN
     };
     __shared__ __attribute__((aligned(16))) Tiles lds;
 
@@ -144,21 +149,22 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
         }
     }
 
-    // ---- loads: wavefront w brings rows 8 w .. 8 w + 7 of each panel of a tile's keys, and 16 rows of panels of its values
-    // a load.  Rows past the last key, and tiles past the last, become zeros.
+    // ---- loads: four wavefronts bring a tile, the w-th of them rows 8 w .. 8 w + 7 of each panel of its keys, and 16 rows of
+    // panels of its values a load.  Rows past the last key, and tiles past the last, become zeros.
     const uint16_t *src_k = a.k + blk.hk * a.k_head + k0 * a.k_stride, *src_v = a.v + blk.hk * a.v_head + k0 * a.v_stride;
     const uint32_t stride_k = (uint32_t)a.k_stride * 2, stride_v = (uint32_t)a.v_stride * 2;
-    const int e = 8 * wave + lane / 8, place = (lane % 8) ^ (e >> 1 & 7);
-    const int v_panel = D == 128 ? wave : wave / 2, v_row = D == 128 ? 0 : wave % 2 * 16;
-    uint32_t off_k[KT], off_v[KT];
+    const int w4 = wave % 4, mine0 = wave / 4;  // its quarter, and its first tile of a step
+    const int e = 8 * w4 + lane / 8, place = (lane % 8) ^ (e >> 1 & 7);
+    const int v_panel = D == 128 ? w4 : w4 / 2, v_row = D == 128 ? 0 : w4 % 2 * 16;
+    uint32_t off_k[kBrings], off_v[kBrings];
 #pragma unroll
-    for (int i = 0; i < KT; ++i) {
-        off_k[i] = (e + i * kKeys) * stride_k + place * 16;
-        off_v[i] = (v_row + i * kKeys + lane / 4) * stride_v + v_panel * 64 + lane % 4 * 16;
+    for (int i = 0; i < kBrings; ++i) {
+        off_k[i] = (e + (mine0 + i) * kKeys) * stride_k + place * 16;
+        off_v[i] = (v_row + (mine0 + i) * kKeys + lane / 4) * stride_v + v_panel * 64 + lane % 4 * 16;
     }
     const uint32_t low = 16 * stride_v;  // the lower half of a panel of values, for heads of 128
-    const uint32_t ring_k = __builtin_amdgcn_readfirstlane(lds_addr(lds.k) + wave * 1024);
-    const uint32_t ring_v = __builtin_amdgcn_readfirstlane(lds_addr(lds.v) + v_panel * 2048 + v_row * 64);
+    const uint32_t ring_k = __builtin_amdgcn_readfirstlane(lds_addr(lds.k) + mine0 * kTile + w4 * 1024);
+    const uint32_t ring_v = __builtin_amdgcn_readfirstlane(lds_addr(lds.v) + mine0 * kTile + v_panel * 2048 + v_row * 64);
     int left_k = nk, left_v = nk;  // keys from the step to load next on
     uint32_t to_k = ring_k, to_v = ring_v;
     u32x4 key_src, value_src;
@@ -180,7 +186,7 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
         if (left_v > 0) src_v += KT * kKeys / 2 * stride_v;
         to_v = to_v == ring_v + (kHeld - KT) * kTile ? ring_v : to_v + KT * kTile;
     };
-    auto load = [&](int i, int n) {  // load n of tile i of a step
+    auto load = [&](int i, int n) {  // load n of the i-th of its tiles
         if (n < kPanels) load16_lds(key_src, off_k[i] + n * 128, to_k + i * kTile + n * (kKeys * 128));
         else if (n == kPanels) load16_lds(value_src, off_v[i], to_v + i * kTile);
         else load16_lds(value_src, off_v[i] + low, to_v + i * kTile + 1024);
@@ -188,20 +194,20 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
     auto load_keys = [&] {
         aim_keys();
 #pragma unroll
-        for (int i = 0; i < KT * kPanels; ++i) load(i / kPanels, i % kPanels);
+        for (int i = 0; i < kBrings * kPanels; ++i) load(i / kPanels, i % kPanels);
         keys_done();
     };
     auto load_values = [&] {
         aim_values();
 #pragma unroll
-        for (int i = 0; i < KT * kPanels; ++i) load(i / kPanels, kPanels + i % kPanels);
+        for (int i = 0; i < kBrings * kPanels; ++i) load(i / kPanels, kPanels + i % kPanels);
         values_done();
     };
 #pragma unroll 1
     for (int t = 0; t < KT + 2; t += KT) load_keys();
     load_values();
     // The values of tile -1, whose weights are zeros.
-    for (int i = threadIdx.x; i < kTile / 16; i += kPromptThreads) reinterpret_cast<u32x4 *>(lds.v[kHeld - 1])[i] = u32x4{0, 0, 0, 0};
+    for (int i = threadIdx.x; i < kTile / 16; i += kThreads) reinterpret_cast<u32x4 *>(lds.v[kHeld - 1])[i] = u32x4{0, 0, 0, 0};
 
     f32x16 o[R][kTiles];
     float m[R], l[R], base[R], down[R], bound[R];
@@ -281,12 +287,12 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
     auto fetch = [&](int f) {
         const int x = f % kOperands;
         if (x == 0) {
-            key_to = key_to == (kHeld - 1) * kTile ? 0 : key_to + kTile;
+            key_to = (key_to + kTile) % (kHeld * kTile);
 #pragma unroll
             for (int i = 0; i < 4; ++i) key_at[i] = k_at[i] + key_to;
         }
         if (x == kSteps) {
-            value_to = value_to == (kHeld - 1) * kTile ? 0 : value_to + kTile;
+            value_to = (value_to + kTile) % (kHeld * kTile);
             value_at = v_at + value_to;
         }
         if (x < kSteps) {
@@ -307,7 +313,7 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
                 __builtin_amdgcn_sched_barrier(0);
                 const int n = f - kSteps;
                 if (f == 0) mfma_first(s[r], ring[0], q[r][0]);
-                else if (f < kSteps) mfma_next<R == 1>(s[r], ring[f % kRing], q[r][f]);
+                else if (f < kSteps) mfma_next<false>(s[r], ring[f % kRing], q[r][f]);
                 else o[r][n % kTiles] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                     ring[f % kRing], __builtin_bit_cast(bf16x8, p[r][n / kTiles]), o[r][n % kTiles], 0, 0, 0);
                 between(f * R + r);
@@ -320,7 +326,7 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
     auto begin = [&](int t) {
         // The keys up to tile t + KT + 1 and the values up to tile t + KT - 1 have landed; every wavefront is past the scores of
         // tile t and the values of tile t - 2.
-        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(KT * kLoads) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kBrings * kLoads) : "memory");
         aim_keys();
         aim_values();
 #pragma unroll 1
@@ -329,7 +335,7 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
             // zeros take its place, and what it gives the rows that see it is added at the end.
             u32x4 *all = reinterpret_cast<u32x4 *>(lds.v[u % kHeld]);
             bool odd = false;
-            for (int i = threadIdx.x; i < kTile / 16; i += kPromptThreads) {
+            for (int i = threadIdx.x; i < kTile / 16; i += kThreads) {
                 u32x4 x = all[i];
                 bool any = false;
 #pragma unroll
@@ -368,7 +374,7 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
 #pragma unroll
             for (int j = c * kPieces / kProducts; j < (c + 1) * kPieces / kProducts; ++j) weights(s, p, j % R, j / R);
             // The loads behind the last products, every other.
-            if (c >= kProducts - 2 * kLoads && (kProducts - c) % 2 == 0) load(i, (c - (kProducts - 2 * kLoads)) / 2);
+            if (i < kBrings && c >= kProducts - 2 * kLoads && (kProducts - c) % 2 == 0) load(i, (c - (kProducts - 2 * kLoads)) / 2);
         });
         if (i == KT - 1) {
             keys_done();
@@ -438,7 +444,7 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
                     *reinterpret_cast<u32x2 *>(a.o + at * D + 32 * d + 8 * i + 4 * half) =
                         u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
                 else
-                    reinterpret_cast<f32x4 *>(parts.o)[(((slot * kPromptWaves + wave) * kTiles + d) * 4 + i) * kWave + lane] = x;
+                    reinterpret_cast<f32x4 *>(parts.o)[(((slot * W + wave) * kTiles + d) * 4 + i) * kWave + lane] = x;
             }
         if (odd_tiles) {
             for (int n = 0; n < D / 2; ++n) {  // the lane's own elements, as above
@@ -459,7 +465,7 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
                     uint16_t *to = a.o + at * D + el;
                     *to = f32_to_bf16_bits(bf16_bits_to_f32(*to) + c);
                 } else {
-                    parts.o[((((slot * kPromptWaves + wave) * kTiles + n / 16) * 4 + n % 16 / 4) * kWave + lane) * 4 + n % 4] += c;
+                    parts.o[((((slot * W + wave) * kTiles + n / 16) * 4 + n % 16 / 4) * kWave + lane) * 4 + n % 4] += c;
                 }
             }
         }
@@ -472,10 +478,10 @@ __global__ __launch_bounds__(kPromptThreads, R == 1 ? 2 : 1) void prompt_kernel(
 // Adds up the chunks of a row block: a workgroup has 32 rows, a lane of a wavefront the four elements that registers 4 i .. of
 // that lane of the accumulators hold.
 template <int D>
-__global__ __launch_bounds__(kPromptThreads) void join_prompt_kernel(GroupedPromptArgs a, int blocks, int most_chunks, PromptParts parts)
+__global__ __launch_bounds__(4 * kWave) void join_prompt_kernel(GroupedPromptArgs a, int blocks, int most_chunks, PromptParts parts)
 {
     constexpr int kTiles = D / 32;
-    const int of = blockIdx.x % kPromptWaves, pb = blockIdx.x / kPromptWaves, pair = pb / blocks;
+    const int of = blockIdx.x % kSplitWaves, pb = blockIdx.x / kSplitWaves, pair = pb / blocks;
     const Block blk(a, pair, pb % blocks, kSplitRows);
     const int chunks = chunks_of(blk.tiles, most_chunks), lane = lane_id(), i = threadIdx.x / kWave;
     const int row = blk.row0 + of * 32 + lane % 32;
@@ -487,7 +493,7 @@ __global__ __launch_bounds__(kPromptThreads) void join_prompt_kernel(GroupedProm
     const float base = top == -INFINITY ? 0.f : top;
     float total = 0.f;
     f32x4 sum[kTiles] = {};
-    const f32x4 *o = reinterpret_cast<const f32x4 *>(parts.o) + (((long)pb * most_chunks * kPromptWaves + of) * kTiles * 4 + i) * kWave + lane;
+    const f32x4 *o = reinterpret_cast<const f32x4 *>(parts.o) + (((long)pb * most_chunks * kSplitWaves + of) * kTiles * 4 + i) * kWave + lane;
 #pragma unroll 4
     for (int c = 0; c < chunks; ++c) {
         const float2 part = ml[c * kSplitRows];
@@ -495,7 +501,7 @@ __global__ __launch_bounds__(kPromptThreads) void join_prompt_kernel(GroupedProm
         total = fmaf(part.y, f, total);
 #pragma unroll
         for (int d = 0; d < kTiles; ++d) {
-            const f32x4 v = o[((long)c * kPromptWaves * kTiles + d) * 4 * kWave];
+            const f32x4 v = o[((long)c * kSplitWaves * kTiles + d) * 4 * kWave];
 #pragma unroll
             for (int n = 0; n < 4; ++n) sum[d][n] = fmaf(v[n], f, sum[d][n]);
         }
@@ -512,6 +518,9 @@ __global__ __launch_bounds__(kPromptThreads) void join_prompt_kernel(GroupedProm
 #ifndef ECOSPEC_GP_R
 #define ECOSPEC_GP_R 1
 #endif
+#ifndef ECOSPEC_GP_W
+#define ECOSPEC_GP_W 4
+#endif
 #ifndef ECOSPEC_GP_KT
 #define ECOSPEC_GP_KT 1
 #endif
@@ -526,15 +535,15 @@ hipError_t launch(const GroupedPromptArgs &a, void *workspace, hipStream_t strea
     const long room = kSlots / ((long)pairs * few), cut = (a.M + kKeys - 1) / kKeys / kMinTiles;
     const int chunks = (int)(room < cut ? room : cut);
     if (chunks > 1) {
-        prompt_kernel<D, 1, 1, true><<<(unsigned)(pairs * few * chunks), kPromptThreads, 0, stream>>>(a, few, chunks, parts);
+        prompt_kernel<D, kSplitWaves, 1, 1, true><<<(unsigned)(pairs * few * chunks), kSplitWaves * kWave, 0, stream>>>(a, few, chunks, parts);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        join_prompt_kernel<D><<<(unsigned)(pairs * few * kPromptWaves), kPromptThreads, 0, stream>>>(a, few, chunks, parts);
+        join_prompt_kernel<D><<<(unsigned)(pairs * few * kSplitWaves), 4 * kWave, 0, stream>>>(a, few, chunks, parts);
         return hipGetLastError();
     }
-    constexpr int R = ECOSPEC_GP_R, KT = ECOSPEC_GP_KT;
-    const int blocks = (int)((rows + 128 * R - 1) / (128 * R));
-    prompt_kernel<D, R, KT, false><<<(unsigned)((long)pairs * blocks), kPromptThreads, 0, stream>>>(a, blocks, 1, parts);
+    constexpr int W = ECOSPEC_GP_W, R = ECOSPEC_GP_R, KT = ECOSPEC_GP_KT;
+    const int blocks = (int)((rows + 32 * R * W - 1) / (32 * R * W));
+    prompt_kernel<D, W, R, KT, false><<<(unsigned)((long)pairs * blocks), W * kWave, 0, stream>>>(a, blocks, 1, parts);
     return hipGetLastError();
 }
 
