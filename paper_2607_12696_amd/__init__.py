@@ -37,6 +37,7 @@ and the two ends of a decoding step:
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 import threading
 from dataclasses import dataclass
@@ -578,16 +579,24 @@ def moe_add_rmsnorm(x, weight, eps: float, residual=None, qfmt: int = MOE_Q_NONE
 
 # --------------------------------------------------------------------------- attention
 
+# One function to a check: with ten tensors a call, the calls between them were a third of its host time.
+
+def _typed_ptr(t, dtype, what: str, shape) -> int:
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{what} must be {str(dtype).removeprefix('torch.')} {list(shape)}")
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a device tensor")
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    return t.data_ptr()
+
+
 def _int32_ptr(t, what: str, *shape) -> int:
-    if t.dtype != _torch().int32 or t.shape != shape:
-        raise ValueError(f"{what} must be int32 {list(shape)}")
-    return _dev_ptr(t, what)
+    return _typed_ptr(t, _torch().int32, what, shape)
 
 
 def _bf16_ptr(t, what: str, *shape) -> int:
-    if t.dtype != _torch().bfloat16 or t.shape != shape:
-        raise ValueError(f"{what} must be bfloat16 {list(shape)}")
-    return _dev_ptr(t, what)
+    return _typed_ptr(t, _torch().bfloat16, what, shape)
 
 
 def _drafts(N: int, token_offsets, mask) -> moe_drafts_t:
@@ -755,21 +764,21 @@ def moe_pages_update(cache_len, token_offsets, block_table, free_pages, n_free, 
     are updated in place.  N: entries of slots and positions, at least the new tokens.  The counts are not changed: the new
     ones are new_len and n_free of the result, whose tensors are those of `out` where it is given."""
     torch = _torch()
+    i32, ptr = torch.int32, _typed_ptr
     B, blocks = block_table.shape
     n_pages, dev = free_pages.shape[0], block_table.device
     if out is None:
-        ints = torch.empty(B + 2 + N, dtype=torch.int32, device=dev).split((B, 1, 1, N))
-        out = PageUpdate(*ints[:3], torch.empty(N, dtype=torch.int64, device=dev), ints[3])
-    if out.slots.dtype != torch.int64 or out.slots.shape != (N,):
-        raise ValueError("slots must be int64 [N]")
-    pool = moe_page_pool_t(B, n_pages, page, blocks, _int32_ptr(block_table, "block_table", B, blocks),
-                           _int32_ptr(cache_len, "cache_len", B), _int32_ptr(free_pages, "free_pages", n_pages),
-                           _int32_ptr(n_free, "n_free", 1))
+        ints = torch.empty(B + 2 + N, dtype=i32, device=dev).split_with_sizes((B, 1, 1, N))
+        out = PageUpdate(ints[0], ints[1], ints[2], torch.empty(N, dtype=torch.int64, device=dev), ints[3])
+    per, one, tokens = (B,), (1,), (N,)
+    pool = moe_page_pool_t(B, n_pages, page, blocks, ptr(block_table, i32, "block_table", (B, blocks)),
+                           ptr(cache_len, i32, "cache_len", per), ptr(free_pages, i32, "free_pages", (n_pages,)),
+                           ptr(n_free, i32, "n_free", one))
     _check("moe_pages_update", lib().moe_pages_update(
-        C.byref(pool), None if keep_len is None else _int32_ptr(keep_len, "keep_len", B),
-        _int32_ptr(token_offsets, "token_offsets", B + 1), N, _int32_ptr(out.new_len, "new_len", B),
-        _int32_ptr(out.n_free, "n_free", 1), _int32_ptr(out.refused, "refused", 1), _dev_ptr(out.slots, "slots"),
-        _int32_ptr(out.positions, "positions", N), _stream(block_table)))
+        C.byref(pool), None if keep_len is None else ptr(keep_len, i32, "keep_len", per),
+        ptr(token_offsets, i32, "token_offsets", (B + 1,)), N, ptr(out.new_len, i32, "new_len", per),
+        ptr(out.n_free, i32, "n_free", one), ptr(out.refused, i32, "refused", one), ptr(out.slots, torch.int64, "slots", tokens),
+        ptr(out.positions, i32, "positions", tokens), _stream(block_table)))
     return out
 
 
@@ -780,14 +789,15 @@ def moe_latent_append(kv_new, pages, slots, rows=None) -> None:
     torch = _torch()
     n_pages, page, width = pages.shape
     n_rows = kv_new.shape[0]
-    N = slots.shape[0]
-    if slots.dtype != torch.int64 or slots.dim() != 1:
-        raise ValueError("slots must be int64 [N]")
+    N, = slots.shape
     _check("moe_latent_append", lib().moe_latent_append(
-        _bf16_ptr(pages, "pages", n_pages, page, width), n_pages, page, width - 64, 64, _bf16_ptr(kv_new, "kv_new", n_rows, width),
-        n_rows, None if rows is None else _int32_ptr(rows, "rows", N), N, _dev_ptr(slots, "slots"), _stream(pages)))
+        _typed_ptr(pages, torch.bfloat16, "pages", (n_pages, page, width)), n_pages, page, width - 64, 64,
+        _typed_ptr(kv_new, torch.bfloat16, "kv_new", (n_rows, width)), n_rows,
+        None if rows is None else _typed_ptr(rows, torch.int32, "rows", (N,)), N, _typed_ptr(slots, torch.int64, "slots", (N,)),
+        _stream(pages)))
 
 
+@functools.cache
 def moe_grouped_prompt_workspace_size(D: int) -> int:
     n = C.c_size_t()
     _check("moe_grouped_prompt_workspace_size", lib().moe_grouped_prompt_workspace_size(D, C.byref(n)))
@@ -830,6 +840,7 @@ class TokenLogprobs:
     top_logprob: object  # fp32 [N, k]
 
 
+@functools.lru_cache(256)
 def moe_token_logprobs_workspace_size(N: int) -> int:
     n = C.c_size_t()
     _check("moe_token_logprobs_workspace_size", lib().moe_token_logprobs_workspace_size(N, C.byref(n)))
@@ -844,37 +855,38 @@ def moe_token_logprobs(logits, tokens=None, k: int = 0, scale: float = 1.0, out:
     (-inf), or None; k: alternatives, largest logit first, equal ones by lower index; scale: the inverse temperature.
     out: tensors to write to (those that are None are not computed, but for what tokens and k ask for)."""
     torch = _torch()
+    f32, i32, ptr = torch.float32, torch.int32, _typed_ptr
     if logits.dim() != 2 or logits.stride(1) != 1 and logits.shape[1] != 1:
         raise ValueError("logits must be [N, V], contiguous along V")
     N, V = logits.shape
-    if not logits.is_cuda or logits.dtype not in (torch.bfloat16, torch.float32):
+    dtype, dev, stride = logits.dtype, logits.device, logits.stride(0)
+    if not logits.is_cuda or dtype is not torch.bfloat16 and dtype is not f32:
         raise ValueError("logits must be bfloat16 or float32, on the device")
-    M = 0
+    if N == 1:
+        stride = max(stride, V)
+    M, shape = 0, None
     if tokens is not None:
-        if tokens.dim() not in (1, 2) or tokens.shape[0] != N:
+        shape = tokens.shape
+        if len(shape) not in (1, 2) or shape[0] != N:
             raise ValueError("tokens must be int32 [N] or [N, M]")
-        M = tokens.numel() // max(N, 1)
-        if not M:
-            tokens = None
-    dev, f32 = logits.device, torch.float32
+        M = shape[1] if len(shape) == 2 else 1
     if out is None:
-        rows = torch.empty(N * (2 + M + k), dtype=f32, device=dev).split((N * M, N, N, N * k))
-        out = TokenLogprobs(rows[0].view(tokens.shape) if M else None, rows[1], rows[2],
-                            torch.empty(N, k, dtype=torch.int32, device=dev) if k else None, rows[3].view(N, k) if k else None)
-    if (out.logprob is None) != (not M) or (out.top_idx is None) != (not k):
+        given, lse, entropy, idx, top = torch.empty(N * (2 + M + 2 * k), dtype=f32, device=dev).split_with_sizes(
+            (N * M, N, N, N * k, N * k))
+        out = TokenLogprobs(given.view(shape) if M else None, lse, entropy, idx.view(i32).view(N, k) if k else None,
+                            top.view(N, k) if k else None)
+    elif (out.logprob is None) != (not M) or (out.top_idx is None) != (not k):
         raise ValueError("out.logprob goes with tokens, out.top_idx with k")
-    for t, what, shape in ((out.logprob, "logprob", tokens.shape if M else None), (out.lse, "lse", (N,)),
-                           (out.entropy, "entropy", (N,)), (out.top_logprob, "top_logprob", (N, k))):
-        if t is not None and (t.dtype != f32 or tuple(t.shape) != tuple(shape)):
-            raise ValueError(f"{what} must be float32 {list(shape)}")
     if workspace is None:
         workspace = torch.empty(moe_token_logprobs_workspace_size(N), dtype=torch.uint8, device=dev)
+    rows, best = (N,), (N, k)
     _check("moe_token_logprobs", lib().moe_token_logprobs(
-        logits.data_ptr(), MOE_BF16 if logits.dtype == torch.bfloat16 else MOE_F32, logits.stride(0) if N > 1 else max(V, logits.stride(0)), N, V, scale,
-        _int32_ptr(tokens, "tokens", *tokens.shape) if M else None, M, k, _dev_ptr(out.logprob, "logprob"), _dev_ptr(out.lse, "lse"),
-        _dev_ptr(out.entropy, "entropy"), _int32_ptr(out.top_idx, "top_idx", N, k) if k else None,
-        _dev_ptr(out.top_logprob, "top_logprob"), _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(),
-        _stream(logits)))
+        logits.data_ptr(), MOE_F32 if dtype is f32 else MOE_BF16, stride, N, V, scale, ptr(tokens, i32, "tokens", shape) if M else None,
+        M, k, ptr(out.logprob, f32, "logprob", shape) if M else None,
+        None if out.lse is None else ptr(out.lse, f32, "lse", rows), None if out.entropy is None else ptr(out.entropy, f32, "entropy", rows),
+        ptr(out.top_idx, i32, "top_idx", best) if k else None,
+        None if out.top_logprob is None else ptr(out.top_logprob, f32, "top_logprob", best), _dev_ptr(workspace, "workspace"),
+        workspace.numel() * workspace.element_size(), _stream(logits)))
     return out
 
 

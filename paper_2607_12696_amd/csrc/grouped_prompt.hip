@@ -70,7 +70,7 @@ struct Block {
 // Sums of a chunk: for each row the reference maximum and the weights' sum, and the output sums in accumulator order.
 struct PromptParts {
     float2 *ml;  // [slot][kRows]
-    float *o;    // [slot][wavefront][D / 32][4][lane][4]
+    float *o;    // [slot][wavefront][D / 8][lane][4]
 };
 
 typedef __attribute__((ext_vector_type(2))) float f32x2;
@@ -331,44 +331,60 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void prompt_kernel(Group
     else if (a.lse) a.lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) / kLog2e;
 }
 
-// Adds up the chunks of a row block: a workgroup has 32 rows, a lane of a wavefront the four elements that registers 4 i .. of
-// that lane of the accumulators hold.
+// Adds up the chunks of a row block: a workgroup has 32 rows by 8 elements, what registers 4 i .. 4 i + 3 of one element tile
+// of the accumulators hold; each wavefront takes every fourth chunk.  (7 tokens over 4008 keys, 31 chunks: 64 rows' groups a
+// workgroup, all chunks one after the other, 23 us.)
 template <int D>
 __global__ __launch_bounds__(kThreads) void join_prompt_kernel(GroupedPromptArgs a, int blocks, int most_chunks, PromptParts parts)
 {
-    constexpr int kTiles = D / 32;
-    const int of = blockIdx.x % kWaves, pb = blockIdx.x / kWaves, pair = pb / blocks;
-    const Block blk(a, pair, pb % blocks, kRows);
-    const int chunks = chunks_of(blk.tiles, most_chunks), lane = lane_id(), i = threadIdx.x / kWave;
+    constexpr int kGroups = D / 32 * 4;
+    __shared__ float tops[kWaves][32];
+    __shared__ f32x4 sums[kWaves - 1][kWave];
+    __shared__ float totals[kWaves - 1][kWave];
+    const int group = blockIdx.x % kGroups, of = blockIdx.x / kGroups % kWaves, pb = blockIdx.x / (kGroups * kWaves);
+    const Block blk(a, pb / blocks, pb % blocks, kRows);
+    const int chunks = chunks_of(blk.tiles, most_chunks), lane = lane_id(), wave = threadIdx.x / kWave;
     const int row = blk.row0 + of * 32 + lane % 32;
-    if (chunks == 1 || row >= blk.rows) return;
+    if (chunks == 1 || blk.row0 + of * 32 >= blk.rows) return;
     const float2 *ml = parts.ml + (long)pb * most_chunks * kRows + of * 32 + lane % 32;
+    const f32x4 *o = reinterpret_cast<const f32x4 *>(parts.o) + (((long)pb * most_chunks * kWaves + of) * kGroups + group) * kWave + lane;
+    constexpr long kStep = kWaves * kGroups * kWave;
     float top = -INFINITY;
 #pragma unroll 8
-    for (int c = 0; c < chunks; ++c) top = fmaxf(top, ml[c * kRows].x);
+    for (int c = wave; c < chunks; c += kWaves) top = fmaxf(top, ml[c * kRows].x);
+    if (lane < 32) tops[wave][lane] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, tops[w][lane % 32]);
     const float base = top == -INFINITY ? 0.f : top;
     float total = 0.f;
-    f32x4 sum[kTiles] = {};
-    const f32x4 *o = reinterpret_cast<const f32x4 *>(parts.o) + (((long)pb * most_chunks * kWaves + of) * kTiles * 4 + i) * kWave + lane;
-#pragma unroll 4
-    for (int c = 0; c < chunks; ++c) {
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int c = wave; c < chunks; c += kWaves) {
+        const f32x4 v = o[c * kStep];
         const float2 part = ml[c * kRows];
         const float f = __builtin_amdgcn_exp2f(part.x - base);
         total = fmaf(part.y, f, total);
 #pragma unroll
-        for (int d = 0; d < kTiles; ++d) {
-            const f32x4 v = o[((long)c * kWaves * kTiles + d) * 4 * kWave];
+        for (int n = 0; n < 4; ++n) sum[n] = fmaf(v[n], f, sum[n]);
+    }
+    if (wave) {
+        sums[wave - 1][lane] = sum;
+        totals[wave - 1][lane] = total;
+    }
+    __syncthreads();
+    if (wave || row >= blk.rows) return;
 #pragma unroll
-            for (int n = 0; n < 4; ++n) sum[d][n] = fmaf(v[n], f, sum[d][n]);
-        }
+    for (int w = 0; w < kWaves - 1; ++w) {
+        total += totals[w][lane];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) sum[n] += sums[w][lane][n];
     }
     const float inv = total == 0.f ? 0.f : 1.f / total;
     const long at = (long)(blk.q0 + row / blk.G) * a.H + blk.hk * blk.G + row % blk.G;
-#pragma unroll
-    for (int d = 0; d < kTiles; ++d)
-        *reinterpret_cast<u32x2 *>(a.o + at * D + 32 * d + 8 * i + lane / 32 * 4) =
-            u32x2{pack_bf16x2(sum[d][0] * inv, sum[d][1] * inv), pack_bf16x2(sum[d][2] * inv, sum[d][3] * inv)};
-    if (a.lse && i == 0 && lane < 32) a.lse[at] = total == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(total)) / kLog2e;
+    *reinterpret_cast<u32x2 *>(a.o + at * D + 8 * group + lane / 32 * 4) =
+        u32x2{pack_bf16x2(sum[0] * inv, sum[1] * inv), pack_bf16x2(sum[2] * inv, sum[3] * inv)};
+    if (a.lse && group == 0 && lane < 32) a.lse[at] = total == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(total)) / kLog2e;
 }
 
 // Two tiles a barrier where LDS has room for all the wavefronts that registers allow (heads of 64: 85 us with one, 83 with two;
@@ -383,13 +399,15 @@ hipError_t launch(const GroupedPromptArgs &a, void *workspace, hipStream_t strea
     const int pairs = a.B * a.Hkv, blocks = (int)((rows + kRows - 1) / kRows);
     char *w = static_cast<char *>(workspace);
     const PromptParts parts{reinterpret_cast<float2 *>(w), reinterpret_cast<float *>(w + kSlots * kRows * sizeof(float2))};
-    const long room = kSlots / ((long)pairs * blocks), cut = (a.M + kKeys - 1) / kKeys / kMinTiles;
+    // The longest sequence's keys are known on the device only; it is taken to have twice the average.  (40 sequences of up to
+    // 53 tokens and keys: a second launch that joins nothing, 5.8 us.)
+    const long room = kSlots / ((long)pairs * blocks), cut = 2L * a.M / ((long)a.B * kKeys * kMinTiles);
     const int chunks = (int)(room < cut ? room : cut);
     if (chunks > 1) {
         prompt_kernel<D, kTilesAStep<D>, true><<<(unsigned)(pairs * blocks * chunks), kThreads, 0, stream>>>(a, blocks, chunks, parts);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        join_prompt_kernel<D><<<(unsigned)(pairs * blocks * kWaves), kThreads, 0, stream>>>(a, blocks, chunks, parts);
+        join_prompt_kernel<D><<<(unsigned)(pairs * blocks * kWaves * (D / 8)), kThreads, 0, stream>>>(a, blocks, chunks, parts);
         return hipGetLastError();
     }
     prompt_kernel<D, kTilesAStep<D>, false><<<(unsigned)((long)pairs * blocks), kThreads, 0, stream>>>(a, blocks, 1, parts);

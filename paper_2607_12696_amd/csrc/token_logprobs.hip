@@ -15,8 +15,10 @@
 // bound, found bit by bit with ballots.  A full list is cut to its k best.
 // Elements come in ascending order, so what only equals the bound of an earlier
 // tile has k better ones before it.
-// Parts of a row by different wavefronts (their sums, their lists) are joined
-// by a second kernel, a wavefront a row.
+// Parts of a row by different wavefronts leave their sums and their k best in
+// order; a second kernel joins the sums and merges the lists, a lane to a part:
+// k times the largest head, the lowest lane among equal ones (its elements come
+// first).
 // What bounds it: memory, for many rows; for few the two launches and the chain
 // of load, bound, list, join.
 #include "device.hpp"
@@ -31,24 +33,29 @@ constexpr int kGroup = 4;           // elements of a lane between looks at the l
 constexpr int kList = (kGroup + 1) * kWave;  // entries of a wavefront's list
 constexpr int kKept = 64;           // most entries that a wavefront leaves
 constexpr int kMinParts = 4096;     // wavefronts that fill the card: 16 a compute unit
-constexpr int kMaxParts = 256;      // of a row
+constexpr int kMaxParts = kWave;    // of a row: a lane each when they are joined
 constexpr float kFloor = -1e30f;    // stands for -inf where -inf * 0 must not arise
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
 
-struct Part {
+// What the parts of a row leave, k lists of the heads, the seconds and so on: entry r of part p at r * parts + p.
+struct Head {
     float m, s, a;
     int count;
-    float value[kKept];
-    int index[kKept];
 };
 
-// Wavefronts of a row.
+struct Work {
+    Head *heads;      // [N][parts]
+    float *values;    // [N][k][parts]
+    int *indices;     // [N][k][parts]
+};
+
+// Wavefronts of a row: all have the same number of tiles but the last.
 __host__ __device__ inline int parts_of(int N, int V)
 {
     const int tiles = (V + kTile - 1) / kTile, want = (kMinParts + N - 1) / N;
-    const int most = want < kMaxParts ? want : kMaxParts;
-    return tiles < most ? tiles : most;
+    const int most = want < kMaxParts ? want : kMaxParts, each = (tiles + most - 1) / most;
+    return (tiles + each - 1) / each;
 }
 
 // Order of a float as an unsigned number; -0 as +0; no NaN.
@@ -175,6 +182,23 @@ struct Best {
         bound = float_of(t);
     }
 
+    // The lane's entry of at most 64, and how many come before it; a rank of at least 64 where it has none.
+    __device__ __forceinline__ int ranked(float &v, int &at) const
+    {
+        wave_fence();
+        const bool has = lane_id() < count;
+        v = has ? value[lane_id()] : 0.f;
+        at = has ? index[lane_id()] : 0;
+        const uint32_t key = v != v ? 0u : order_of(v);  // NaN after every number
+        int rank = has ? 0 : kWave;
+        for (int i = 0; i < count; ++i) {
+            const uint32_t other = __builtin_amdgcn_readlane(key, i);
+            const int x = __builtin_amdgcn_readlane(at, i);
+            rank += other > key || (other == key && x < at);
+        }
+        return rank;
+    }
+
     // A tile of E elements a lane, of higher index than all before; top: the lane's largest.
     template <int E, class F>
     __device__ __forceinline__ void tile(const float (&v)[E], float top, F index_of)
@@ -219,7 +243,7 @@ __device__ __forceinline__ float largest(const float (&v)[32])
 }
 
 template <bool BF16, bool TOP>
-__global__ __launch_bounds__(kThreads) void parts_kernel(LogprobArgs a, int parts, Part *out)
+__global__ __launch_bounds__(kThreads) void parts_kernel(LogprobArgs a, int parts, Work out)
 {
     constexpr int kVec = BF16 ? 8 : 4, kLoads = 32 / kVec, kBytes = BF16 ? 2 : 4;
     __shared__ float values[TOP ? kWaves : 1][TOP ? kList : 1];
@@ -232,7 +256,7 @@ __global__ __launch_bounds__(kThreads) void parts_kernel(LogprobArgs a, int part
     // The row from its first whole 16 bytes on; what lies before and behind goes element by element.
     const int head = min((int)(-(uintptr_t)p % 16) / kBytes, a.V), vectors = (a.V - head) / kVec;
     const int tail = head + vectors * kVec, tiles = (vectors + kLoads * kWave - 1) / (kLoads * kWave);
-    const int first = (int)((long)tiles * part / parts), last = (int)((long)tiles * (part + 1) / parts);
+    const int each = (tiles + parts - 1) / parts, first = min(part * each, tiles), last = min(first + each, tiles);
     const float scale2 = a.scale * kLog2e;
 
     Sums sums;
@@ -271,101 +295,124 @@ __global__ __launch_bounds__(kThreads) void parts_kernel(LogprobArgs a, int part
             }
         const float top = largest(v);
         if (top > sums.m) sums.move(top, scale2);
+        // Four sums of 8 and their sum, not 32 in a row: shorter chains, of additions as of their roundings.
+        Sums four[4];
 #pragma unroll
-        for (int e = 0; e < 32; ++e) sums.add(v[e], scale2);
+        for (int e = 0; e < 32; ++e) {
+            four[e % 4].m = sums.m;
+            four[e % 4].add(v[e], scale2);
+        }
+        sums.s += (four[0].s + four[1].s) + (four[2].s + four[3].s);
+        sums.a += (four[0].a + four[1].a) + (four[2].a + four[3].a);
         if (TOP)
             best.tile(v, top, [&](int e) { return head + (at + e / kVec * kWave) * kVec + e % kVec; });
     }
     if (part == parts - 1 && tail < a.V) edge(tail, a.V);
 
     sums.join_lanes(scale2);
-    Part *to = out + id;
     if (TOP) {
         if (best.count > kKept) best.cut();
-        wave_fence();
-        if (lane < best.count) {
-            to->value[lane] = best.value[lane];
-            to->index[lane] = best.index[lane];
+        float v;
+        int at;
+        const int rank = best.ranked(v, at);
+        if (rank < a.k) {
+            const long to = ((long)row * a.k + rank) * parts + part;
+            out.values[to] = v;
+            out.indices[to] = at;
         }
     }
-    if (lane == 0) {
-        to->m = sums.m;
-        to->s = sums.s;
-        to->a = sums.a;
-        to->count = best.count;
-    }
+    if (lane == 0) out.heads[id] = Head{sums.m, sums.s, sums.a, min(best.count, a.k)};
+}
+
+// Largest of the lanes' numbers, uniform (lane moves: lane 63 ends with it).
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ uint32_t max_step(uint32_t v)
+{
+    const uint32_t o = __builtin_amdgcn_update_dpp(0u, v, CTRL, ROW_MASK, 0xf, false);
+    return o > v ? o : v;
+}
+
+__device__ __forceinline__ uint32_t largest_of_lanes(uint32_t v)
+{
+    v = max_step<0x111, 0xf>(v);  // row_shr:1
+    v = max_step<0x112, 0xf>(v);  // row_shr:2
+    v = max_step<0x114, 0xf>(v);  // row_shr:4
+    v = max_step<0x118, 0xf>(v);  // row_shr:8
+    v = max_step<0x142, 0xa>(v);  // row_bcast:15 into rows 1 and 3
+    v = max_step<0x143, 0xc>(v);  // row_bcast:31 into rows 2 and 3
+    return __builtin_amdgcn_readlane(v, kWave - 1);
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(kWave) void join_kernel(LogprobArgs a, int parts, const Part *in)
+__global__ __launch_bounds__(kThreads) void join_kernel(LogprobArgs a, int parts, Work in)
 {
-    constexpr int kBytes = BF16 ? 2 : 4, kAtOnce = 8;
-    __shared__ float values[kList];
-    __shared__ int indices[kList];
-    const int row = blockIdx.x, lane = lane_id();
+    constexpr int kBytes = BF16 ? 2 : 4;
+    extern __shared__ uint32_t lists[];  // [k][parts] orders, then [k][parts] indices
+    const int row = blockIdx.x, lane = lane_id(), wave = threadIdx.x / kWave;
     const char *p = static_cast<const char *>(a.logits) + row * a.stride * kBytes;
-    const Part *mine = in + (long)row * parts;
     const float scale2 = a.scale * kLog2e;
 
-    Sums sums;
-    for (int i = lane; i < parts; i += kWave) sums.join(Sums{mine[i].m, mine[i].s, mine[i].a}, scale2);
+    const Head head = lane < parts ? in.heads[(long)row * parts + lane] : Head{kLowest, 0.f, 0.f, 0};
+    const int entries = a.k * parts;
+    for (int i = threadIdx.x; i < entries; i += blockDim.x) {
+        lists[i] = __float_as_uint(in.values[(long)row * entries + i]);
+        lists[entries + i] = (uint32_t)in.indices[(long)row * entries + i];
+    }
+    Sums sums{head.m, head.s, head.a};
     sums.join_lanes(scale2);
     const bool nothing = sums.s == 0.f;  // every logit is -inf
     const float log_s = logf(sums.s);
-    if (lane == 0) {
+    if (threadIdx.x == 0) {
         if (a.lse) a.lse[row] = nothing ? -INFINITY : fmaf(sums.m, a.scale, log_s);
         if (a.entropy) a.entropy[row] = nothing ? 0.f : fmaf(-kLn2, sums.a / sums.s, log_s);
     }
     auto logprob = [&](float l) { return nothing ? -INFINITY : fmaf(l - sums.m, a.scale, -log_s); };
-    for (int i = lane; i < a.M; i += kWave) {
+    for (int i = threadIdx.x; i < a.M; i += blockDim.x) {
         const int t = a.tokens[(long)row * a.M + i];
         a.logprob[(long)row * a.M + i] = t >= 0 && t < a.V ? logprob(logit<BF16>(p, t)) : -INFINITY;
     }
-    if (!a.k) return;
+    __syncthreads();
+    if (!a.k || wave) return;
 
-    Best best{values, indices, a.k};
-    for (int i0 = 0; i0 < parts; i0 += kAtOnce) {
-        float v[kAtOnce], top = -INFINITY;
-        int at[kAtOnce];
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            const bool has = i0 + i < parts && lane < mine[i0 + i].count;
-            v[i] = has ? mine[i0 + i].value[lane] : -INFINITY;
-            at[i] = has ? mine[i0 + i].index[lane] : 0;
-            top = fmaxf(top, v[i]);
+    // Lane r keeps what comes r-th.
+    float v = 0.f;
+    int at = 0, count = 0, next = 0;
+    auto order_at = [&](int r) { return r < head.count ? order_of(__uint_as_float(lists[r * parts + lane])) : 0u; };
+    uint32_t key = order_at(0), second = order_at(1);
+    for (; count < a.k; ++count) {
+        const uint32_t win = largest_of_lanes(key);
+        if (!win) break;
+        const int from = (int)__builtin_ctzll(__ballot(key == win));
+        const int place = __builtin_amdgcn_readlane(next, from) * parts + from;
+        if (lane == count) {
+            v = float_of(win);
+            at = place;
         }
-        best.tile(v, top, [&](int e) { return at[e]; });
+        if (lane == from) {
+            ++next;
+            key = second;
+            second = order_at(next + 1);
+        }
     }
-    best.cut();
+    at = lane < count ? (int)lists[entries + at] : 0;
     // Fewer than k numbers above -inf: the first -inf, then the first NaN.
-    for (int pass = 0; pass < 2 && best.count < a.k; ++pass) {
-        for (int i0 = 0; i0 < a.V && best.count < a.k; i0 += kWave) {
+    for (int pass = 0; pass < 2 && count < a.k; ++pass) {
+        for (int i0 = 0; i0 < a.V && count < a.k; i0 += kWave) {
             const float l = i0 + lane < a.V ? logit<BF16>(p, i0 + lane) : 0.f;
-            const bool is = pass ? l != l : l == -INFINITY;
-            const uint64_t mask = __ballot(is);
-            const int place = best.count + lanes_before(mask);
-            if (is && place < a.k) {
-                values[place] = l;
-                indices[place] = i0 + lane;
+            uint64_t mask = __ballot(pass ? l != l : l == -INFINITY);
+            for (; mask && count < a.k; ++count, mask &= mask - 1) {
+                const int from = (int)__builtin_ctzll(mask);
+                const float w = __shfl(l, from, kWave);
+                if (lane == count) {
+                    v = w;
+                    at = i0 + from;
+                }
             }
-            best.count = min(best.count + (int)__builtin_popcountll(mask), a.k);
         }
     }
-    // Each lane's entry, and how many come before it.
-    wave_fence();
-    const bool has = lane < best.count;
-    const float v = has ? values[lane] : 0.f;
-    const int at = has ? indices[lane] : 0;
-    const uint32_t key = v != v ? 0u : order_of(v);
-    int rank = 0;
-    for (int i = 0; i < best.count; ++i) {
-        const uint32_t k = __builtin_amdgcn_readlane(key, i);
-        const int x = __builtin_amdgcn_readlane(at, i);
-        rank += k > key || (k == key && x < at);
-    }
-    if (!has) return;
-    a.top_idx[(long)row * a.k + rank] = at;
-    if (a.top_logprob) a.top_logprob[(long)row * a.k + rank] = logprob(v);
+    if (lane >= a.k) return;
+    a.top_idx[(long)row * a.k + lane] = at;
+    if (a.top_logprob) a.top_logprob[(long)row * a.k + lane] = logprob(v);
 }
 
 }  // namespace
@@ -373,25 +420,31 @@ __global__ __launch_bounds__(kWave) void join_kernel(LogprobArgs a, int parts, c
 size_t logprobs_workspace(int N)
 {
     // parts_of(N, V) <= kMinParts / N + 1 for every V.
-    return ((size_t)kMinParts + N) * sizeof(Part);
+    return ((size_t)kMinParts + N) * (sizeof(Head) + kKept * (sizeof(float) + sizeof(int)));
 }
 
 hipError_t launch_token_logprobs(const LogprobArgs &a, bool bf16, void *workspace, hipStream_t stream)
 {
     const int parts = parts_of(a.N, a.V);
-    Part *p = static_cast<Part *>(workspace);
-    const unsigned grid = (unsigned)(((long)a.N * parts + kWaves - 1) / kWaves);
+    const long n = (long)a.N * parts;
+    Work w;
+    w.heads = static_cast<Head *>(workspace);
+    w.values = reinterpret_cast<float *>(w.heads + n);
+    w.indices = reinterpret_cast<int *>(w.values + n * a.k);
+    const unsigned grid = (unsigned)((n + kWaves - 1) / kWaves);
     if (bf16) {
-        if (a.k) parts_kernel<true, true><<<grid, kThreads, 0, stream>>>(a, parts, p);
-        else parts_kernel<true, false><<<grid, kThreads, 0, stream>>>(a, parts, p);
+        if (a.k) parts_kernel<true, true><<<grid, kThreads, 0, stream>>>(a, parts, w);
+        else parts_kernel<true, false><<<grid, kThreads, 0, stream>>>(a, parts, w);
     } else {
-        if (a.k) parts_kernel<false, true><<<grid, kThreads, 0, stream>>>(a, parts, p);
-        else parts_kernel<false, false><<<grid, kThreads, 0, stream>>>(a, parts, p);
+        if (a.k) parts_kernel<false, true><<<grid, kThreads, 0, stream>>>(a, parts, w);
+        else parts_kernel<false, false><<<grid, kThreads, 0, stream>>>(a, parts, w);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (bf16) join_kernel<true><<<(unsigned)a.N, kWave, 0, stream>>>(a, parts, p);
-    else join_kernel<false><<<(unsigned)a.N, kWave, 0, stream>>>(a, parts, p);
+    // One wavefront does the merging; more of them bring long lists.
+    const int entries = a.k * parts, threads = entries > 4 * kWave ? kThreads : kWave;
+    if (bf16) join_kernel<true><<<(unsigned)a.N, threads, entries * 8, stream>>>(a, parts, w);
+    else join_kernel<false><<<(unsigned)a.N, threads, entries * 8, stream>>>(a, parts, w);
     return hipGetLastError();
 }
 
