@@ -1,12 +1,12 @@
 // Log probabilities of given tokens, log-sum, entropy and the k best
 // alternatives of rows of logits, read once.
 //
-// The sums: with a reference logit m and x = (l - m) * scale * log2 e,
+// The sums: with a reference logit m, c = scale * log2 e and x = (l - m) c,
 //   S = sum 2^x,  A = sum 2^x x,
 //   lse = m * scale + ln S,  entropy = ln S - ln 2 * A / S:
 // both terms of the entropy are at least 0 where m is the largest logit, so
-// nothing cancels.  Moving the reference by d = (m - m') * scale * log2 e takes A
-// to (A + d S) 2^d and S to S 2^d, so every lane has a reference of its own, and
+// nothing cancels.  Moving the reference by d = (m - m') c takes A to
+// (A + d S) 2^d and S to S 2^d, so every lane has a reference of its own, and
 // they are joined at the end.
 // The alternatives: a wavefront holds a bound below which nothing can be among
 // its k best, and a list in LDS of what has passed it.  A tile of 32 elements a
@@ -40,7 +40,8 @@ constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
 
 // What the parts of a row leave, k lists of the heads, the seconds and so on: entry r of part p at r * parts + p.
 struct Head {
-    float m, s, a;
+    double s;
+    float m, a;
     int count;
 };
 
@@ -81,34 +82,54 @@ __device__ __forceinline__ int lanes_before(uint64_t mask)
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
 }
 
+// S is held in 64 bits: where one token has almost all of the probability, S is 1 and a little, and ln S, the token's log
+// probability and most of the entropy are that little.
 struct Sums {
-    float m = kLowest, s = 0.f, a = 0.f;
+    float m = kLowest, a = 0.f;
+    double s = 0.;
 
-    __device__ __forceinline__ void move(float to, float scale2)  // to >= m
+    __device__ __forceinline__ void move(float to, float c)  // to >= m
     {
-        const float d = fmaxf((m - to) * scale2, kFloor), f = __builtin_amdgcn_exp2f(d);
-        a = fmaf(d, s, a) * f;
+        const float d = fmaxf((m - to) * c, kFloor), f = __builtin_amdgcn_exp2f(d);
+        a = fmaf(d, (float)s, a) * f;
         s *= f;
         m = to;
     }
-    __device__ __forceinline__ void add(float l, float scale2)
-    {
-        const float x = (l - m) * scale2, e = __builtin_amdgcn_exp2f(x);
-        s += e;
-        a = fmaf(e, fmaxf(x, kFloor), a);
-    }
-    __device__ __forceinline__ void join(Sums o, float scale2)
+    __device__ __forceinline__ void join(Sums o, float c)
     {
         const float top = fmaxf(m, o.m);
-        move(top, scale2);
-        o.move(top, scale2);
+        move(top, c);
+        o.move(top, c);
         s += o.s;
         a += o.a;
     }
-    __device__ __forceinline__ void join_lanes(float scale2)
+    __device__ __forceinline__ void join_lanes(float c)
     {
 #pragma unroll
-        for (int x = 32; x >= 1; x >>= 1) join(Sums{__shfl_xor(m, x, kWave), __shfl_xor(s, x, kWave), __shfl_xor(a, x, kWave)}, scale2);
+        for (int x = 32; x >= 1; x >>= 1) join(Sums{__shfl_xor(m, x, kWave), __shfl_xor(a, x, kWave), __shfl_xor(s, x, kWave)}, c);
+    }
+    // E logits, none above m: two chains of additions.
+    template <int E>
+    __device__ __forceinline__ void add(const float (&l)[E], float c)
+    {
+        double t[2];
+        float u[2];
+        auto sum = [&](float floor) {
+            t[0] = t[1] = 0.;
+            u[0] = u[1] = 0.f;
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const float x = (l[i] - m) * c, e = __builtin_amdgcn_exp2f(x);
+                t[i % 2] += e;
+                u[i % 2] = fmaf(e, floor == 0.f ? x : fmaxf(x, floor), u[i % 2]);
+            }
+        };
+        sum(0.f);
+        // 0 * -inf where a logit is -inf: once more, with a finite number in its place.  (A maximum for each element instead
+        // is a ninth of the instructions.)
+        if (__any(u[0] + u[1] != u[0] + u[1])) sum(kFloor);
+        s += t[0] + t[1];
+        a += u[0] + u[1];
     }
 };
 
@@ -257,15 +278,15 @@ __global__ __launch_bounds__(kThreads) void parts_kernel(LogprobArgs a, int part
     const int head = min((int)(-(uintptr_t)p % 16) / kBytes, a.V), vectors = (a.V - head) / kVec;
     const int tail = head + vectors * kVec, tiles = (vectors + kLoads * kWave - 1) / (kLoads * kWave);
     const int each = (tiles + parts - 1) / parts, first = min(part * each, tiles), last = min(first + each, tiles);
-    const float scale2 = a.scale * kLog2e;
+    const float c = a.scale * kLog2e;
 
     Sums sums;
     Best best{values[TOP ? wave : 0], indices[TOP ? wave : 0], a.k};
     auto edge = [&](int from, int to) {  // up to 64 elements, one a lane
         const float v[1] = {from + lane < to ? logit<BF16>(p, from + lane) : -INFINITY};
         if (from + lane < to) {
-            if (v[0] > sums.m) sums.move(v[0], scale2);
-            sums.add(v[0], scale2);
+            if (v[0] > sums.m) sums.move(v[0], c);
+            sums.add(v, c);
         }
         if (TOP) best.tile(v, v[0], [&](int) { return from + lane; });
     };
@@ -294,22 +315,14 @@ __global__ __launch_bounds__(kThreads) void parts_kernel(LogprobArgs a, int part
                 }
             }
         const float top = largest(v);
-        if (top > sums.m) sums.move(top, scale2);
-        // Four sums of 8 and their sum, not 32 in a row: shorter chains, of additions as of their roundings.
-        Sums four[4];
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-            four[e % 4].m = sums.m;
-            four[e % 4].add(v[e], scale2);
-        }
-        sums.s += (four[0].s + four[1].s) + (four[2].s + four[3].s);
-        sums.a += (four[0].a + four[1].a) + (four[2].a + four[3].a);
+        if (top > sums.m) sums.move(top, c);
+        sums.add(v, c);
         if (TOP)
             best.tile(v, top, [&](int e) { return head + (at + e / kVec * kWave) * kVec + e % kVec; });
     }
     if (part == parts - 1 && tail < a.V) edge(tail, a.V);
 
-    sums.join_lanes(scale2);
+    sums.join_lanes(c);
     if (TOP) {
         if (best.count > kKept) best.cut();
         float v;
@@ -321,7 +334,7 @@ __global__ __launch_bounds__(kThreads) void parts_kernel(LogprobArgs a, int part
             out.indices[to] = at;
         }
     }
-    if (lane == 0) out.heads[id] = Head{sums.m, sums.s, sums.a, min(best.count, a.k)};
+    if (lane == 0) out.heads[id] = Head{sums.s, sums.m, sums.a, min(best.count, a.k)};
 }
 
 // Largest of the lanes' numbers, uniform (lane moves: lane 63 ends with it).
@@ -350,21 +363,21 @@ __global__ __launch_bounds__(kThreads) void join_kernel(LogprobArgs a, int parts
     extern __shared__ uint32_t lists[];  // [k][parts] orders, then [k][parts] indices
     const int row = blockIdx.x, lane = lane_id(), wave = threadIdx.x / kWave;
     const char *p = static_cast<const char *>(a.logits) + row * a.stride * kBytes;
-    const float scale2 = a.scale * kLog2e;
+    const float c = a.scale * kLog2e;
 
-    const Head head = lane < parts ? in.heads[(long)row * parts + lane] : Head{kLowest, 0.f, 0.f, 0};
+    const Head head = lane < parts ? in.heads[(long)row * parts + lane] : Head{0., kLowest, 0.f, 0};
     const int entries = a.k * parts;
     for (int i = threadIdx.x; i < entries; i += blockDim.x) {
         lists[i] = __float_as_uint(in.values[(long)row * entries + i]);
         lists[entries + i] = (uint32_t)in.indices[(long)row * entries + i];
     }
-    Sums sums{head.m, head.s, head.a};
-    sums.join_lanes(scale2);
-    const bool nothing = sums.s == 0.f;  // every logit is -inf
-    const float log_s = logf(sums.s);
+    Sums sums{head.m, head.a, head.s};
+    sums.join_lanes(c);
+    const bool nothing = sums.s == 0.;  // every logit is -inf
+    const float log_s = (float)log(sums.s);
     if (threadIdx.x == 0) {
         if (a.lse) a.lse[row] = nothing ? -INFINITY : fmaf(sums.m, a.scale, log_s);
-        if (a.entropy) a.entropy[row] = nothing ? 0.f : fmaf(-kLn2, sums.a / sums.s, log_s);
+        if (a.entropy) a.entropy[row] = nothing ? 0.f : fmaf(-kLn2, sums.a / (float)sums.s, log_s);
     }
     auto logprob = [&](float l) { return nothing ? -INFINITY : fmaf(l - sums.m, a.scale, -log_s); };
     for (int i = threadIdx.x; i < a.M; i += blockDim.x) {
