@@ -663,9 +663,10 @@ def moe_latent_attn(q, kv_new, token_offsets, pages, block_table, cache_len, r: 
 
 def _strided_ptr(t, what: str, M: int, H: int) -> tuple[int, int, int, int]:
     """Pointer, head width, token stride and head stride of bf16 [M, H, width] with contiguous heads."""
-    if not t.is_cuda or t.dtype != _torch().bfloat16 or t.dim() != 3 or t.shape[0] != M or t.shape[1] != H or t.stride(2) != 1:
+    shape, stride = t.shape, t.stride()
+    if not t.is_cuda or t.dtype is not _torch().bfloat16 or len(shape) != 3 or shape[0] != M or shape[1] != H or stride[2] != 1:
         raise ValueError(f"{what} must be bfloat16 [{M}, {H}, width] on the device, contiguous along its last axis")
-    return t.data_ptr(), t.shape[2], t.stride(0), t.stride(1)
+    return t.data_ptr(), shape[2], stride[0], stride[1]
 
 
 def moe_latent_prompt(q, k, k_rope, v, q_offsets, kv_offsets, scale: float, max_tokens: int | None = None, o=None, lse=None):
@@ -767,18 +768,21 @@ def moe_pages_update(cache_len, token_offsets, block_table, free_pages, n_free, 
     i32, ptr = torch.int32, _typed_ptr
     B, blocks = block_table.shape
     n_pages, dev = free_pages.shape[0], block_table.device
-    if out is None:
-        ints = torch.empty(B + 2 + N, dtype=i32, device=dev).split_with_sizes((B, 1, 1, N))
-        out = PageUpdate(ints[0], ints[1], ints[2], torch.empty(N, dtype=torch.int64, device=dev), ints[3])
     per, one, tokens = (B,), (1,), (N,)
+    if out is None:
+        ints, slots = torch.empty(B + 2 + N, dtype=i32, device=dev), torch.empty(N, dtype=torch.int64, device=dev)
+        parts, at = ints.split_with_sizes((B, 1, 1, N)), ints.data_ptr()
+        out = PageUpdate(parts[0], parts[1], parts[2], slots, parts[3])
+        to = at, at + 4 * B, at + 4 * B + 4, slots.data_ptr(), at + 4 * B + 8
+    else:
+        to = (ptr(out.new_len, i32, "new_len", per), ptr(out.n_free, i32, "n_free", one), ptr(out.refused, i32, "refused", one),
+              ptr(out.slots, torch.int64, "slots", tokens), ptr(out.positions, i32, "positions", tokens))
     pool = moe_page_pool_t(B, n_pages, page, blocks, ptr(block_table, i32, "block_table", (B, blocks)),
                            ptr(cache_len, i32, "cache_len", per), ptr(free_pages, i32, "free_pages", (n_pages,)),
                            ptr(n_free, i32, "n_free", one))
     _check("moe_pages_update", lib().moe_pages_update(
         C.byref(pool), None if keep_len is None else ptr(keep_len, i32, "keep_len", per),
-        ptr(token_offsets, i32, "token_offsets", (B + 1,)), N, ptr(out.new_len, i32, "new_len", per),
-        ptr(out.n_free, i32, "n_free", one), ptr(out.refused, i32, "refused", one), ptr(out.slots, torch.int64, "slots", tokens),
-        ptr(out.positions, i32, "positions", tokens), _stream(block_table)))
+        ptr(token_offsets, i32, "token_offsets", (B + 1,)), N, *to, _stream(block_table)))
     return out
 
 
@@ -811,6 +815,7 @@ def moe_grouped_prompt(q, k, v, q_offsets, kv_offsets, scale: float, max_tokens:
     q [N, H, D], k, v [M, Hkv, D] bf16 (strided views of a projection's output, contiguous along D); q_offsets, kv_offsets
     [B + 1] int32.  A sequence's queries are the last of its keys' tokens.  max_tokens: at least the most queries of a
     sequence (None: N)."""
+    torch = _torch()
     N, H = q.shape[:2]
     M, Hkv = k.shape[:2]
     B = q_offsets.shape[0] - 1
@@ -821,10 +826,11 @@ def moe_grouped_prompt(q, k, v, q_offsets, kv_offsets, scale: float, max_tokens:
         raise ValueError("q, k and v must have heads of one width")
     o, lse, op, lp = _attn_outputs(q, D, o, lse)
     if workspace is None:
-        workspace = _torch().empty(moe_grouped_prompt_workspace_size(D), dtype=_torch().uint8, device=q.device)
+        workspace = torch.empty(moe_grouped_prompt_workspace_size(D), dtype=torch.uint8, device=q.device)
+    off = (B + 1,)
     a = moe_grouped_prompt_t(N, M, B, H, Hkv, D, N if max_tokens is None else max_tokens,
-                             _int32_ptr(q_offsets, "q_offsets", B + 1), _int32_ptr(kv_offsets, "kv_offsets", B + 1), qp, kp, vp,
-                             qs, qh, ks, kh, vs, vh, scale)
+                             _typed_ptr(q_offsets, torch.int32, "q_offsets", off), _typed_ptr(kv_offsets, torch.int32, "kv_offsets", off),
+                             qp, kp, vp, qs, qh, ks, kh, vs, vh, scale)
     _check("moe_grouped_prompt", lib().moe_grouped_prompt(C.byref(a), op, lp, _dev_ptr(workspace, "workspace"),
                                                           workspace.numel() * workspace.element_size(), _stream(q)))
     return o, lse
@@ -871,22 +877,24 @@ def moe_token_logprobs(logits, tokens=None, k: int = 0, scale: float = 1.0, out:
             raise ValueError("tokens must be int32 [N] or [N, M]")
         M = shape[1] if len(shape) == 2 else 1
     if out is None:
-        given, lse, entropy, idx, top = torch.empty(N * (2 + M + 2 * k), dtype=f32, device=dev).split_with_sizes(
-            (N * M, N, N, N * k, N * k))
+        sizes = N * M, N, N, N * k, N * k
+        flat = torch.empty(N * (2 + M + 2 * k), dtype=f32, device=dev)
+        (given, lse, entropy, idx, top), at = flat.split_with_sizes(sizes), flat.data_ptr()
         out = TokenLogprobs(given.view(shape) if M else None, lse, entropy, idx.view(i32).view(N, k) if k else None,
                             top.view(N, k) if k else None)
-    elif (out.logprob is None) != (not M) or (out.top_idx is None) != (not k):
-        raise ValueError("out.logprob goes with tokens, out.top_idx with k")
+        at1, at2, at3 = at + 4 * N * M, at + 4 * N * (M + 1), at + 4 * N * (M + 2)
+        to = at if M else None, at1, at2, at3 if k else None, at3 + 4 * N * k if k else None
+    else:
+        if (out.logprob is None) != (not M) or (out.top_idx is None) != (not k):
+            raise ValueError("out.logprob goes with tokens, out.top_idx with k")
+        to = [None if t is None else ptr(t, kind, what, of) for t, kind, what, of in (
+            (out.logprob, f32, "logprob", shape), (out.lse, f32, "lse", (N,)), (out.entropy, f32, "entropy", (N,)),
+            (out.top_idx, i32, "top_idx", (N, k)), (out.top_logprob, f32, "top_logprob", (N, k)))]
     if workspace is None:
         workspace = torch.empty(moe_token_logprobs_workspace_size(N), dtype=torch.uint8, device=dev)
-    rows, best = (N,), (N, k)
     _check("moe_token_logprobs", lib().moe_token_logprobs(
         logits.data_ptr(), MOE_F32 if dtype is f32 else MOE_BF16, stride, N, V, scale, ptr(tokens, i32, "tokens", shape) if M else None,
-        M, k, ptr(out.logprob, f32, "logprob", shape) if M else None,
-        None if out.lse is None else ptr(out.lse, f32, "lse", rows), None if out.entropy is None else ptr(out.entropy, f32, "entropy", rows),
-        ptr(out.top_idx, i32, "top_idx", best) if k else None,
-        None if out.top_logprob is None else ptr(out.top_logprob, f32, "top_logprob", best), _dev_ptr(workspace, "workspace"),
-        workspace.numel() * workspace.element_size(), _stream(logits)))
+        M, k, *to, _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(logits)))
     return out
 
 
