@@ -29,8 +29,9 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr int kTile = 32 * kWave;   // elements
-constexpr int kGroup = 4;           // elements of a lane between looks at the list's room
-constexpr int kList = (kGroup + 1) * kWave;  // entries of a wavefront's list
+constexpr int kGroup = 8;           // elements of a lane that are looked at together
+constexpr int kRoom = 4 * kWave;    // entries that may come between looks at the list's length
+constexpr int kList = 2 * kWave + kRoom;  // entries of a wavefront's list
 constexpr int kKept = 64;           // most entries that a wavefront leaves
 constexpr int kMinParts = 4096;     // wavefronts that fill the card: 16 a compute unit
 constexpr int kMaxParts = kWave;    // of a row: a lane each when they are joined
@@ -144,15 +145,17 @@ __device__ __forceinline__ void wave_fence()
 struct Best {
     float *value;  // kList entries
     int *index;
-    int k, count = 0;
+    // A list of more than `longest` is cut before it grows: twice k, and at least 64.  (A longer one is cut less often, but
+    // the bound stays low until it is: 2048 rows of 200000, k = 5, up to 256 entries 171 us, 64 entries 164.)
+    int k, longest, count = 0;
     float bound = -INFINITY;  // k entries of the list are at least this; -inf: perhaps fewer
 
-    // The largest order that at least k of the lanes' n keys reach.
-    template <int E>
+    // The largest number, of the BITS upper bits, that at least k of the lanes' keys reach.
+    template <int BITS, int E>
     __device__ __forceinline__ static uint32_t kth(const uint32_t (&key)[E], int k)
     {
         uint32_t t = 0;
-        for (int bit = 31; bit >= 0; --bit) {
+        for (int bit = 31; bit >= 32 - BITS; --bit) {
             const uint32_t x = t | 1u << bit;
             int n = 0;
 #pragma unroll
@@ -179,7 +182,7 @@ struct Best {
             at[e] = i < count ? index[i] : 0;
             key[e] = i < count ? order_of(v[e]) : 0u;  // no number has order 0
         }
-        const uint32_t t = kth(key, k);
+        const uint32_t t = kth<32>(key, k);
         int more = 0;
 #pragma unroll
         for (int e = 0; e < E; ++e) more += __builtin_popcountll(__ballot(key[e] > t));
@@ -187,7 +190,7 @@ struct Best {
         uint32_t tie[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) tie[e] = key[e] == t ? ~(uint32_t)at[e] : 0u;
-        const uint32_t last = kth(tie, k - more);
+        const uint32_t last = kth<32>(tie, k - more);
         wave_fence();
         count = 0;
 #pragma unroll
@@ -220,31 +223,36 @@ struct Best {
         return rank;
     }
 
-    // A tile of E elements a lane, of higher index than all before; top: the lane's largest.
-    template <int E, class F>
-    __device__ __forceinline__ void tile(const float (&v)[E], float top, F index_of)
+    // A tile of E elements a lane, of higher index than all before; top: the lane's largest, group[g]: of the g-th kGroup.
+    template <int E, int G, class F>
+    __device__ __forceinline__ void tile(const float (&v)[E], float top, const float (&group)[G], F index_of)
     {
         const uint64_t pass = __ballot(top > bound);
         if (!pass) return;
         float from = above(bound);
         if (__builtin_popcountll(pass) >= k) {
+            // Sixteen bits, a bf16's, are near enough; fewer lanes pass a whole number's.
             const uint32_t key[1] = {top > bound ? order_of(top) : 0u};
-            bound = from = float_of(kth(key, k));
+            bound = from = fmaxf(from, float_of(kth<16>(key, k)));
         }
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            if (e % kGroup == 0 && count > kList - kGroup * kWave) {
-                cut();
-                from = fmaxf(from, bound);  // equal ones of this tile may have a lower index than what is listed
+        for (int g = 0; g < G; ++g) {
+            if (!__any(group[g] >= from)) continue;
+#pragma unroll
+            for (int e = g * kGroup; e < min(E, (g + 1) * kGroup); ++e) {
+                if (e % (kRoom / kWave) == 0 && count > longest) {
+                    cut();
+                    from = fmaxf(from, bound);  // equal ones of this tile may have a lower index than what is listed
+                }
+                const bool in = v[e] >= from;
+                const uint64_t mask = __ballot(in);
+                if (!mask) continue;
+                if (in) {
+                    value[count + lanes_before(mask)] = v[e];
+                    index[count + lanes_before(mask)] = index_of(e);
+                }
+                count += __builtin_popcountll(mask);
             }
-            const bool in = v[e] >= from;
-            const uint64_t mask = __ballot(in);
-            if (!mask) continue;
-            if (in) {
-                value[count + lanes_before(mask)] = v[e];
-                index[count + lanes_before(mask)] = index_of(e);
-            }
-            count += __builtin_popcountll(mask);
         }
     }
 };
@@ -255,12 +263,17 @@ __device__ __forceinline__ float logit(const void *p, long i)
     return BF16 ? bf16_bits_to_f32(static_cast<const uint16_t *>(p)[i]) : static_cast<const float *>(p)[i];
 }
 
-__device__ __forceinline__ float largest(const float (&v)[32])
+__device__ __forceinline__ float largest(const float (&v)[32], float (&group)[32 / kGroup])
 {
-    float t = fmaxf(fmaxf(v[0], v[1]), v[2]);
 #pragma unroll
-    for (int e = 3; e + 1 < 32; e += 2) t = fmaxf(fmaxf(v[e], v[e + 1]), t);
-    return fmaxf(t, v[31]);
+    for (int g = 0; g < 32 / kGroup; ++g) {
+        float t = fmaxf(v[g * kGroup], v[g * kGroup + 1]);
+#pragma unroll
+        for (int e = 2; e + 1 < kGroup; e += 2) t = fmaxf(fmaxf(v[g * kGroup + e], v[g * kGroup + e + 1]), t);
+        group[g] = t;
+    }
+    static_assert(kGroup % 2 == 0 && kGroup == 8, "four groups");
+    return fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3]));
 }
 
 template <bool BF16, bool TOP>
@@ -281,14 +294,14 @@ __global__ __launch_bounds__(kThreads) void parts_kernel(LogprobArgs a, int part
     const float c = a.scale * kLog2e;
 
     Sums sums;
-    Best best{values[TOP ? wave : 0], indices[TOP ? wave : 0], a.k};
+    Best best{values[TOP ? wave : 0], indices[TOP ? wave : 0], a.k, max(2 * a.k, kWave)};
     auto edge = [&](int from, int to) {  // up to 64 elements, one a lane
         const float v[1] = {from + lane < to ? logit<BF16>(p, from + lane) : -INFINITY};
         if (from + lane < to) {
             if (v[0] > sums.m) sums.move(v[0], c);
             sums.add(v, c);
         }
-        if (TOP) best.tile(v, v[0], [&](int) { return from + lane; });
+        if (TOP) best.tile(v, v[0], v, [&](int) { return from + lane; });
     };
     if (part == 0 && head) edge(0, head);
     const u32x4 *src = reinterpret_cast<const u32x4 *>(p + (long)head * kBytes);
@@ -314,11 +327,12 @@ __global__ __launch_bounds__(kThreads) void parts_kernel(LogprobArgs a, int part
                     v[i * 4 + c] = __uint_as_float(w[i][c]);
                 }
             }
-        const float top = largest(v);
+        float group[32 / kGroup];
+        const float top = largest(v, group);
         if (top > sums.m) sums.move(top, c);
         sums.add(v, c);
         if (TOP)
-            best.tile(v, top, [&](int e) { return head + (at + e / kVec * kWave) * kVec + e % kVec; });
+            best.tile(v, top, group, [&](int e) { return head + (at + e / kVec * kWave) * kVec + e % kVec; });
     }
     if (part == parts - 1 && tail < a.V) edge(tail, a.V);
 
