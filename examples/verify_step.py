@@ -4,9 +4,9 @@
 
 A step takes a draft tree of each sequence through all layers at once.  Per layer: residual addition and norm, attention of
 the drafts over the paged cache and each other, residual addition and norm, routing, the experts.  Then the longest path
-whose tokens the model would have chosen is accepted and appended to the cache.  `latent` attends over a cache of latent
-rows: its prompts go through the expanded form, its drafts through the absorbed one.  `grouped` has the 8-bit cache of
-grouped-query attention, which takes its prompts in pieces of 64 tokens like long drafts.
+whose tokens the model would have chosen is accepted, gets pages where it needs them, and is appended to the cache; each
+token's log probability is kept.  `latent` attends over a cache of latent rows: its prompts go through the expanded form, its
+drafts through the absorbed one.  `grouped` has the 8-bit cache of grouped-query attention.
 """
 from __future__ import annotations
 
@@ -40,13 +40,29 @@ def heads(x, w):
 
 
 class Pages:
-    """Pages of B sequences of at most `room` tokens, in any order, and the tokens that each has."""
+    """Pages of B sequences of at most `room` tokens each: handed out as the sequences grow, in any order."""
 
     def __init__(self, B, room, page, dev):
         blocks = -(-room // page)
-        self.page, self.count = page, B * blocks
-        self.table = torch.randperm(B * blocks, generator=torch.Generator().manual_seed(0)).int().view(B, blocks).to(dev)
+        self.page, self.count, self.B, self.dev = page, B * blocks, B, dev
+        self.table = torch.zeros(B, blocks, dtype=torch.int32, device=dev)
+        self.free = torch.randperm(B * blocks, generator=torch.Generator().manual_seed(0)).int().to(dev)
+        self.n_free = torch.tensor([B * blocks], dtype=torch.int32, device=dev)
         self.len = torch.zeros(B, dtype=torch.int32, device=dev)
+
+    def grow(self, off, n, keep=None):
+        """Pages for n new tokens (sequence b's are off[b] .. off[b + 1] - 1): their slots and positions.  The old lengths
+        hold until `settle`."""
+        return moe.moe_pages_update(self.len, off, self.table, self.free, self.n_free, self.page, n, keep_len=keep)
+
+    def settle(self, update):
+        self.len, self.n_free = update.new_len, update.n_free
+
+    def end(self, b):
+        """Sequence b's pages are free again."""
+        keep = self.len.clone()
+        keep[b] = 0
+        self.settle(self.grow(torch.zeros(self.B + 1, dtype=torch.int32, device=self.dev), 1, keep))
 
 
 class LatentAttention:
@@ -82,9 +98,8 @@ class LatentAttention:
         o, _ = moe.moe_latent_attn(q, new, off, self.cache, self.pages.table, self.pages.len, self.R, self.scale, mask=mask)
         return heads(o, self.w_v).flatten(1) @ self.w_o
 
-    def append(self, new, off, rows, seq, pos):
-        at = pos.long()
-        self.cache[self.pages.table[seq, at // self.pages.page].long(), at % self.pages.page] = new[rows.long()]
+    def append(self, new, off, rows, slots):
+        moe.moe_latent_append(new, self.cache, slots, rows=rows)
 
 
 class GroupedAttention:
@@ -104,12 +119,16 @@ class GroupedAttention:
         q, k, v = qkv.split([self.H, self.HKV, self.HKV], 1)
         return rotate(q, pos), (rotate(k, pos), v.contiguous())
 
+    def prompt(self, q, new, off, most):
+        o, _ = moe.moe_grouped_prompt(q, *new, off, off, self.scale, max_tokens=most)
+        return o.flatten(1) @ self.w_o
+
     def drafts(self, q, new, off, mask):
         o, _ = moe.moe_cache_attn(q, *new, off, self.k, self.v, self.ks, self.vs, self.pages.table, self.pages.len, self.scale,
                                   mask=mask)
         return o.flatten(1) @ self.w_o
 
-    def append(self, new, off, rows, seq, pos):
+    def append(self, new, off, rows, slots):
         moe.moe_cache_append(*new, off, self.k, self.v, self.ks, self.vs, self.pages.table, self.pages.len, rows=rows)
 
 
@@ -124,6 +143,7 @@ class Model:
         d = self.shape.d
         self.pages = Pages(B, room, 16, self.dev)
         self.embed, self.head = weight(vocab, d, fan=1), weight(d, vocab)
+        self.scores = [[] for _ in range(B)]  # log probability of every chosen token
         self.ones = torch.ones(d, dtype=BF16, device=self.dev)
         make = LatentAttention if kind == "latent" else GroupedAttention
         self.attn = [make(d, self.pages, weight, self.dev) for _ in range(layers)]
@@ -144,37 +164,37 @@ class Model:
         _, y, _, _ = moe.moe_add_rmsnorm(out, self.ones, EPS, residual=h, want_sum=False)
         return (y @ self.head).float(), kept
 
+    def offsets(self, counts):
+        return torch.tensor([0, *torch.tensor(counts).cumsum(0)], dtype=torch.int32, device=self.dev)
+
+    def store(self, kept, rows, off, update):
+        for attn, new in zip(self.attn, kept):
+            attn.append(new, off, rows, update.slots)
+        self.pages.settle(update)
+
     def append(self, kept, rows, counts):
         """Rows of the last forward, counts[b] of them sequence b's, to the caches."""
-        off = torch.tensor([0, *torch.tensor(counts).cumsum(0)], dtype=torch.int32, device=self.dev)
-        seq = torch.repeat_interleave(torch.arange(len(counts), device=self.dev), off.diff().long())
-        pos = self.pages.len[seq] + torch.arange(len(rows), device=self.dev) - off[seq]
-        for attn, new in zip(self.attn, kept):
-            attn.append(new, off, rows, seq, pos)
-        self.pages.len += off.diff()
+        off = self.offsets(counts)
+        self.store(kept, rows, off, self.pages.grow(off, len(rows)))
+
+    def best(self, logits):
+        """Each row's most probable token and its log probability."""
+        r = moe.moe_token_logprobs(logits, k=1)
+        return r.top_idx[:, 0].tolist(), r.top_logprob[:, 0].tolist()
 
     def prompt(self, prompts):
-        """Whole prompts into the cache -> each one's next token."""
-        if isinstance(self.attn[0], LatentAttention):
-            counts = [len(p) for p in prompts]
-            return self._piece(prompts, counts, lambda a, q, n, off: a.prompt(q, n, off, max(counts)))
-        last = [None] * len(prompts)
-        for at in range(0, max(map(len, prompts)), 64):
-            pieces = [p[at:at + 64] for p in prompts]
-            counts = [len(p) for p in pieces]
-            for b, t in enumerate(self._piece(pieces, counts, lambda a, q, n, off: a.drafts(q, n, off, None))):
-                last[b] = t if counts[b] else last[b]
-        return last
-
-    def _piece(self, pieces, counts, attend):
-        off = torch.tensor([0, *torch.tensor(counts).cumsum(0)], dtype=torch.int32, device=self.dev)
-        start = self.pages.len.tolist()
-        tokens = torch.tensor([t for p in pieces for t in p], device=self.dev)
-        pos = torch.tensor([start[b] + i for b, n in enumerate(counts) for i in range(n)], device=self.dev)
-        logits, kept = self.forward(tokens, pos, lambda a, q, n: attend(a, q, n, off))
-        self.append(kept, torch.arange(len(tokens), dtype=torch.int32, device=self.dev), counts)
-        best = logits.argmax(1)
-        return [int(best[max(e - 1, 0)]) for e in off[1:].tolist()]
+        """Whole prompts into the cache (an empty one leaves its sequence as it is) -> each one's next token."""
+        counts = [len(p) for p in prompts]
+        off = self.offsets(counts)
+        update = self.pages.grow(off, sum(counts))
+        tokens = torch.tensor([t for p in prompts for t in p], device=self.dev)
+        logits, kept = self.forward(tokens, update.positions, lambda a, q, n: a.prompt(q, n, off, max(counts)))
+        self.store(kept, None, off, update)
+        best, scores = self.best(logits)
+        for b, e in enumerate(off[1:].tolist()):
+            if counts[b]:
+                self.scores[b].append(scores[e - 1])
+        return [best[max(e - 1, 0)] for e in off[1:].tolist()]
 
     def draft_tree(self, token, depth=3):
         """Tokens, parents and depths of a tree below `token`: two guesses a level by the embedding alone, the better one
@@ -195,12 +215,12 @@ class Model:
             for i, p in enumerate(parent):
                 bits.append((bits[p] if p >= 0 else 0) | 1 << i)
             mask += bits
-        off = torch.tensor([0, *torch.tensor([len(t[0]) for t in trees]).cumsum(0)], dtype=torch.int32, device=self.dev)
+        off = self.offsets([len(t[0]) for t in trees])
         masks = torch.tensor(mask, dtype=torch.int64, device=self.dev)
         tokens = torch.tensor([x for t in trees for x in t[0]], device=self.dev)
         pos = torch.tensor([start[b] + n for b, t in enumerate(trees) for n in t[2]], device=self.dev)
         logits, kept = self.forward(tokens, pos, lambda a, q, n: a.drafts(q, n, off, masks))
-        best, base, rows, counts, out = logits.argmax(1).tolist(), off.tolist(), [], [], []
+        (best, scores), base, rows, counts, out = self.best(logits), off.tolist(), [], [], []
         for b, (toks, parent, _) in enumerate(trees):
             path, at = [0], 0
             while True:
@@ -212,6 +232,7 @@ class Model:
             rows += [base[b] + i for i in path]
             counts.append(len(path))
             out.append([toks[i] for i in path[1:]] + [best[base[b] + at]])
+            self.scores[b] += [scores[base[b] + i] for i in path]
         self.append(kept, torch.tensor(rows, dtype=torch.int32, device=self.dev), counts)
         return out
 
@@ -231,4 +252,5 @@ def decode(kind, lengths=(70, 1, 33), steps=8, seed=0):
 if __name__ == "__main__":
     for which in sys.argv[1:] or ["latent", "grouped"]:
         m, prompts, out = decode(which)
-        print(f"{which}: prompts of {[len(p) for p in prompts]} tokens, 8 verifications, {[len(o) for o in out]} tokens")
+        print(f"{which}: prompts of {[len(p) for p in prompts]} tokens, 8 verifications, {[len(o) for o in out]} tokens of log "
+              f"probability {[round(sum(s) / len(s), 2) for s in m.scores]} on average")

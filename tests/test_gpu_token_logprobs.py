@@ -189,3 +189,23 @@ def test_stream_and_graph():
         g.replay()
         torch.cuda.synchronize()
         check(x, t, 10, 1.0, out)
+
+
+@pytest.mark.parametrize("type", TYPES)
+def test_rows_with_almost_all_probability_on_one_token(type):
+    """Entropy and the token's log probability are as small as what is left to the others, and right to fp32's precision: the
+    exponents' roundings (|x| up to 60: 60 * 4 * 2^-24 of a term), the terms' sums and one rounding of the result."""
+    for N, V, over in ((4, 500, 12), (3, 40000, 25), (2, 130003, 18)):
+        x = fill("normal", N, V, V)
+        x[:, V // 2] = x.amax(1) + over
+        x = x.to(TYPES[type])
+        r = moe.moe_token_logprobs(x.to(DEV), torch.full((N,), V // 2, dtype=torch.int32, device=DEV), k=1)
+        d = x.double()
+        rest = torch.exp(d - d[:, V // 2:V // 2 + 1])
+        rest[:, V // 2] = 0
+        total, mean = rest.sum(1), (rest * (d - d[:, V // 2:V // 2 + 1])).sum(1)
+        log_s = torch.log1p(total)
+        entropy = log_s - mean / (1 + total)
+        rel = 60 * 4 * 2.0 ** -24 + (V / 64 + 200) * 2.0 ** -24
+        for got, want in ((r.logprob, -log_s), (r.top_logprob[:, 0], -log_s), (r.entropy, entropy)):
+            assert ((got.cpu().double() - want).abs() <= rel * want.abs()).all(), (N, V, got, want)
