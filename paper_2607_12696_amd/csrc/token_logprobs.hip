@@ -16,11 +16,13 @@
 // Elements come in ascending order, so what only equals the bound of an earlier
 // tile has k better ones before it.
 // Parts of a row by different wavefronts leave their sums and their k best in
-// order; a second kernel joins the sums and merges the lists, a lane to a part:
-// k times the largest head, the lowest lane among equal ones (its elements come
-// first).
-// What bounds it: memory, for many rows; for few the two launches and the chain
-// of load, bound, list, join.
+// order; they are joined in LDS, or by a second kernel, which merges the lists
+// with a lane to a part: k times the largest head, the lowest lane among equal
+// ones (its elements come first).
+// What bounds it: memory, for many rows (2048 of 200000 in bf16, k = 5: 158 us,
+// 5.2 TB/s; k = 64 250); for few the chain of load, bound, list, join and the
+// launches (4 of 128000, k = 2: 5.5 us, and 4 the join).  Rising logits, of which
+// every tile passes whole, take four times as long as others.
 #include "device.hpp"
 #include "step.hpp"
 
@@ -35,6 +37,8 @@ constexpr int kList = 2 * kWave + kRoom;  // entries of a wavefront's list
 constexpr int kKept = 64;           // most entries that a wavefront leaves
 constexpr int kMinParts = 4096;     // wavefronts that fill the card: 16 a compute unit
 constexpr int kMaxParts = kWave;    // of a row: a lane each when they are joined
+constexpr int kCus = 256, kManyRows = 4 * kCus;
+constexpr int kMostWaves = 16;      // of a workgroup that has a row to itself
 constexpr float kFloor = -1e30f;    // stands for -inf where -inf * 0 must not arise
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
@@ -53,10 +57,10 @@ struct Work {
 };
 
 // Wavefronts of a row: all have the same number of tiles but the last.
-__host__ __device__ inline int parts_of(int N, int V)
+inline int parts_of(int N, int V, int limit)
 {
     const int tiles = (V + kTile - 1) / kTile, want = (kMinParts + N - 1) / N;
-    const int most = want < kMaxParts ? want : kMaxParts, each = (tiles + most - 1) / most;
+    const int most = want < limit ? want : limit, each = (tiles + most - 1) / most;
     return (tiles + each - 1) / each;
 }
 
@@ -276,16 +280,12 @@ __device__ __forceinline__ float largest(const float (&v)[32], float (&group)[32
     return fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3]));
 }
 
+// One wavefront's part of a row.
 template <bool BF16, bool TOP>
-__global__ __launch_bounds__(kThreads) void parts_kernel(LogprobArgs a, int parts, Work out)
+__device__ __forceinline__ void scan(const LogprobArgs &a, int row, int part, int parts, Sums &sums, Best &best)
 {
     constexpr int kVec = BF16 ? 8 : 4, kLoads = 32 / kVec, kBytes = BF16 ? 2 : 4;
-    __shared__ float values[TOP ? kWaves : 1][TOP ? kList : 1];
-    __shared__ int indices[TOP ? kWaves : 1][TOP ? kList : 1];
-    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const long id = (long)blockIdx.x * kWaves + wave;
-    if (id >= (long)a.N * parts) return;
-    const int row = (int)(id / parts), part = (int)(id % parts);
+    const int lane = lane_id();
     const char *p = static_cast<const char *>(a.logits) + row * a.stride * kBytes;
     // The row from its first whole 16 bytes on; what lies before and behind goes element by element.
     const int head = min((int)(-(uintptr_t)p % 16) / kBytes, a.V), vectors = (a.V - head) / kVec;
@@ -293,8 +293,6 @@ __global__ __launch_bounds__(kThreads) void parts_kernel(LogprobArgs a, int part
     const int each = (tiles + parts - 1) / parts, first = min(part * each, tiles), last = min(first + each, tiles);
     const float c = a.scale * kLog2e;
 
-    Sums sums;
-    Best best{values[TOP ? wave : 0], indices[TOP ? wave : 0], a.k, max(2 * a.k, kWave)};
     auto edge = [&](int from, int to) {  // up to 64 elements, one a lane
         const float v[1] = {from + lane < to ? logit<BF16>(p, from + lane) : -INFINITY};
         if (from + lane < to) {
@@ -337,18 +335,7 @@ __global__ __launch_bounds__(kThreads) void parts_kernel(LogprobArgs a, int part
     if (part == parts - 1 && tail < a.V) edge(tail, a.V);
 
     sums.join_lanes(c);
-    if (TOP) {
-        if (best.count > kKept) best.cut();
-        float v;
-        int at;
-        const int rank = best.ranked(v, at);
-        if (rank < a.k) {
-            const long to = ((long)row * a.k + rank) * parts + part;
-            out.values[to] = v;
-            out.indices[to] = at;
-        }
-    }
-    if (lane == 0) out.heads[id] = Head{sums.s, sums.m, sums.a, min(best.count, a.k)};
+    if (TOP && best.count > kKept) best.cut();
 }
 
 // Largest of the lanes' numbers, uniform (lane moves: lane 63 ends with it).
@@ -370,21 +357,15 @@ __device__ __forceinline__ uint32_t largest_of_lanes(uint32_t v)
     return __builtin_amdgcn_readlane(v, kWave - 1);
 }
 
+// A row's results from its parts (head: the lane's part's), by a whole workgroup.  Lists in LDS: entry r of part p at
+// r * parts + p, the values, then the indices.
 template <bool BF16>
-__global__ __launch_bounds__(kThreads) void join_kernel(LogprobArgs a, int parts, Work in)
+__device__ __forceinline__ void finish(const LogprobArgs &a, int row, int parts, const Head &head, const uint32_t *lists)
 {
     constexpr int kBytes = BF16 ? 2 : 4;
-    extern __shared__ uint32_t lists[];  // [k][parts] orders, then [k][parts] indices
-    const int row = blockIdx.x, lane = lane_id(), wave = threadIdx.x / kWave;
+    const int lane = lane_id(), wave = threadIdx.x / kWave, entries = a.k * parts;
     const char *p = static_cast<const char *>(a.logits) + row * a.stride * kBytes;
     const float c = a.scale * kLog2e;
-
-    const Head head = lane < parts ? in.heads[(long)row * parts + lane] : Head{0., kLowest, 0.f, 0};
-    const int entries = a.k * parts;
-    for (int i = threadIdx.x; i < entries; i += blockDim.x) {
-        lists[i] = __float_as_uint(in.values[(long)row * entries + i]);
-        lists[entries + i] = (uint32_t)in.indices[(long)row * entries + i];
-    }
     Sums sums{head.m, head.a, head.s};
     sums.join_lanes(c);
     const bool nothing = sums.s == 0.;  // every logit is -inf
@@ -398,7 +379,6 @@ __global__ __launch_bounds__(kThreads) void join_kernel(LogprobArgs a, int parts
         const int t = a.tokens[(long)row * a.M + i];
         a.logprob[(long)row * a.M + i] = t >= 0 && t < a.V ? logprob(logit<BF16>(p, t)) : -INFINITY;
     }
-    __syncthreads();
     if (!a.k || wave) return;
 
     // Lane r keeps what comes r-th.
@@ -442,37 +422,110 @@ __global__ __launch_bounds__(kThreads) void join_kernel(LogprobArgs a, int parts
     if (a.top_logprob) a.top_logprob[(long)row * a.k + lane] = logprob(v);
 }
 
-}  // namespace
-
-size_t logprobs_workspace(int N)
+template <bool BF16, bool TOP>
+__global__ __launch_bounds__(kThreads) void parts_kernel(LogprobArgs a, int parts, Work out)
 {
-    // parts_of(N, V) <= kMinParts / N + 1 for every V.
-    return ((size_t)kMinParts + N) * (sizeof(Head) + kKept * (sizeof(float) + sizeof(int)));
+    __shared__ float values[TOP ? kWaves : 1][TOP ? kList : 1];
+    __shared__ int indices[TOP ? kWaves : 1][TOP ? kList : 1];
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const long id = (long)blockIdx.x * kWaves + wave;
+    if (id >= (long)a.N * parts) return;
+    const int row = (int)(id / parts), part = (int)(id % parts);
+    Sums sums;
+    Best best{values[TOP ? wave : 0], indices[TOP ? wave : 0], a.k, max(2 * a.k, kWave)};
+    scan<BF16, TOP>(a, row, part, parts, sums, best);
+    if (TOP) {
+        float v;
+        int at;
+        const int rank = best.ranked(v, at);
+        if (rank < a.k) {
+            const long to = ((long)row * a.k + rank) * parts + part;
+            out.values[to] = v;
+            out.indices[to] = at;
+        }
+    }
+    if (lane == 0) out.heads[id] = Head{sums.s, sums.m, sums.a, min(best.count, a.k)};
 }
 
-hipError_t launch_token_logprobs(const LogprobArgs &a, bool bf16, void *workspace, hipStream_t stream)
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void join_kernel(LogprobArgs a, int parts, Work in)
 {
-    const int parts = parts_of(a.N, a.V);
+    extern __shared__ uint32_t lists[];
+    const int row = blockIdx.x, lane = lane_id(), entries = a.k * parts;
+    const Head head = lane < parts ? in.heads[(long)row * parts + lane] : Head{0., kLowest, 0.f, 0};
+    for (int i = threadIdx.x; i < entries; i += blockDim.x) {
+        lists[i] = __float_as_uint(in.values[(long)row * entries + i]);
+        lists[entries + i] = (uint32_t)in.indices[(long)row * entries + i];
+    }
+    __syncthreads();
+    finish<BF16>(a, row, parts, head, lists);
+}
+
+// A row by one workgroup, a part by each of its wavefronts, joined in LDS.
+template <bool BF16, bool TOP>
+__global__ __launch_bounds__(kMostWaves *kWave) void row_kernel(LogprobArgs a, int parts)
+{
+    extern __shared__ double shared[];
+    Head *heads = reinterpret_cast<Head *>(shared);
+    uint32_t *lists = reinterpret_cast<uint32_t *>(heads + parts);
+    float *values = reinterpret_cast<float *>(lists + 2 * a.k * parts);
+    const int row = blockIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    Sums sums;
+    Best best{values + wave * kList, reinterpret_cast<int *>(values + (parts + wave) * kList), a.k, max(2 * a.k, kWave)};
+    scan<BF16, TOP>(a, row, wave, parts, sums, best);
+    if (TOP) {
+        float v;
+        int at;
+        const int rank = best.ranked(v, at);
+        if (rank < a.k) {
+            lists[rank * parts + wave] = __float_as_uint(v);
+            lists[(a.k + rank) * parts + wave] = (uint32_t)at;
+        }
+    }
+    if (lane == 0) heads[wave] = Head{sums.s, sums.m, sums.a, min(best.count, a.k)};
+    __syncthreads();
+    finish<BF16>(a, row, parts, lane < parts ? heads[lane] : Head{0., kLowest, 0.f, 0}, lists);
+}
+
+template <bool BF16, bool TOP>
+hipError_t launch(const LogprobArgs &a, void *workspace, hipStream_t stream)
+{
+    const int waves = parts_of(a.N, a.V, kMostWaves), tiles = (a.V + kTile - 1) / kTile;
+    // A workgroup a row, in one launch, where each has a compute unit and each wavefront a tile (60 rows of 20000, k = 20: 14.6 us,
+    // in two launches 18), or where there are enough rows for even shares of the card (2048 of 200000, k = 5: 158 and 160).
+    // Between, some compute units would have a row more than others (300 rows of 50000, k = 20: 36 and 24).
+    if (a.N >= kManyRows || (a.N <= kCus && tiles <= kMostWaves)) {
+        const size_t lds = waves * (sizeof(Head) + (TOP ? 8 * a.k + 8 * kList : 0));
+        row_kernel<BF16, TOP><<<(unsigned)a.N, waves * kWave, lds, stream>>>(a, waves);
+        return hipGetLastError();
+    }
+    const int parts = parts_of(a.N, a.V, kMaxParts);
     const long n = (long)a.N * parts;
     Work w;
     w.heads = static_cast<Head *>(workspace);
     w.values = reinterpret_cast<float *>(w.heads + n);
     w.indices = reinterpret_cast<int *>(w.values + n * a.k);
-    const unsigned grid = (unsigned)((n + kWaves - 1) / kWaves);
-    if (bf16) {
-        if (a.k) parts_kernel<true, true><<<grid, kThreads, 0, stream>>>(a, parts, w);
-        else parts_kernel<true, false><<<grid, kThreads, 0, stream>>>(a, parts, w);
-    } else {
-        if (a.k) parts_kernel<false, true><<<grid, kThreads, 0, stream>>>(a, parts, w);
-        else parts_kernel<false, false><<<grid, kThreads, 0, stream>>>(a, parts, w);
-    }
+    parts_kernel<BF16, TOP><<<(unsigned)((n + kWaves - 1) / kWaves), kThreads, 0, stream>>>(a, parts, w);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     // One wavefront does the merging; more of them bring long lists.
     const int entries = a.k * parts, threads = entries > 4 * kWave ? kThreads : kWave;
-    if (bf16) join_kernel<true><<<(unsigned)a.N, threads, entries * 8, stream>>>(a, parts, w);
-    else join_kernel<false><<<(unsigned)a.N, threads, entries * 8, stream>>>(a, parts, w);
+    join_kernel<BF16><<<(unsigned)a.N, threads, entries * 8, stream>>>(a, parts, w);
     return hipGetLastError();
+}
+
+}  // namespace
+
+size_t logprobs_workspace(int N)
+{
+    // parts_of(N, V, most) <= kMinParts / N + 1 for every V.
+    return ((size_t)kMinParts + N) * (sizeof(Head) + kKept * (sizeof(float) + sizeof(int)));
+}
+
+hipError_t launch_token_logprobs(const LogprobArgs &a, bool bf16, void *workspace, hipStream_t stream)
+{
+    if (bf16) return a.k ? launch<true, true>(a, workspace, stream) : launch<true, false>(a, workspace, stream);
+    return a.k ? launch<false, true>(a, workspace, stream) : launch<false, false>(a, workspace, stream);
 }
 
 }  // namespace ecospec
