@@ -87,6 +87,43 @@ __device__ __forceinline__ int lanes_before(uint64_t mask)
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
 }
 
+// Lane moves within a register (row shifts, then row totals into the later rows), a few cycles each: lane 63 ends with f over
+// all lanes.
+template <int CTRL, int ROW_MASK, class T>
+__device__ __forceinline__ T lane_move(T v, T none)
+{
+    if constexpr (sizeof(T) == 8) {
+        const u32x2 x = __builtin_bit_cast(u32x2, v), n = __builtin_bit_cast(u32x2, none);
+        return __builtin_bit_cast(T, u32x2{lane_move<CTRL, ROW_MASK>(x[0], n[0]), lane_move<CTRL, ROW_MASK>(x[1], n[1])});
+    } else {
+        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v), CTRL, ROW_MASK,
+                                                                 0xf, false));
+    }
+}
+
+template <class T, class F>
+__device__ __forceinline__ T along_lanes(T v, T none, F f)
+{
+    v = f(v, lane_move<0x111, 0xf>(v, none));  // row_shr:1
+    v = f(v, lane_move<0x112, 0xf>(v, none));  // row_shr:2
+    v = f(v, lane_move<0x114, 0xf>(v, none));  // row_shr:4
+    v = f(v, lane_move<0x118, 0xf>(v, none));  // row_shr:8
+    v = f(v, lane_move<0x142, 0xa>(v, none));  // row_bcast:15 into rows 1 and 3
+    v = f(v, lane_move<0x143, 0xc>(v, none));  // row_bcast:31 into rows 2 and 3
+    return v;
+}
+
+template <class T>
+__device__ __forceinline__ T last_lane(T v)
+{
+    if constexpr (sizeof(T) == 8) {
+        const u32x2 x = __builtin_bit_cast(u32x2, v);
+        return __builtin_bit_cast(T, u32x2{last_lane(x[0]), last_lane(x[1])});
+    } else {
+        return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), kWave - 1));
+    }
+}
+
 // S is held in 64 bits: where one token has almost all of the probability, S is 1 and a little, and ln S, the token's log
 // probability and most of the entropy are that little.
 struct Sums {
@@ -100,18 +137,12 @@ struct Sums {
         s *= f;
         m = to;
     }
-    __device__ __forceinline__ void join(Sums o, float c)
-    {
-        const float top = fmaxf(m, o.m);
-        move(top, c);
-        o.move(top, c);
-        s += o.s;
-        a += o.a;
-    }
+    // Over the wavefront: the largest reference, then plain sums.
     __device__ __forceinline__ void join_lanes(float c)
     {
-#pragma unroll
-        for (int x = 32; x >= 1; x >>= 1) join(Sums{__shfl_xor(m, x, kWave), __shfl_xor(a, x, kWave), __shfl_xor(s, x, kWave)}, c);
+        move(last_lane(along_lanes(m, kLowest, [](float x, float y) { return fmaxf(x, y); })), c);
+        a = last_lane(along_lanes(a, 0.f, [](float x, float y) { return x + y; }));
+        s = last_lane(along_lanes(s, 0., [](double x, double y) { return x + y; }));
     }
     // E logits, none above m: two chains of additions.
     template <int E>
@@ -338,25 +369,6 @@ __device__ __forceinline__ void scan(const LogprobArgs &a, int row, int part, in
     if (TOP && best.count > kKept) best.cut();
 }
 
-// Largest of the lanes' numbers, uniform (lane moves: lane 63 ends with it).
-template <int CTRL, int ROW_MASK>
-__device__ __forceinline__ uint32_t max_step(uint32_t v)
-{
-    const uint32_t o = __builtin_amdgcn_update_dpp(0u, v, CTRL, ROW_MASK, 0xf, false);
-    return o > v ? o : v;
-}
-
-__device__ __forceinline__ uint32_t largest_of_lanes(uint32_t v)
-{
-    v = max_step<0x111, 0xf>(v);  // row_shr:1
-    v = max_step<0x112, 0xf>(v);  // row_shr:2
-    v = max_step<0x114, 0xf>(v);  // row_shr:4
-    v = max_step<0x118, 0xf>(v);  // row_shr:8
-    v = max_step<0x142, 0xa>(v);  // row_bcast:15 into rows 1 and 3
-    v = max_step<0x143, 0xc>(v);  // row_bcast:31 into rows 2 and 3
-    return __builtin_amdgcn_readlane(v, kWave - 1);
-}
-
 // A row's results from its parts (head: the lane's part's), by a whole workgroup.  Lists in LDS: entry r of part p at
 // r * parts + p, the values, then the indices.
 template <bool BF16>
@@ -387,7 +399,7 @@ __device__ __forceinline__ void finish(const LogprobArgs &a, int row, int parts,
     auto order_at = [&](int r) { return r < head.count ? order_of(__uint_as_float(lists[r * parts + lane])) : 0u; };
     uint32_t key = order_at(0), second = order_at(1);
     for (; count < a.k; ++count) {
-        const uint32_t win = largest_of_lanes(key);
+        const uint32_t win = last_lane(along_lanes(key, 0u, [](uint32_t x, uint32_t y) { return x > y ? x : y; }));
         if (!win) break;
         const int from = (int)__builtin_ctzll(__ballot(key == win));
         const int place = __builtin_amdgcn_readlane(next, from) * parts + from;
