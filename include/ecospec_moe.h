@@ -577,7 +577,7 @@ moe_status_t moe_cache_attn(const moe_cache_t *cache, const moe_drafts_t *drafts
 
 /*
  * The two ends of a decoding step: pages and prompts in, log probabilities
- * out.
+ * out.  A call runs on its stream's device, whichever is the current one.
  */
 
 /* Pages of B sequences, for caches paged as in moe_latent_cache_t (one update
@@ -605,10 +605,11 @@ typedef struct {
  *     the returned pages of all sequences, in order, go behind the free ones;
  *   where want > have, the sequence takes want - have pages, from the end of
  *     that list, in order of the sequences;
- *   a sequence of want > max_blocks takes nothing, and so does one whose last
- *     page, counted with all that the sequences before it ask for, is past
- *     what the list holds: it is refused and stays as it was, none of its
- *     tokens kept back or added.
+ *   a sequence of want > max_blocks is refused and counts for nothing; one
+ *   whose last page, counted with all that the sequences before it ask for,
+ *   is past what the list holds, is refused, and so are those behind it that
+ *   ask for any.  A refused sequence stays as it was, with cache_len[b] tokens
+ *   and its pages.
  *   token_offsets [B+1]: from 0 to at most N, none decreasing.
  *   block_table, free_pages: updated in place (what free_pages holds from
  *   *n_free_out on is left over and means nothing).
@@ -707,7 +708,7 @@ typedef enum {
  * Arithmetic: fp32, the exponentials and their sums relative to the largest
  * logits so far; the logits are read once.  Deterministic.
  * Limits: 1 <= N <= 2^22, 1 <= V <= 2^24, 0 <= k <= min(V, 64), 0 <= M <= 65536,
- * N * M <= 2^30, scale finite and > 0.  Two kernels.
+ * N * M <= 2^30, scale finite and > 0.  One or two kernels.
  */
 moe_status_t moe_token_logprobs_workspace_size(int N, size_t *bytes);
 moe_status_t moe_token_logprobs(const void *logits, int dtype, int64_t stride, int N, int V, float scale,

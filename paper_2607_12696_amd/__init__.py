@@ -591,6 +591,14 @@ def _typed_ptr(t, dtype, what: str, shape) -> int:
     return t.data_ptr()
 
 
+def _one_device(t, *others) -> None:
+    """All tensors that are given are on t's device: a call runs there."""
+    device = t.get_device()
+    for o in others:
+        if o is not None and o.get_device() != device:
+            raise ValueError("the tensors of a call must be on one device")
+
+
 def _int32_ptr(t, what: str, *shape) -> int:
     return _typed_ptr(t, _torch().int32, what, shape)
 
@@ -777,6 +785,7 @@ def moe_pages_update(cache_len, token_offsets, block_table, free_pages, n_free, 
     else:
         to = (ptr(out.new_len, i32, "new_len", per), ptr(out.n_free, i32, "n_free", one), ptr(out.refused, i32, "refused", one),
               ptr(out.slots, torch.int64, "slots", tokens), ptr(out.positions, i32, "positions", tokens))
+    _one_device(block_table, cache_len, free_pages, n_free, keep_len, token_offsets, out.slots, out.new_len)
     pool = moe_page_pool_t(B, n_pages, page, blocks, ptr(block_table, i32, "block_table", (B, blocks)),
                            ptr(cache_len, i32, "cache_len", per), ptr(free_pages, i32, "free_pages", (n_pages,)),
                            ptr(n_free, i32, "n_free", one))
@@ -794,6 +803,7 @@ def moe_latent_append(kv_new, pages, slots, rows=None) -> None:
     n_pages, page, width = pages.shape
     n_rows = kv_new.shape[0]
     N, = slots.shape
+    _one_device(pages, kv_new, slots, rows)
     _check("moe_latent_append", lib().moe_latent_append(
         _typed_ptr(pages, torch.bfloat16, "pages", (n_pages, page, width)), n_pages, page, width - 64, 64,
         _typed_ptr(kv_new, torch.bfloat16, "kv_new", (n_rows, width)), n_rows,
@@ -828,6 +838,7 @@ def moe_grouped_prompt(q, k, v, q_offsets, kv_offsets, scale: float, max_tokens:
     if workspace is None:
         workspace = torch.empty(moe_grouped_prompt_workspace_size(D), dtype=torch.uint8, device=q.device)
     off = (B + 1,)
+    _one_device(q, k, v, q_offsets, kv_offsets, o, lse, workspace)
     a = moe_grouped_prompt_t(N, M, B, H, Hkv, D, N if max_tokens is None else max_tokens,
                              _typed_ptr(q_offsets, torch.int32, "q_offsets", off), _typed_ptr(kv_offsets, torch.int32, "kv_offsets", off),
                              qp, kp, vp, qs, qh, ks, kh, vs, vh, scale)
@@ -892,6 +903,7 @@ def moe_token_logprobs(logits, tokens=None, k: int = 0, scale: float = 1.0, out:
             (out.top_idx, i32, "top_idx", (N, k)), (out.top_logprob, f32, "top_logprob", (N, k)))]
     if workspace is None:
         workspace = torch.empty(moe_token_logprobs_workspace_size(N), dtype=torch.uint8, device=dev)
+    _one_device(logits, tokens, workspace, out.logprob, out.lse, out.entropy, out.top_idx, out.top_logprob)
     _check("moe_token_logprobs", lib().moe_token_logprobs(
         logits.data_ptr(), MOE_F32 if dtype is f32 else MOE_BF16, stride, N, V, scale, ptr(tokens, i32, "tokens", shape) if M else None,
         M, k, *to, _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(logits)))

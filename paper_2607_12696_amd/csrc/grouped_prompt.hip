@@ -43,6 +43,9 @@ __device__ __forceinline__ float max2(float a, float b)  // without the copies t
     return r;
 }
 
+// A number that is the same in all lanes, in a scalar register.
+__device__ __forceinline__ float uniform(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }
+
 // The chunks of a row block of `tiles` tiles.
 __device__ __forceinline__ int chunks_of(int tiles, int most) { return min(most, max(tiles / kMinTiles, 1)); }
 
@@ -167,8 +170,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void prompt_kernel(Group
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
     uint32_t odd_tiles = 0;  // edge tiles with infinities or NaN among the values
-    const float scale2 = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-126f);  // not zero: it meets infinities
-    const float slack = kSlack / scale2;
+    const float scale2 = uniform(fmaxf(fabsf(a.scale) * kLog2e, 0x1p-126f));  // not zero: it meets infinities
+    const float slack = uniform(kSlack / scale2);
     uint32_t k_at[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) k_at[i] = (uint32_t)(col * 128 + ((2 * i + half) ^ (col >> 1 & 7)) * 16);

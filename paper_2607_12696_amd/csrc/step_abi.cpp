@@ -21,6 +21,24 @@ moe_status_t from_hip(hipError_t e)
     return MOE_ERR_HIP;
 }
 
+// The stream's device is the current one for the launches of a call: a kernel is looked up on the current device.
+struct OnDeviceOf {
+    int was = -1;
+    explicit OnDeviceOf(void *stream)
+    {
+        int now = 0;
+        hipDevice_t of = 0;
+        if (!stream || hipGetDevice(&now) != hipSuccess || hipStreamGetDevice((hipStream_t)stream, &of) != hipSuccess) return;
+        if (now != of && hipSetDevice(of) == hipSuccess) was = now;
+    }
+    ~OnDeviceOf()
+    {
+        if (was >= 0) (void)hipSetDevice(was);
+    }
+    OnDeviceOf(const OnDeviceOf &) = delete;
+    OnDeviceOf &operator=(const OnDeviceOf &) = delete;
+};
+
 bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
 bool page_ok(int page) { return page == 16 || page == 32 || page == 64 || page == 128; }
@@ -67,6 +85,7 @@ moe_status_t moe_pages_update(const moe_page_pool_t *p, const int32_t *keep_len,
     a.refused = refused;
     a.slots = slots;
     a.positions = positions;
+    const OnDeviceOf device(stream);
     return from_hip(ecospec::launch_pages_update(a, (hipStream_t)stream));
 }
 
@@ -86,6 +105,7 @@ moe_status_t moe_latent_append(void *pages, int n_pages, int page, int r, int p,
     a.kv_new = static_cast<const uint16_t *>(kv_new);
     a.rows = rows;
     a.slots = slots;
+    const OnDeviceOf device(stream);
     return from_hip(ecospec::launch_latent_append(a, (hipStream_t)stream));
 }
 
@@ -137,6 +157,7 @@ moe_status_t moe_grouped_prompt(const moe_grouped_prompt_t *p, void *o, float *l
     a.scale = p->scale;
     a.o = static_cast<uint16_t *>(o);
     a.lse = lse;
+    const OnDeviceOf device(stream);
     return from_hip(ecospec::launch_grouped_prompt(a, p->D, workspace, (hipStream_t)stream));
 }
 
@@ -175,6 +196,7 @@ moe_status_t moe_token_logprobs(const void *logits, int dtype, int64_t stride, i
     a.entropy = entropy;
     a.top_logprob = top_logprob;
     a.top_idx = top_idx;
+    const OnDeviceOf device(stream);
     return from_hip(ecospec::launch_token_logprobs(a, dtype == MOE_BF16, workspace, (hipStream_t)stream));
 }
 

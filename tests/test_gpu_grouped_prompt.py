@@ -225,3 +225,27 @@ def test_stream_and_graph(nq, nk):
         g.replay()
         torch.cuda.synchronize()
         check(c, o, lse, some_rows(c, rng, most=20))
+
+
+def test_calls_at_once():
+    """Calls on two streams that overlap, each with a workspace of its own: as one after the other."""
+    cases = [case([5, 9], [6000, 3000], 16, 2, 128, seed=31), case([300], [300], 8, 8, 64, seed=32), case([3], [9000], 8, 1, 64, seed=33)]
+    inputs = [[c[x].to(DEV) for x in ("q", "kv", "qo", "ko")] + [c["scale"], max(c["nq"])] for c in cases]
+
+    def call(i, out):
+        q, kv, qo, ko, scale, most = inputs[i]
+        out.append(moe.moe_grouped_prompt(q, kv[:, 0], kv[:, 1], qo, ko, scale, max_tokens=most))
+
+    want = []
+    for i in range(3):
+        call(i, want)
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(3)], []
+    for _ in range(8):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                call(i, got)
+    torch.cuda.synchronize()
+    for n, (o, lse) in enumerate(got):
+        rows = sum(cases[n % 3]["nq"])
+        assert torch.equal(o[:rows], want[n % 3][0][:rows]) and torch.equal(lse[:rows], want[n % 3][1][:rows])

@@ -172,3 +172,23 @@ def test_graph_of_a_step():
         for i, (slot, _) in enumerate(tokens):
             expect[slot] = new[i].cpu()
         assert torch.equal(cache.view(-1, 576).cpu(), expect)
+
+
+def test_a_graph_and_an_eager_call_share_nothing():
+    """The same pool updated by a replayed graph and eagerly, in turn: each from the counts that it is given."""
+    table, frees, total = pool([20, 40], 6, 5, 16, 3)
+    t, f, n = dev(table), dev(frees + [0] * (total - len(frees))), dev([len(frees)])
+    ln, off = dev([20, 40]), dev([0, 13, 20])
+    out = moe.moe_pages_update(ln, off, t, f, n, 16, 24)
+    first = [x.clone() for x in (out.new_len, out.n_free, out.refused, out.slots, out.positions, t, f)]
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        moe.moe_pages_update(ln, off, t, f, n, 16, 24, out=out)
+    for _ in range(3):
+        out.slots.fill_(5)
+        g.replay()
+        eager = moe.moe_pages_update(ln, off, t, f, n, 16, 24)
+        torch.cuda.synchronize()
+        for r in (out, eager):
+            assert all(torch.equal(x, y) for x, y in zip(first, (r.new_len, r.n_free, r.refused, r.slots, r.positions, t, f)))

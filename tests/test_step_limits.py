@@ -116,6 +116,22 @@ def test_binding_refuses_wrong_tensors():
             call()
 
 
+class OnDevice:
+    """Stands for a tensor of some device where there is none."""
+
+    def __init__(self, device):
+        self.device = device
+
+    def get_device(self):
+        return self.device
+
+
+def test_binding_refuses_tensors_of_several_devices():
+    moe._one_device(OnDevice(1), OnDevice(1), None, OnDevice(1))
+    with pytest.raises(ValueError):
+        moe._one_device(OnDevice(1), None, OnDevice(1), OnDevice(0))
+
+
 # ----------------------------------------------------------------------------- the oracle's own pins
 
 def test_oracle_pages():
