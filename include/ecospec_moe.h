@@ -578,6 +578,8 @@ moe_status_t moe_cache_attn(const moe_cache_t *cache, const moe_drafts_t *drafts
 /*
  * The two ends of a decoding step: pages and prompts in, log probabilities
  * out.  A call runs on its stream's device, whichever is the current one.
+ * Nothing that a call writes may overlap anything else that it is given
+ * (MOE_ERR_INVALID_ARG).
  */
 
 /* Pages of B sequences, for caches paged as in moe_latent_cache_t (one update
@@ -705,8 +707,8 @@ typedef enum {
  *   workspace: device scratch of moe_token_logprobs_workspace_size bytes,
  *   256-byte aligned; its contents on entry do not matter.  The size for N rows
  *   is enough for every call of no more rows.
- * Arithmetic: fp32, the exponentials and their sums relative to the largest
- * logits so far; the logits are read once.  Deterministic.
+ * Arithmetic: exponentials in fp32, relative to the largest logits so far, their
+ * sum in fp64; the logits are read once.  Deterministic.
  * Limits: 1 <= N <= 2^22, 1 <= V <= 2^24, 0 <= k <= min(V, 64), 0 <= M <= 65536,
  * N * M <= 2^30, scale finite and > 0.  One or two kernels.
  */

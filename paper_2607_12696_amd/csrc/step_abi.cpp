@@ -41,6 +41,31 @@ struct OnDeviceOf {
 
 bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
+// A range of memory that a call reads or writes; null: none.
+struct Range {
+    const void *at;
+    size_t bytes;
+};
+
+bool overlap(const Range &x, const Range &y)
+{
+    const uintptr_t a = (uintptr_t)x.at, b = (uintptr_t)y.at;
+    return x.at && y.at && a < b + y.bytes && b < a + x.bytes;
+}
+
+// Whether something that a call writes overlaps anything else of it.
+template <size_t OUT, size_t IN>
+bool any_overlap(const Range (&out)[OUT], const Range (&in)[IN])
+{
+    for (size_t i = 0; i < OUT; ++i) {
+        for (const Range &x : in)
+            if (overlap(out[i], x)) return true;
+        for (size_t j = 0; j < i; ++j)
+            if (overlap(out[i], out[j])) return true;
+    }
+    return false;
+}
+
 bool page_ok(int page) { return page == 16 || page == 32 || page == 64 || page == 128; }
 
 constexpr int kMaxTokens = 1 << 30;        // of one page update
@@ -64,10 +89,13 @@ moe_status_t moe_pages_update(const moe_page_pool_t *p, const int32_t *keep_len,
     if (p->B < 1 || p->B > ecospec::kMaxSequences || p->n_pages < 1 || p->max_blocks < 1 || !page_ok(p->page))
         return MOE_ERR_INVALID_ARG;
     if ((long)p->max_blocks * p->page > 1L << 30 || N < 1 || N > kMaxTokens) return MOE_ERR_INVALID_ARG;
-    // Workgroups read the counts while others write the new ones.
-    if (new_len == p->cache_len || new_len == keep_len || n_free_out == p->n_free || n_free_out == refused)
-        return MOE_ERR_INVALID_ARG;
     if (!aligned(slots, 8)) return MOE_ERR_INVALID_ARG;
+    // Workgroups read the counts while others write the new ones.
+    const size_t B = p->B, n = N;
+    const Range out[] = {{new_len, B * 4}, {n_free_out, 4}, {refused, 4}, {slots, n * 8}, {positions, n * 4},
+                         {p->block_table, B * p->max_blocks * 4}, {p->free_pages, (size_t)p->n_pages * 4}};
+    const Range in[] = {{p->cache_len, B * 4}, {keep_len, B * 4}, {token_offsets, (B + 1) * 4}, {p->n_free, 4}};
+    if (any_overlap(out, in)) return MOE_ERR_INVALID_ARG;
     ecospec::PagesArgs a{};
     a.B = p->B;
     a.N = N;
@@ -95,8 +123,12 @@ moe_status_t moe_latent_append(void *pages, int n_pages, int page, int r, int p,
     if (!pages || !kv_new || !slots || n_pages < 1 || !page_ok(page) || r < 1 || p < 0 || N < 1 || n_rows < 1)
         return MOE_ERR_INVALID_ARG;
     if (!rows && n_rows < N) return MOE_ERR_INVALID_ARG;
-    if (pages == kv_new || !aligned(pages, 16) || !aligned(kv_new, 16) || !aligned(slots, 8)) return MOE_ERR_INVALID_ARG;
+    if (!aligned(pages, 16) || !aligned(kv_new, 16) || !aligned(slots, 8)) return MOE_ERR_INVALID_ARG;
     if (r != 512 || p != 64 || N > kMaxAppended) return MOE_ERR_UNSUPPORTED;
+    const size_t row = (size_t)(r + p) * 2;
+    const Range out[] = {{pages, (size_t)n_pages * page * row}};
+    const Range in[] = {{kv_new, n_rows * row}, {rows, (size_t)N * 4}, {slots, (size_t)N * 8}};
+    if (any_overlap(out, in)) return MOE_ERR_INVALID_ARG;
     ecospec::RowsArgs a{};
     a.N = N;
     a.n_rows = n_rows;
@@ -123,7 +155,7 @@ moe_status_t moe_grouped_prompt(const moe_grouped_prompt_t *p, void *o, float *l
     if (!p || !o || !workspace || !p->q || !p->k || !p->v || !p->q_offsets || !p->kv_offsets) return MOE_ERR_INVALID_ARG;
     if (p->N < 1 || p->M < 1 || p->B < 1 || p->B > ecospec::kMaxSequences || p->max_tokens < 1) return MOE_ERR_INVALID_ARG;
     if (p->Hkv < 1 || p->Hkv > 256 || p->H < 1 || p->H > kMaxHeads || p->H % p->Hkv || p->D < 1) return MOE_ERR_INVALID_ARG;
-    if (!isfinite(p->scale) || o == p->q || o == p->k || o == p->v) return MOE_ERR_INVALID_ARG;
+    if (!isfinite(p->scale)) return MOE_ERR_INVALID_ARG;
     const void *ptr[] = {p->q, p->k, p->v, o};
     for (const void *x : ptr)
         if (!aligned(x, 16)) return MOE_ERR_INVALID_ARG;
@@ -136,6 +168,14 @@ moe_status_t moe_grouped_prompt(const moe_grouped_prompt_t *p, void *o, float *l
     const int most = p->max_tokens < p->N ? p->max_tokens : p->N;
     if ((long)p->N * p->H > kMaxPromptRows || (long)p->B * p->H * most > kMaxPromptRows) return MOE_ERR_UNSUPPORTED;  // the grid
     if (workspace_bytes < ecospec::grouped_prompt_workspace(p->D)) return MOE_ERR_WORKSPACE;
+    auto spans = [&](const void *x, int n, int64_t stride, int heads, int64_t head) {
+        return Range{x, ((size_t)(n - 1) * stride + (size_t)(heads - 1) * head + p->D) * 2};
+    };
+    const size_t rows = (size_t)p->N * p->H, table = (size_t)(p->B + 1) * 4;
+    const Range out[] = {{o, rows * p->D * 2}, {lse, rows * 4}, {workspace, ecospec::grouped_prompt_workspace(p->D)}};
+    const Range in[] = {spans(p->q, p->N, p->q_stride, p->H, p->q_head), spans(p->k, p->M, p->k_stride, p->Hkv, p->k_head),
+                        spans(p->v, p->M, p->v_stride, p->Hkv, p->v_head), {p->q_offsets, table}, {p->kv_offsets, table}};
+    if (any_overlap(out, in)) return MOE_ERR_INVALID_ARG;
     ecospec::GroupedPromptArgs a{};
     a.N = p->N;
     a.M = p->M;
@@ -173,7 +213,8 @@ moe_status_t moe_token_logprobs(const void *logits, int dtype, int64_t stride, i
                                 int32_t *top_idx, float *top_logprob, void *workspace, size_t workspace_bytes,
                                 void *stream)
 {
-    if (!logits || !workspace || N < 1 || N > kMaxLogitRows || V < 1 || V > kMaxVocabulary || stride < V) return MOE_ERR_INVALID_ARG;
+    if (!logits || !workspace || N < 1 || N > kMaxLogitRows || V < 1 || V > kMaxVocabulary || stride < V)
+        return MOE_ERR_INVALID_ARG;
     if (dtype != MOE_F32 && dtype != MOE_BF16) return MOE_ERR_INVALID_ARG;
     if (!isfinite(scale) || !(scale > 0.f)) return MOE_ERR_INVALID_ARG;
     if (k < 0 || k > kMaxTop || k > V || M < 0 || M > kMaxGiven || (long)N * M > 1L << 30) return MOE_ERR_INVALID_ARG;
@@ -182,6 +223,11 @@ moe_status_t moe_token_logprobs(const void *logits, int dtype, int64_t stride, i
     if (!logprob && !lse && !entropy && !top_idx) return MOE_ERR_INVALID_ARG;
     if (!aligned(logits, dtype == MOE_BF16 ? 2 : 4) || !aligned(workspace, 256)) return MOE_ERR_INVALID_ARG;
     if (workspace_bytes < ecospec::logprobs_workspace(N)) return MOE_ERR_WORKSPACE;
+    const size_t n = N;
+    const Range out[] = {{logprob, n * M * 4}, {lse, n * 4}, {entropy, n * 4}, {top_idx, n * k * 4}, {top_logprob, n * k * 4},
+                         {workspace, ecospec::logprobs_workspace(N)}};
+    const Range in[] = {{logits, ((n - 1) * (size_t)stride + V) * (dtype == MOE_BF16 ? 2 : 4)}, {tokens, n * M * 4}};
+    if (any_overlap(out, in)) return MOE_ERR_INVALID_ARG;
     ecospec::LogprobArgs a{};
     a.logits = logits;
     a.stride = stride;

@@ -100,6 +100,45 @@ def test_logprobs_workspace_serves_fewer_rows():
     assert moe.lib().moe_token_logprobs_workspace_size(4, None) == BAD
 
 
+@pytest.mark.parametrize("change", [
+    dict(new_len=0x10004), dict(new_len=0x20004), dict(new_len=0x30004), dict(n_out=0x40000), dict(refused=0x50004),
+    dict(slots=0x60000 - 8), dict(pos=0x70000 - 4 * 7), dict(block_table=0x10000), dict(free_pages=0x60000 - 4 * 7),
+    dict(pos=0x50008 - 32), dict(refused=0x10000), dict(free_pages=0x60004)])
+def test_pages_rejects_overlaps(change):
+    """Two sequences, four blocks each, eight pages and tokens: a buffer moved so that its first or last element is another's."""
+    at = dict(cache_len=0x10000, keep=0x20000, off=0x30000, n_free=0x40000, new_len=0x50000, n_out=0x50008, refused=0x5000c,
+              block_table=0x60000, free_pages=0x70000, slots=0x80000, pos=0x90000)
+    at.update(change)
+    assert pages(**at) == BAD
+
+
+@pytest.mark.parametrize("change", [dict(new=FAKE + 4 * 16 * 1152 - 16), dict(new=FAKE - 8 * 1152 + 16), dict(rows=FAKE + 8),
+                                    dict(slots=FAKE - 56)])
+def test_latent_append_rejects_overlaps(change):
+    at = dict(new=FAKE << 8, slots=FAKE << 4)
+    at.update(change)
+    assert append(**at) == BAD
+
+
+@pytest.mark.parametrize("change", [
+    dict(o=0x20000 + 2 * (3 * 256 + 3 * 64 + 56)), dict(o=0x20000 - 2 * (4 * 4 * 64 - 8)), dict(o=0x30000 + 2 * (3 * 128 + 64 + 56)),
+    dict(o=0x40000 + 64), dict(lse=0x20000 + 16), dict(lse=0x10000 + 16), dict(lse=0x50004), dict(ws=0x20000), dict(ws=0x10000 + 256),
+    dict(lse=0x1000004)])
+def test_grouped_prompt_rejects_overlaps(change):
+    at = dict(o=0x10000, q=0x20000, k=0x30000, v=0x40000, q_offsets=0x50000, kv_offsets=0x60000, ws=0x1000000)
+    at.update(change)
+    assert prompt(**at) == BAD
+
+
+@pytest.mark.parametrize("change", [
+    dict(lp=0x10000 + 4 * (3 * 100 + 99)), dict(lse=0x10000 - 12), dict(ent=0x20000 + 28), dict(idx=0x40000 + 12), dict(top=0x60000 + 44),
+    dict(top=0x10000), dict(ws=0x10000), dict(lse=0x1000010), dict(lp=0x20000)])
+def test_logprobs_rejects_overlaps(change):
+    at = dict(logits=0x10000, tokens=0x20000, lp=0x30000, lse=0x40000, ent=0x50000, idx=0x60000, top=0x70000, ws=0x1000000)
+    at.update(change)
+    assert logprobs(**at) == BAD
+
+
 def test_binding_refuses_wrong_tensors():
     """The Python entry points check types and shapes before the library is called; none of these is on the device."""
     i, x = torch.zeros(4, dtype=torch.int32), torch.zeros(3, 4, 64, dtype=torch.bfloat16)
