@@ -599,6 +599,17 @@ def _one_device(t, *others) -> None:
             raise ValueError("the tensors of a call must be on one device")
 
 
+def _enqueue(name: str, fn, t, *args) -> None:
+    """fn(*args, stream) on the current stream of t's device.  A default stream's handle is null and means the current device's."""
+    stream = _stream(t)
+    if not stream:
+        cuda, device = _torch().cuda, t.get_device()
+        if cuda.current_device() != device:
+            with cuda.device(device):
+                return _check(name, fn(*args, stream))
+    _check(name, fn(*args, stream))
+
+
 def _int32_ptr(t, what: str, *shape) -> int:
     return _typed_ptr(t, _torch().int32, what, shape)
 
@@ -771,7 +782,8 @@ def moe_pages_update(cache_len, token_offsets, block_table, free_pages, n_free, 
 
     cache_len, keep_len [B], token_offsets [B + 1], n_free [1] int32; block_table [B, blocks] and free_pages [n_pages] int32
     are updated in place.  N: entries of slots and positions, at least the new tokens.  The counts are not changed: the new
-    ones are new_len and n_free of the result, whose tensors are those of `out` where it is given."""
+    ones are new_len and n_free of the result, whose tensors are those of `out` where it is given (slots and positions may be
+    None there)."""
     torch = _torch()
     i32, ptr = torch.int32, _typed_ptr
     B, blocks = block_table.shape
@@ -783,15 +795,17 @@ def moe_pages_update(cache_len, token_offsets, block_table, free_pages, n_free, 
         out = PageUpdate(parts[0], parts[1], parts[2], slots, parts[3])
         to = at, at + 4 * B, at + 4 * B + 4, slots.data_ptr(), at + 4 * B + 8
     else:
-        to = (ptr(out.new_len, i32, "new_len", per), ptr(out.n_free, i32, "n_free", one), ptr(out.refused, i32, "refused", one),
-              ptr(out.slots, torch.int64, "slots", tokens), ptr(out.positions, i32, "positions", tokens))
-    _one_device(block_table, cache_len, free_pages, n_free, keep_len, token_offsets, out.slots, out.new_len)
+        to = [None if t is None else ptr(t, kind, what, of) for t, kind, what, of in (
+            (out.new_len, i32, "new_len", per), (out.n_free, i32, "n_free", one), (out.refused, i32, "refused", one),
+            (out.slots, torch.int64, "slots", tokens), (out.positions, i32, "positions", tokens))]
+        _one_device(block_table, out.new_len, out.n_free, out.refused, out.slots, out.positions)
+    _one_device(block_table, cache_len, free_pages, n_free, keep_len, token_offsets)
     pool = moe_page_pool_t(B, n_pages, page, blocks, ptr(block_table, i32, "block_table", (B, blocks)),
                            ptr(cache_len, i32, "cache_len", per), ptr(free_pages, i32, "free_pages", (n_pages,)),
                            ptr(n_free, i32, "n_free", one))
-    _check("moe_pages_update", lib().moe_pages_update(
-        C.byref(pool), None if keep_len is None else ptr(keep_len, i32, "keep_len", per),
-        ptr(token_offsets, i32, "token_offsets", (B + 1,)), N, *to, _stream(block_table)))
+    _enqueue("moe_pages_update", lib().moe_pages_update, block_table,
+             C.byref(pool), None if keep_len is None else ptr(keep_len, i32, "keep_len", per),
+             ptr(token_offsets, i32, "token_offsets", (B + 1,)), N, *to)
     return out
 
 
@@ -804,11 +818,11 @@ def moe_latent_append(kv_new, pages, slots, rows=None) -> None:
     n_rows = kv_new.shape[0]
     N, = slots.shape
     _one_device(pages, kv_new, slots, rows)
-    _check("moe_latent_append", lib().moe_latent_append(
-        _typed_ptr(pages, torch.bfloat16, "pages", (n_pages, page, width)), n_pages, page, width - 64, 64,
-        _typed_ptr(kv_new, torch.bfloat16, "kv_new", (n_rows, width)), n_rows,
-        None if rows is None else _typed_ptr(rows, torch.int32, "rows", (N,)), N, _typed_ptr(slots, torch.int64, "slots", (N,)),
-        _stream(pages)))
+    ptr = _typed_ptr
+    _enqueue("moe_latent_append", lib().moe_latent_append, pages,
+             ptr(pages, torch.bfloat16, "pages", (n_pages, page, width)), n_pages, page, width - 64, 64,
+             ptr(kv_new, torch.bfloat16, "kv_new", (n_rows, width)), n_rows,
+             None if rows is None else ptr(rows, torch.int32, "rows", (N,)), N, ptr(slots, torch.int64, "slots", (N,)))
 
 
 @functools.cache
@@ -840,10 +854,10 @@ def moe_grouped_prompt(q, k, v, q_offsets, kv_offsets, scale: float, max_tokens:
     off = (B + 1,)
     _one_device(q, k, v, q_offsets, kv_offsets, o, lse, workspace)
     a = moe_grouped_prompt_t(N, M, B, H, Hkv, D, N if max_tokens is None else max_tokens,
-                             _typed_ptr(q_offsets, torch.int32, "q_offsets", off), _typed_ptr(kv_offsets, torch.int32, "kv_offsets", off),
-                             qp, kp, vp, qs, qh, ks, kh, vs, vh, scale)
-    _check("moe_grouped_prompt", lib().moe_grouped_prompt(C.byref(a), op, lp, _dev_ptr(workspace, "workspace"),
-                                                          workspace.numel() * workspace.element_size(), _stream(q)))
+                             _typed_ptr(q_offsets, torch.int32, "q_offsets", off),
+                             _typed_ptr(kv_offsets, torch.int32, "kv_offsets", off), qp, kp, vp, qs, qh, ks, kh, vs, vh, scale)
+    _enqueue("moe_grouped_prompt", lib().moe_grouped_prompt, q, C.byref(a), op, lp, _dev_ptr(workspace, "workspace"),
+             workspace.numel() * workspace.element_size())
     return o, lse
 
 
@@ -904,9 +918,10 @@ def moe_token_logprobs(logits, tokens=None, k: int = 0, scale: float = 1.0, out:
     if workspace is None:
         workspace = torch.empty(moe_token_logprobs_workspace_size(N), dtype=torch.uint8, device=dev)
     _one_device(logits, tokens, workspace, out.logprob, out.lse, out.entropy, out.top_idx, out.top_logprob)
-    _check("moe_token_logprobs", lib().moe_token_logprobs(
-        logits.data_ptr(), MOE_F32 if dtype is f32 else MOE_BF16, stride, N, V, scale, ptr(tokens, i32, "tokens", shape) if M else None,
-        M, k, *to, _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(logits)))
+    _enqueue("moe_token_logprobs", lib().moe_token_logprobs, logits,
+             logits.data_ptr(), MOE_F32 if dtype is f32 else MOE_BF16, stride, N, V, scale,
+             ptr(tokens, i32, "tokens", shape) if M else None, M, k, *to, _dev_ptr(workspace, "workspace"),
+             workspace.numel() * workspace.element_size())
     return out
 
 

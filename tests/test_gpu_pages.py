@@ -69,6 +69,26 @@ def test_single_tokens_and_page_ends():
                 check([old], [old], [new], page, 12, 6, extra=0 if new else 1)
 
 
+@pytest.mark.parametrize("without", [("slots",), ("positions",), ("slots", "positions")])
+def test_what_is_not_asked_for(without):
+    table, frees, total = pool([20, 3], 6, 5, 16, 1)
+
+    def call(out):
+        t_dev, f_dev = dev(table), torch.zeros(total, dtype=torch.int32, device=DEV)
+        f_dev[:5] = dev(frees)
+        r = moe.moe_pages_update(dev([20, 3]), dev([0, 15, 40]), t_dev, f_dev, dev([5]), 16, 41, out=out)
+        return r, t_dev
+
+    full, t_full = call(None)
+    out = moe.PageUpdate(*(torch.full_like(x, -7) for x in (full.new_len, full.n_free, full.refused, full.slots, full.positions)))
+    for name in without:
+        setattr(out, name, None)
+    part, t_part = call(out)
+    assert part is out and torch.equal(t_full, t_part) and full.refused.item() == 0
+    for name in ("new_len", "n_free", "refused", "slots", "positions"):
+        assert getattr(part, name) is None if name in without else torch.equal(getattr(part, name), getattr(full, name))
+
+
 def test_ends_and_begins():
     assert check([100, 40, 0, 17, 64], [100, 0, 0, 17, 10], [1, 0, 30, 0, 90], 16, 20, 4) == 0
     assert check([100, 40, 0, 17, 64], [1000, 0, 5, 17, 10], [1, 0, 30, 0, 90], 16, 20, 4, keep_null=False) == 0  # more kept than there is

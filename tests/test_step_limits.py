@@ -171,6 +171,32 @@ def test_binding_refuses_tensors_of_several_devices():
         moe._one_device(OnDevice(1), None, OnDevice(1), OnDevice(0))
 
 
+@pytest.mark.parametrize("stream,current,entered", [(0, 0, []), (0, 1, [0]), (5, 0, []), (5, 1, [])])
+def test_a_default_stream_makes_its_device_the_current_one(monkeypatch, stream, current, entered):
+    calls, devices = [], []
+
+    class Device:
+        def __init__(self, device):
+            self.device = device
+
+        def __enter__(self):
+            devices.append(self.device)
+
+        def __exit__(self, *_):
+            devices.append("left")
+
+    monkeypatch.setattr(moe, "_stream", lambda t: stream)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current)
+    monkeypatch.setattr(torch.cuda, "device", Device)
+
+    def fn(*args):
+        calls.append((args, list(devices)))
+        return OK
+
+    moe._enqueue("fn", fn, OnDevice(0), 7, 8)
+    assert calls == [((7, 8, stream), entered)] and devices == entered + ["left"] * len(entered)
+
+
 # ----------------------------------------------------------------------------- the oracle's own pins
 
 def test_oracle_pages():
