@@ -599,10 +599,15 @@ def _one_device(t, *others) -> None:
             raise ValueError("the tensors of a call must be on one device")
 
 
+@functools.cache
+def _several_devices() -> bool:
+    return _torch().cuda.device_count() > 1
+
+
 def _enqueue(name: str, fn, t, *args) -> None:
     """fn(*args, stream) on the current stream of t's device.  A default stream's handle is null and means the current device's."""
     stream = _stream(t)
-    if not stream:
+    if not stream and _several_devices():
         cuda, device = _torch().cuda, t.get_device()
         if cuda.current_device() != device:
             with cuda.device(device):

@@ -11,11 +11,17 @@
 //   values (rows of 64 bytes: half a read is 256 in a row).  One barrier a step.
 //   Products, maximum, exponentials and sums of a tile follow each other in a wavefront; what overlaps them is the other
 //   wavefronts of its SIMD, of other workgroups, so registers are kept for four of them with heads of 64 and three with 128.
-//   (Two, each with three tiles under way at once, a piece of the exponentials behind each product, and 176 and 248
-//   registers: 100 and 575 us in the first two cases below.  64 rows a wavefront, one a SIMD, halve the LDS reads, but one
-//   wavefront issues an instruction every seven cycles at best: 143 and 580.)
 //   Where there are few row blocks, each one's keys are cut into chunks, a workgroup each, whose sums join_prompt_kernel
 //   adds up in order.
+//   Measured: one prompt of 6007 tokens, 64 heads on 4 of 128, 525 us, 1.13 PFLOP/s (a bf16 product of 8192^3: 1.415): the
+//   matrix cores are busy 60% of the cycles and the vector unit issues in half of them, at 1.8 GHz, which the power leaves
+//   (operands of zeros run at 2.2); six prompts of 563 to 1201 tokens, 64 heads on 8 of 64, 84 us: the vector unit (five
+//   instructions a weight, half the products of a head of 128 to hide them), and wavefronts that end unevenly; 7 tokens over
+//   4008 keys, 64 heads on 4 of 128, 13 us and 4.1 of the join: a chain of offsets, queries, first tile, four tiles at 1.2 us
+//   (a lone wavefront's latency), parts; loads two and three steps ahead, or two and four tiles a step, did not shorten it.
+//   With two wavefronts a SIMD, each with three tiles under way at once and a piece of the exponentials behind each product
+//   (176 and 248 registers), the first two took 575 and 100 us; with 64 rows a wavefront, one a SIMD, half the LDS reads,
+//   580 and 143: one wavefront issues an instruction every seven cycles at best.
 #include "attn_plan.hpp"
 #include "step.hpp"
 
@@ -25,6 +31,7 @@ namespace {
 constexpr int kKeys = 32, kWaves = 4, kThreads = kWaves * kWave, kRows = 32 * kWaves;
 constexpr int kSlots = 2 * kCus;  // most workgroups of a call whose keys are cut
 constexpr int kMinTiles = 4;      // of a chunk
+constexpr int kJoinWaves = 8;
 constexpr float kSlack = 8.f;  // powers of two that weights may pass 1 by before their reference maximum moves
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
@@ -82,6 +89,7 @@ __device__ __forceinline__ uint32_t to_bf16x2(float lo, float hi)  // one conver
 {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
 }
+
 // D: width of a head; KT: key tiles a barrier; SPLIT: keys are cut into chunks.
 template <int D, int KT, bool SPLIT>
 __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void prompt_kernel(GroupedPromptArgs a, int blocks, int most_chunks,
@@ -185,7 +193,9 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void prompt_kernel(Group
         for (int i = 0; i < 16; ++i) s[i] = 0.f;
         {
             bf16x8 ring[kRing];
-            auto key = [&](int st) { ring[st % kRing] = *reinterpret_cast<const bf16x8 *>(kt + k_at[st % 4] + st / 4 * (kKeys * 128)); };
+            auto key = [&](int st) {
+                ring[st % kRing] = *reinterpret_cast<const bf16x8 *>(kt + k_at[st % 4] + st / 4 * (kKeys * 128));
+            };
 #pragma unroll
             for (int st = 0; st < kRing - 1; ++st) key(st);
 #pragma unroll
@@ -248,7 +258,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void prompt_kernel(Group
 #pragma unroll
         for (int n = 0; n < 2 * kTiles; ++n) {
             if (n + kRing - 1 < 2 * kTiles) value(n + kRing - 1);
-            o[n % kTiles] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[n % kRing], __builtin_bit_cast(bf16x8, p[n / kTiles]), o[n % kTiles], 0, 0, 0);
+            const bf16x8 weights = __builtin_bit_cast(bf16x8, p[n / kTiles]);
+            o[n % kTiles] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[n % kRing], weights, o[n % kTiles], 0, 0, 0);
         }
     };
     // Tiles t .. t + KT - 1, in this buffer.
@@ -280,11 +291,18 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void prompt_kernel(Group
         for (int i = 0; i < KT; ++i)
             if (KT == 1 || t + i < tiles) tile(t + i, lds.k[buffer][i], lds.v[buffer][i]);
     };
+    if (SPLIT) {
+        // Few steps, whose first costs its instructions' way to the compute unit: one copy of them (4 to 8 tiles a workgroup, a
+        // call of 18.5 to 21.9 us becomes 18.1 to 21.2; in long runs two copies are 3% faster).
 #pragma unroll 1
-    for (int t = 0; t < tiles; t += 2 * KT) {
-        step(t, 0);
-        if (t + KT >= tiles) break;
-        step(t + KT, 1);
+        for (int t = 0, buffer = 0; t < tiles; t += KT, buffer ^= 1) step(t, buffer);
+    } else {
+#pragma unroll 1
+        for (int t = 0; t < tiles; t += 2 * KT) {
+            step(t, 0);
+            if (t + KT >= tiles) break;
+            step(t + KT, 1);
+        }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing is on its way to LDS when the workgroup ends
 
@@ -335,54 +353,80 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void prompt_kernel(Group
 }
 
 // Adds up the chunks of a row block: a workgroup has 32 rows by 8 elements, what registers 4 i .. 4 i + 3 of one element tile
-// of the accumulators hold; each wavefront takes every fourth chunk.  (7 tokens over 4008 keys, 31 chunks: 64 rows' groups a
-// workgroup, all chunks one after the other, 23 us.)
+// of the accumulators hold; each of its wavefronts takes every eighth chunk, four of them together, in one pass with a running
+// reference maximum.  What bounds it: latency (offsets, one read for 32 chunks, barrier).  7 tokens over 4008 keys, 31 chunks,
+// 8 MB: 4.1 us (with the references read first, behind a barrier of their own, 6.4).  The whole call for 3 tokens over 30003
+// keys, 8 heads on one, 234 chunks: 17.1 us (by four wavefronts 20.4; eight chunks together, or 16 wavefronts, are no better
+// here and 5 us worse for 50 tokens over 20050 keys, 64 heads on 4, where 52).
 template <int D>
-__global__ __launch_bounds__(kThreads) void join_prompt_kernel(GroupedPromptArgs a, int blocks, int most_chunks, PromptParts parts)
+__global__ __launch_bounds__(kJoinWaves *kWave) void join_prompt_kernel(GroupedPromptArgs a, int blocks, int most_chunks,
+                                                                        PromptParts parts)
 {
     constexpr int kGroups = D / 32 * 4;
-    __shared__ float tops[kWaves][32];
-    __shared__ f32x4 sums[kWaves - 1][kWave];
-    __shared__ float totals[kWaves - 1][kWave];
+    constexpr int kTogether = 4;  // chunks
+    __shared__ f32x4 sums[kJoinWaves - 1][kWave];
+    __shared__ float2 totals[kJoinWaves - 1][kWave];
     const int group = blockIdx.x % kGroups, of = blockIdx.x / kGroups % kWaves, pb = blockIdx.x / (kGroups * kWaves);
     const Block blk(a, pb / blocks, pb % blocks, kRows);
     const int chunks = chunks_of(blk.tiles, most_chunks), lane = lane_id(), wave = threadIdx.x / kWave;
     const int row = blk.row0 + of * 32 + lane % 32;
     if (chunks == 1 || blk.row0 + of * 32 >= blk.rows) return;
     const float2 *ml = parts.ml + (long)pb * most_chunks * kRows + of * 32 + lane % 32;
-    const f32x4 *o = reinterpret_cast<const f32x4 *>(parts.o) + (((long)pb * most_chunks * kWaves + of) * kGroups + group) * kWave + lane;
+    const long first = ((long)pb * most_chunks * kWaves + of) * kGroups + group;
+    const f32x4 *o = reinterpret_cast<const f32x4 *>(parts.o) + first * kWave + lane;
     constexpr long kStep = kWaves * kGroups * kWave;
-    float top = -INFINITY;
-#pragma unroll 8
-    for (int c = wave; c < chunks; c += kWaves) top = fmaxf(top, ml[c * kRows].x);
-    if (lane < 32) tops[wave][lane] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, tops[w][lane % 32]);
-    const float base = top == -INFINITY ? 0.f : top;
-    float total = 0.f;
+    float top = -INFINITY, base = 0.f, total = 0.f;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int c = wave; c < chunks; c += kWaves) {
-        const f32x4 v = o[c * kStep];
-        const float2 part = ml[c * kRows];
-        const float f = __builtin_amdgcn_exp2f(part.x - base);
-        total = fmaf(part.y, f, total);
+    auto reach = [&](float to) {  // a reference maximum of at least `to`
+        const float now = fmaxf(top, to), next = now == -INFINITY ? 0.f : now;
+        const float down = __builtin_amdgcn_exp2f((top == -INFINITY ? next : top) - next);
+        total *= down;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) sum[n] *= down;
+        top = now;
+        base = next;
+    };
+    auto add = [&](float m, float l, const f32x4 &v) {
+        const float f = __builtin_amdgcn_exp2f(m - base);
+        total = fmaf(l, f, total);
 #pragma unroll
         for (int n = 0; n < 4; ++n) sum[n] = fmaf(v[n], f, sum[n]);
+    };
+#pragma unroll 1
+    for (int c0 = wave; c0 < chunks; c0 += kTogether * kJoinWaves) {
+        float2 part[kTogether];
+        f32x4 v[kTogether];
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i) {
+            const int c = min(c0 + i * kJoinWaves, chunks - 1);
+            part[i] = ml[c * kRows];
+            v[i] = o[c * kStep];
+        }
+        float most = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i) {
+            if (c0 + i * kJoinWaves >= chunks) {  // the last one again
+                part[i] = float2{-INFINITY, 0.f};
+                v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+            most = fmaxf(most, part[i].x);
+        }
+        reach(most);
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i) add(part[i].x, part[i].y, v[i]);
     }
     if (wave) {
         sums[wave - 1][lane] = sum;
-        totals[wave - 1][lane] = total;
+        totals[wave - 1][lane] = float2{top, total};
     }
     __syncthreads();
     if (wave || row >= blk.rows) return;
+    float most = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kWaves - 1; ++w) {
-        total += totals[w][lane];
+    for (int w = 0; w < kJoinWaves - 1; ++w) most = fmaxf(most, totals[w][lane].x);
+    reach(most);
 #pragma unroll
-        for (int n = 0; n < 4; ++n) sum[n] += sums[w][lane][n];
-    }
+    for (int w = 0; w < kJoinWaves - 1; ++w) add(totals[w][lane].x, totals[w][lane].y, sums[w][lane]);
     const float inv = total == 0.f ? 0.f : 1.f / total;
     const long at = (long)(blk.q0 + row / blk.G) * a.H + blk.hk * blk.G + row % blk.G;
     *reinterpret_cast<u32x2 *>(a.o + at * D + 8 * group + lane / 32 * 4) =
@@ -406,14 +450,16 @@ hipError_t launch(const GroupedPromptArgs &a, void *workspace, hipStream_t strea
     // 53 tokens and keys: a second launch that joins nothing, 5.8 us.)
     const long room = kSlots / ((long)pairs * blocks), cut = 2L * a.M / ((long)a.B * kKeys * kMinTiles);
     const int chunks = (int)(room < cut ? room : cut);
+    const int groups = pairs * blocks, join_groups = groups * kWaves * (D / 8);
+    constexpr int KT = kTilesAStep<D>;
     if (chunks > 1) {
-        prompt_kernel<D, kTilesAStep<D>, true><<<(unsigned)(pairs * blocks * chunks), kThreads, 0, stream>>>(a, blocks, chunks, parts);
+        prompt_kernel<D, KT, true><<<(unsigned)(groups * chunks), kThreads, 0, stream>>>(a, blocks, chunks, parts);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        join_prompt_kernel<D><<<(unsigned)(pairs * blocks * kWaves * (D / 8)), kThreads, 0, stream>>>(a, blocks, chunks, parts);
+        join_prompt_kernel<D><<<(unsigned)join_groups, kJoinWaves * kWave, 0, stream>>>(a, blocks, chunks, parts);
         return hipGetLastError();
     }
-    prompt_kernel<D, kTilesAStep<D>, false><<<(unsigned)((long)pairs * blocks), kThreads, 0, stream>>>(a, blocks, 1, parts);
+    prompt_kernel<D, KT, false><<<(unsigned)groups, kThreads, 0, stream>>>(a, blocks, 1, parts);
     return hipGetLastError();
 }
 

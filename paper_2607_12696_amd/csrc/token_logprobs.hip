@@ -96,8 +96,8 @@ __device__ __forceinline__ T lane_move(T v, T none)
         const u32x2 x = __builtin_bit_cast(u32x2, v), n = __builtin_bit_cast(u32x2, none);
         return __builtin_bit_cast(T, u32x2{lane_move<CTRL, ROW_MASK>(x[0], n[0]), lane_move<CTRL, ROW_MASK>(x[1], n[1])});
     } else {
-        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v), CTRL, ROW_MASK,
-                                                                 0xf, false));
+        const int to = __builtin_bit_cast(int, none), from = __builtin_bit_cast(int, v);
+        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(to, from, CTRL, ROW_MASK, 0xf, false));
     }
 }
 
@@ -503,8 +503,8 @@ template <bool BF16, bool TOP>
 hipError_t launch(const LogprobArgs &a, void *workspace, hipStream_t stream)
 {
     const int waves = parts_of(a.N, a.V, kMostWaves), tiles = (a.V + kTile - 1) / kTile;
-    // A workgroup a row, in one launch, where each has a compute unit and each wavefront a tile (60 rows of 20000, k = 20: 14.6 us,
-    // in two launches 18), or where there are enough rows for even shares of the card (2048 of 200000, k = 5: 158 and 160).
+    // A workgroup a row, in one launch, where each has a compute unit and each wavefront a tile (60 rows of 20000, k = 20:
+    // 14.6 us, in two launches 18), or where there are enough rows for even shares of the card (2048 of 200000, k = 5: 158 and 160).
     // Between, some compute units would have a row more than others (300 rows of 50000, k = 20: 36 and 24).
     if (a.N >= kManyRows || (a.N <= kCus && tiles <= kMostWaves)) {
         const size_t lds = waves * (sizeof(Head) + (TOP ? 8 * a.k + 8 * kList : 0));

@@ -186,6 +186,7 @@ def test_a_default_stream_makes_its_device_the_current_one(monkeypatch, stream, 
             devices.append("left")
 
     monkeypatch.setattr(moe, "_stream", lambda t: stream)
+    monkeypatch.setattr(moe, "_several_devices", lambda: True)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: current)
     monkeypatch.setattr(torch.cuda, "device", Device)
 
