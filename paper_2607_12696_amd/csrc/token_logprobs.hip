@@ -37,8 +37,8 @@ constexpr int kList = 2 * kWave + kRoom;  // entries of a wavefront's list
 constexpr int kKept = 64;           // most entries that a wavefront leaves
 constexpr int kMinParts = 4096;     // wavefronts that fill the card: 16 a compute unit
 constexpr int kMaxParts = kWave;    // of a row: a lane each when they are joined
-constexpr int kCus = 256, kManyRows = 4 * kCus;
-constexpr int kMostWaves = 16;      // of a workgroup that has a row to itself
+constexpr int kCus = 256, kManyRows = 2 * kCus;
+constexpr int kMostWaves = 16;      // of a workgroup that has a row to itself (waves_of)
 constexpr float kFloor = -1e30f;    // stands for -inf where -inf * 0 must not arise
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
@@ -56,12 +56,23 @@ struct Work {
     int *indices;     // [N][k][parts]
 };
 
-// Wavefronts of a row: all have the same number of tiles but the last.
-inline int parts_of(int N, int V, int limit)
+// Wavefronts of a row of `tiles` tiles, at most `most`: all have the same number of tiles but the last.
+inline int parts_of(int tiles, int most)
 {
-    const int tiles = (V + kTile - 1) / kTile, want = (kMinParts + N - 1) / N;
-    const int most = want < limit ? want : limit, each = (tiles + most - 1) / most;
+    const int each = (tiles + most - 1) / most;
     return (tiles + each - 1) / each;
+}
+
+// Wavefronts of a workgroup that has a row to itself: the most with which all rows' workgroups are there at once, of the 16
+// wavefronts a compute unit that registers leave room for.  (2048 rows of 200000, k = 5: two, 157 us; one workgroup more than
+// there is room for waits for all others: 2047 rows by three 185.  Five spread unevenly over four SIMDs: 700 rows 91, by four 73.)
+inline int waves_of(int N)
+{
+    for (int w : {16, 8, 4, 3, 2})
+        if (N <= kCus * (16 / w)) return w;
+    // Twice what three have room for (2100 rows of 200000: 186 us, by one wavefront 221); then the least joining (3000 rows of
+    // 50000, k = 20: 97, by two 113, by four 125; of 200000, k = 5, 236 to 248).
+    return N <= 2 * kCus * (16 / 3) ? 3 : 1;
 }
 
 // Order of a float as an unsigned number; -0 as +0; no NaN.
@@ -502,16 +513,17 @@ __global__ __launch_bounds__(kMostWaves *kWave) void row_kernel(LogprobArgs a, i
 template <bool BF16, bool TOP>
 hipError_t launch(const LogprobArgs &a, void *workspace, hipStream_t stream)
 {
-    const int waves = parts_of(a.N, a.V, kMostWaves), tiles = (a.V + kTile - 1) / kTile;
-    // A workgroup a row, in one launch, where each has a compute unit and each wavefront a tile (60 rows of 20000, k = 20:
-    // 14.6 us, in two launches 18), or where there are enough rows for even shares of the card (2048 of 200000, k = 5: 158 and 160).
-    // Between, some compute units would have a row more than others (300 rows of 50000, k = 20: 36 and 24).
-    if (a.N >= kManyRows || (a.N <= kCus && tiles <= kMostWaves)) {
+    const int tiles = (a.V + kTile - 1) / kTile, most = waves_of(a.N);
+    // A workgroup a row, in one launch, where each wavefront has a tile (60 rows of 20000, k = 20: 14.6 us, in two launches 18),
+    // or where there are rows enough for them to fill the card (1000 of 200000, k = 5: 88 and 109 us; 512 of 50000, k = 20: 35 and
+    // 38).  With fewer the parts of a row are more than a workgroup's wavefronts (300 of 50000, k = 20: 34 and 25).
+    if (a.N >= kManyRows || tiles <= most) {
+        const int waves = parts_of(tiles, most);
         const size_t lds = waves * (sizeof(Head) + (TOP ? 8 * a.k + 8 * kList : 0));
         row_kernel<BF16, TOP><<<(unsigned)a.N, waves * kWave, lds, stream>>>(a, waves);
         return hipGetLastError();
     }
-    const int parts = parts_of(a.N, a.V, kMaxParts);
+    const int want = kMinParts / a.N, parts = parts_of(tiles, want < kMaxParts ? want : kMaxParts);
     const long n = (long)a.N * parts;
     Work w;
     w.heads = static_cast<Head *>(workspace);
@@ -530,7 +542,7 @@ hipError_t launch(const LogprobArgs &a, void *workspace, hipStream_t stream)
 
 size_t logprobs_workspace(int N)
 {
-    // parts_of(N, V, most) <= kMinParts / N + 1 for every V.
+    // At most kMinParts parts, of at least one a row.
     return ((size_t)kMinParts + N) * (sizeof(Head) + kKept * (sizeof(float) + sizeof(int)));
 }
 

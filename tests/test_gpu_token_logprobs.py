@@ -142,6 +142,17 @@ def test_many_rows_and_few():
         assert all(torch.equal(getattr(r, n), getattr(again, n)) for n in ("logprob", "lse", "entropy", "top_idx", "top_logprob"))
 
 
+@pytest.mark.parametrize("V", [9, 4097, 19999])
+def test_as_many_rows_as_workgroups_and_one_more(V):
+    """Row counts at which another number of wavefronts takes a row."""
+    whole = fill("ties", 2600, V, V).to(torch.bfloat16).to(DEV)
+    for N in (256, 257, 511, 512, 513, 1023, 1024, 1025, 1280, 1281, 2048, 2049, 2560, 2561):
+        print(f"logprobs rows N={N} V={V}", flush=True)
+        x = whole[-N:]
+        t = given(N, V, 1, N)
+        check(x, t, 6, 1.0, moe.moe_token_logprobs(x, t, k=6), [0, N // 2, N - 1])
+
+
 def test_forms_of_the_call():
     x = fill("normal", 6, 3000, 1).to(DEV)
     t = given(6, 3000, 4, 1)
