@@ -29,8 +29,11 @@ namespace ecospec {
 namespace {
 
 constexpr int kKeys = 32, kWaves = 4, kThreads = kWaves * kWave, kRows = 32 * kWaves;
-constexpr int kSlots = 2 * kCus;  // most workgroups of a call whose keys are cut
-constexpr int kMinTiles = 4;      // of a chunk
+// Most workgroups of a call whose keys are cut: all that registers leave room for, if chunks are long; else two a compute unit.
+template <int D>
+constexpr int kSlots = (D == 64 ? 4 : 3) * kCus;
+constexpr int kFewSlots = 2 * kCus;
+constexpr int kMinTiles = 4, kLongTiles = 96;  // of a chunk
 constexpr int kJoinWaves = 8;
 constexpr float kSlack = 8.f;  // powers of two that weights may pass 1 by before their reference maximum moves
 
@@ -445,12 +448,16 @@ hipError_t launch(const GroupedPromptArgs &a, void *workspace, hipStream_t strea
     const long rows = (long)a.max_tokens * (a.H / a.Hkv);
     const int pairs = a.B * a.Hkv, blocks = (int)((rows + kRows - 1) / kRows);
     char *w = static_cast<char *>(workspace);
-    const PromptParts parts{reinterpret_cast<float2 *>(w), reinterpret_cast<float *>(w + kSlots * kRows * sizeof(float2))};
+    const PromptParts parts{reinterpret_cast<float2 *>(w), reinterpret_cast<float *>(w + kSlots<D> * kRows * sizeof(float2))};
+    const long groups = (long)pairs * blocks, tiles = a.M / ((long)a.B * kKeys);  // of the average sequence
+    // Chunks that fill the card, if they are long beside their sums (64 heads on 8 of 64, 20000 keys behind: 400 tokens 174 us, 208
+    // in the fewer, 600 270 and 351, but 800 383 and 364; 32 on 8 of 128, 50000 behind: 700 tokens 613 and 743), else few (64 on 4 of
+    // 128, 20000 behind: 16 tokens 29 us, for three workgroups a compute unit 33, 200 tokens 158 and 170; 32 on 8 of 128, 4000
+    // behind: 1200 tokens uncut 123, in two chunks 145).
+    const long full = kSlots<D> / groups, room = tiles >= kLongTiles * full ? full : kFewSlots / groups;
     // The longest sequence's keys are known on the device only; it is taken to have twice the average.  (40 sequences of up to
     // 53 tokens and keys: a second launch that joins nothing, 5.8 us.)
-    const long room = kSlots / ((long)pairs * blocks), cut = 2L * a.M / ((long)a.B * kKeys * kMinTiles);
-    const int chunks = (int)(room < cut ? room : cut);
-    const int groups = pairs * blocks, join_groups = groups * kWaves * (D / 8);
+    const int chunks = (int)min(room, 2 * tiles / kMinTiles), join_groups = (int)groups * kWaves * (D / 8);
     constexpr int KT = kTilesAStep<D>;
     if (chunks > 1) {
         prompt_kernel<D, KT, true><<<(unsigned)(groups * chunks), kThreads, 0, stream>>>(a, blocks, chunks, parts);
@@ -465,7 +472,10 @@ hipError_t launch(const GroupedPromptArgs &a, void *workspace, hipStream_t strea
 
 }  // namespace
 
-size_t grouped_prompt_workspace(int D) { return (size_t)kSlots * kRows * (sizeof(float2) + D * sizeof(float)); }
+size_t grouped_prompt_workspace(int D)
+{
+    return (size_t)(D == 64 ? kSlots<64> : kSlots<128>) * kRows * (sizeof(float2) + D * sizeof(float));
+}
 
 hipError_t launch_grouped_prompt(const GroupedPromptArgs &a, int D, void *workspace, hipStream_t stream)
 {

@@ -87,7 +87,8 @@ def test_lengths(H, Hkv, D):
 
 @pytest.mark.parametrize("nq,nk,H,Hkv,D", [([2500], [2500], 8, 2, 128), ([1900, 3], [2111, 1500], 16, 2, 64), ([100], [30000], 16, 1, 128),
                                            ([5], [70000], 8, 8, 64), ([2], [60000], 4, 1, 128),
-                                           ([40, 2, 17], [9000, 11, 20000], 20, 4, 128)])
+                                           ([40, 2, 17], [9000, 11, 20000], 20, 4, 128), ([600], [20600], 64, 8, 64),
+                                           ([300], [20301], 64, 4, 128)])
 def test_long(nq, nk, H, Hkv, D):
     c = case(nq, nk, H, Hkv, D, seed=3)
     check(c, *run(c), some_rows(c, np.random.default_rng(2), most=60))
