@@ -11,18 +11,20 @@
 // The alternatives: a wavefront holds a bound below which nothing can be among
 // its k best, and a list in LDS of what has passed it.  A tile of 32 elements a
 // lane costs one maximum and one comparison (the maximum is needed anyway);
-// where k lanes or more pass, the k-th largest of the lanes' maxima is a better
-// bound, found bit by bit with ballots.  A full list is cut to its k best.
+// where k lanes or more pass, the k-th largest of the lanes' maxima, for a large k
+// of the maxima of eight elements, is a better bound, found bit by bit with
+// ballots.  A full list is cut to its k best.
 // Elements come in ascending order, so what only equals the bound of an earlier
 // tile has k better ones before it.
 // Parts of a row by different wavefronts leave their sums and their k best in
-// order; they are joined in LDS, or by a second kernel, which merges the lists
-// with a lane to a part: k times the largest head, the lowest lane among equal
-// ones (its elements come first).
-// What bounds it: memory, for many rows (2048 of 200000 in bf16, k = 5: 158 us,
-// 5.2 TB/s; k = 64 250); for few the chain of load, bound, list, join and the
-// launches (4 of 128000, k = 2: 5.5 us, and 4 the join).  Rising logits, of which
-// every tile passes whole, take four times as long as others.
+// order; they are joined in LDS, or by a second kernel: for a small k with a lane
+// to a part, k times the largest head, the lowest lane among equal ones (its
+// elements come first); for a larger one the lists in pairs.
+// What bounds it: memory, for many rows (2048 of 200000 in bf16, k = 5: 157 us,
+// 5.2 TB/s; k = 20 168, k = 64 234); for few the chain of load, bound, list, join
+// and the launches (4 of 128000, k = 2: 5 us, and 3.7 the join; one of 32000, k =
+// 5, 20 and 64: 8, 11.4 and 24).  Rising logits, of which every tile passes whole,
+// take four times as long as others.
 #include "device.hpp"
 #include "step.hpp"
 
@@ -43,17 +45,15 @@ constexpr float kFloor = -1e30f;    // stands for -inf where -inf * 0 must not a
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
 
-// What the parts of a row leave, k lists of the heads, the seconds and so on: entry r of part p at r * parts + p.
+// What the parts of a row leave, next to a list of k entries each, in order, zeros behind the last.
 struct Head {
     double s;
     float m, a;
-    int count;
 };
 
 struct Work {
-    Head *heads;      // [N][parts]
-    float *values;    // [N][k][parts]
-    int *indices;     // [N][k][parts]
+    Head *heads;        // [N][parts]
+    uint64_t *entries;  // [N][parts][k]
 };
 
 // Wavefronts of a row of `tiles` tiles, at most `most`: all have the same number of tiles but the last.
@@ -92,6 +92,9 @@ __device__ __forceinline__ float above(float v)
 {
     return v == INFINITY ? __uint_as_float(0x7fc00000u) : float_of(order_of(v) + 1);
 }
+
+// An alternative as one number: what comes first is larger, and none is 0.
+__device__ __forceinline__ uint64_t entry_of(float v, int at) { return (uint64_t)order_of(v) << 32 | ~(uint32_t)at; }
 
 __device__ __forceinline__ int lanes_before(uint64_t mask)
 {
@@ -187,86 +190,102 @@ __device__ __forceinline__ void wave_fence()
     __builtin_amdgcn_wave_barrier();
 }
 
+// A number that at least k of the lanes' keys reach, the largest of the BITS upper bits or one that just k reach; `reach`: how
+// many do.  0, and `reach` as it was, if there are fewer than k of 1 and more.
+template <int BITS, int E>
+__device__ __forceinline__ uint32_t kth(const uint32_t (&key)[E], int k, int &reach)
+{
+    uint32_t t = 0;
+    for (int bit = 31; bit >= 32 - BITS; --bit) {
+        const uint32_t x = t | 1u << bit;
+        int n = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) n += __builtin_popcountll(__ballot(key[e] >= x));
+        if (n < k) continue;
+        t = x;
+        reach = n;
+        if (n == k) break;
+    }
+    return t;
+}
+
 // The k best of what a wavefront has seen, in its list.  All members are uniform.
 struct Best {
-    float *value;  // kList entries
-    int *index;
+    u32x2 *list;  // kList pairs of value and index
     // A list of more than `longest` is cut before it grows: twice k, and at least 64.  (A longer one is cut less often, but
     // the bound stays low until it is: 2048 rows of 200000, k = 5, up to 256 entries 171 us, 64 entries 164.)
     int k, longest, count = 0;
     float bound = -INFINITY;  // k entries of the list are at least this; -inf: perhaps fewer
 
-    // The largest number, of the BITS upper bits, that at least k of the lanes' keys reach.
-    template <int BITS, int E>
-    __device__ __forceinline__ static uint32_t kth(const uint32_t (&key)[E], int k)
+    // The list, of at most E entries a lane, cut to its k best, equal ones by the lower index.
+    template <int E>
+    __device__ __forceinline__ void cut_of()
     {
-        uint32_t t = 0;
-        for (int bit = 31; bit >= 32 - BITS; --bit) {
-            const uint32_t x = t | 1u << bit;
-            int n = 0;
-#pragma unroll
-            for (int e = 0; e < E; ++e) n += __builtin_popcountll(__ballot(key[e] >= x));
-            if (n >= k) t = x;
-        }
-        return t;
-    }
-
-    // The list cut to its k best, equal ones by the lower index.
-    __device__ __forceinline__ void cut()
-    {
-        if (count <= k) return;
         wave_fence();
-        constexpr int E = kList / kWave;
         const int lane = lane_id();
-        float v[E];
-        int at[E];
+        u32x2 entry[E];
         uint32_t key[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const int i = e * kWave + lane;
-            v[e] = i < count ? value[i] : 0.f;
-            at[e] = i < count ? index[i] : 0;
-            key[e] = i < count ? order_of(v[e]) : 0u;  // no number has order 0
+            entry[e] = i < count ? list[i] : u32x2{0u, 0u};
+            key[e] = i < count ? order_of(__uint_as_float(entry[e][0])) : 0u;  // no number has order 0
         }
-        const uint32_t t = kth<32>(key, k);
-        int more = 0;
+        int reach = count;
+        const uint32_t t = kth<32>(key, k, reach);
+        uint32_t last = 0;
+        if (reach > k) {
+            // Some are equal to the k-th: those of lowest index stay, whose complements are the largest.
+            int more = 0;
 #pragma unroll
-        for (int e = 0; e < E; ++e) more += __builtin_popcountll(__ballot(key[e] > t));
-        // Of the equal ones the k - more of lowest index: their indices' complements as keys.
-        uint32_t tie[E];
+            for (int e = 0; e < E; ++e) more += __builtin_popcountll(__ballot(key[e] > t));
+            uint32_t tie[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) tie[e] = key[e] == t ? ~(uint32_t)at[e] : 0u;
-        const uint32_t last = kth<32>(tie, k - more);
+            for (int e = 0; e < E; ++e) tie[e] = key[e] == t ? ~entry[e][1] : 0u;
+            last = kth<32>(tie, k - more, reach);
+        }
         wave_fence();
         count = 0;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const bool stays = key[e] > t || (tie[e] && tie[e] >= last);
+            const bool stays = key[e] > t || (key[e] == t && ~entry[e][1] >= last);
             const uint64_t mask = __ballot(stays);
-            if (stays) {
-                value[count + lanes_before(mask)] = v[e];
-                index[count + lanes_before(mask)] = at[e];
-            }
+            if (stays) list[count + lanes_before(mask)] = entry[e];
             count += __builtin_popcountll(mask);
         }
         bound = float_of(t);
     }
 
+    __device__ __forceinline__ void cut()
+    {
+        if (count <= k) return;
+        if (count <= 2 * kWave) cut_of<2>();
+        else cut_of<kList / kWave>();
+    }
+
     // The lane's entry of at most 64, and how many come before it; a rank of at least 64 where it has none.
-    __device__ __forceinline__ int ranked(float &v, int &at) const
+    __device__ __forceinline__ int ranked(uint64_t &mine) const
     {
         wave_fence();
         const bool has = lane_id() < count;
-        v = has ? value[lane_id()] : 0.f;
-        at = has ? index[lane_id()] : 0;
-        const uint32_t key = v != v ? 0u : order_of(v);  // NaN after every number
+        const u32x2 entry = has ? list[lane_id()] : u32x2{0u, 0u};
+        mine = has ? entry_of(__uint_as_float(entry[0]), (int)entry[1]) : 0;
         int rank = has ? 0 : kWave;
+#pragma unroll 4
         for (int i = 0; i < count; ++i) {
-            const uint32_t other = __builtin_amdgcn_readlane(key, i);
-            const int x = __builtin_amdgcn_readlane(at, i);
-            rank += other > key || (other == key && x < at);
+            const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(mine >> 32), i), lo = __builtin_amdgcn_readlane((uint32_t)mine, i);
+            rank += ((uint64_t)hi << 32 | lo) > mine;
         }
         return rank;
+    }
+
+    // Its k best, in order, to k entries from `to` on, zeros behind the last.
+    __device__ __forceinline__ void leave(uint64_t *to) const
+    {
+        uint64_t mine;
+        const int rank = ranked(mine);
+        if (rank < k) to[rank] = mine;
+        if (lane_id() >= count && lane_id() < k) to[lane_id()] = 0;
     }
 
     // A tile of E elements a lane, of higher index than all before; top: the lane's largest, group[g]: of the g-th kGroup.
@@ -276,10 +295,23 @@ struct Best {
         const uint64_t pass = __ballot(top > bound);
         if (!pass) return;
         float from = above(bound);
-        if (__builtin_popcountll(pass) >= k) {
-            // Sixteen bits, a bf16's, are near enough; fewer lanes pass a whole number's.
-            const uint32_t key[1] = {top > bound ? order_of(top) : 0u};
-            bound = from = fmaxf(from, float_of(kth<16>(key, k)));
+        // Sixteen bits, a bf16's, are near enough; fewer pass a whole number's.
+        int reach;
+        if (k <= kWave / 2 || G == 1) {
+            if (__builtin_popcountll(pass) >= k) {
+                const uint32_t key[1] = {top > bound ? order_of(top) : 0u};
+                bound = from = fmaxf(from, float_of(kth<16>(key, k, reach)));
+            }
+        } else {
+            // By the groups' maxima: of a first tile's 2048 elements 70 pass for k = 64, by the lanes' 250.
+            uint32_t key[G];
+            int n = 0;
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                n += __builtin_popcountll(__ballot(group[g] > bound));
+                key[g] = group[g] > bound ? order_of(group[g]) : 0u;
+            }
+            if (n >= k) bound = from = fmaxf(from, float_of(kth<16>(key, k, reach)));
         }
 #pragma unroll
         for (int g = 0; g < G; ++g) {
@@ -293,10 +325,7 @@ struct Best {
                 const bool in = v[e] >= from;
                 const uint64_t mask = __ballot(in);
                 if (!mask) continue;
-                if (in) {
-                    value[count + lanes_before(mask)] = v[e];
-                    index[count + lanes_before(mask)] = index_of(e);
-                }
+                if (in) list[count + lanes_before(mask)] = u32x2{__float_as_uint(v[e]), (uint32_t)index_of(e)};
                 count += __builtin_popcountll(mask);
             }
         }
@@ -380,13 +409,51 @@ __device__ __forceinline__ void scan(const LogprobArgs &a, int row, int part, in
     if (TOP && best.count > kKept) best.cut();
 }
 
-// A row's results from its parts (head: the lane's part's), by a whole workgroup.  Lists in LDS: entry r of part p at
-// r * parts + p, the values, then the indices.
+// Whether a row's alternatives are taken one after the other from its parts' heads, by one wavefront, or by joining the lists.
+// (One row of 32000, 16 parts: k = 13 10.3 us either way, k = 20 12.2 and 11.4, k = 64 29.5 and 23.6.  One of 200000, 49 parts:
+// k = 25 20.5 either way, k = 64 41.2 and 37.1.)
+__host__ __device__ inline bool in_steps(int k, int parts) { return k <= (parts > kMostWaves ? 24 : 12); }
+
+// Lists of k entries in order, `parts` of them one after the other at `from`, joined in pairs until one is left: an entry's place
+// is its own in its list and that of the first smaller one in the other.  By a whole workgroup; `spare` has room for half of the
+// lists, rounded up.  Where the list is, then.
+__device__ __forceinline__ const uint64_t *join_lists(uint64_t *from, uint64_t *spare, int parts, int k)
+{
+    for (int n = parts; n > 1; n = (n + 1) / 2) {
+        const int half = (n + 1) / 2;
+        for (int i = threadIdx.x; i < n * k; i += blockDim.x) {
+            const int p = i / k, other = p < half ? p + half : p - half;
+            const uint64_t mine = from[i];
+            int place = i - p * k;
+            if (other < n) {
+                // Equal are zeros only: those of the first list come first.
+                const uint64_t *list = from + other * k;
+                int lo = 0, hi = k;
+                while (lo < hi) {
+                    const int mid = (lo + hi) / 2;
+                    const uint64_t x = list[mid];
+                    if (x > mine || (p >= half && x == mine)) lo = mid + 1;
+                    else hi = mid;
+                }
+                place += lo;
+            }
+            if (place < k) spare[min(p, other) * k + place] = mine;
+        }
+        __syncthreads();
+        uint64_t *const x = from;
+        from = spare;
+        spare = x;
+    }
+    return from;
+}
+
+// A row's results from its parts (head: the lane's part's), by a whole workgroup.  Lists in LDS, one after the other, and room
+// for half of them.
 template <bool BF16>
-__device__ __forceinline__ void finish(const LogprobArgs &a, int row, int parts, const Head &head, const uint32_t *lists)
+__device__ __forceinline__ void finish(const LogprobArgs &a, int row, int parts, const Head &head, uint64_t *lists, uint64_t *spare)
 {
     constexpr int kBytes = BF16 ? 2 : 4;
-    const int lane = lane_id(), wave = threadIdx.x / kWave, entries = a.k * parts;
+    const int lane = lane_id(), wave = threadIdx.x / kWave;
     const char *p = static_cast<const char *>(a.logits) + row * a.stride * kBytes;
     const float c = a.scale * kLog2e;
     Sums sums{head.m, head.a, head.s};
@@ -402,29 +469,34 @@ __device__ __forceinline__ void finish(const LogprobArgs &a, int row, int parts,
         const int t = a.tokens[(long)row * a.M + i];
         a.logprob[(long)row * a.M + i] = t >= 0 && t < a.V ? logprob(logit<BF16>(p, t)) : -INFINITY;
     }
-    if (!a.k || wave) return;
+    if (!a.k) return;
 
-    // Lane r keeps what comes r-th.
-    float v = 0.f;
-    int at = 0, count = 0, next = 0;
-    auto order_at = [&](int r) { return r < head.count ? order_of(__uint_as_float(lists[r * parts + lane])) : 0u; };
-    uint32_t key = order_at(0), second = order_at(1);
-    for (; count < a.k; ++count) {
-        const uint32_t win = last_lane(along_lanes(key, 0u, [](uint32_t x, uint32_t y) { return x > y ? x : y; }));
-        if (!win) break;
-        const int from = (int)__builtin_ctzll(__ballot(key == win));
-        const int place = __builtin_amdgcn_readlane(next, from) * parts + from;
-        if (lane == count) {
-            v = float_of(win);
-            at = place;
-        }
-        if (lane == from) {
-            ++next;
-            key = second;
-            second = order_at(next + 1);
+    // Lane r of the first wavefront keeps what comes r-th.
+    uint64_t mine = 0;
+    if (!in_steps(a.k, parts)) {
+        const uint64_t *all = join_lists(lists, spare, parts, a.k);
+        if (wave) return;
+        if (lane < a.k) mine = all[lane];
+    } else {
+        if (wave) return;
+        auto entry_at = [&](int r) { return lane < parts && r < a.k ? lists[lane * a.k + r] : 0; };
+        uint64_t head_of = entry_at(0), second = entry_at(1);
+        for (int n = 0, next = 0; n < a.k; ++n) {
+            const uint32_t key = (uint32_t)(head_of >> 32);
+            const uint32_t win = last_lane(along_lanes(key, 0u, [](uint32_t x, uint32_t y) { return x > y ? x : y; }));
+            if (!win) break;
+            // The lowest lane among equal ones: its elements come first.
+            const int from = (int)__builtin_ctzll(__ballot(key == win));
+            const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)head_of, from);
+            if (lane == n) mine = (uint64_t)win << 32 | lo;
+            if (lane == from) {
+                head_of = second;
+                second = entry_at(++next + 1);
+            }
         }
     }
-    at = lane < count ? (int)lists[entries + at] : 0;
+    float v = float_of((uint32_t)(mine >> 32));
+    int at = (int)~(uint32_t)mine, count = __builtin_popcountll(__ballot(mine != 0));
     // Fewer than k numbers above -inf: the first -inf, then the first NaN.
     for (int pass = 0; pass < 2 && count < a.k; ++pass) {
         for (int i0 = 0; i0 < a.V && count < a.k; i0 += kWave) {
@@ -448,40 +520,27 @@ __device__ __forceinline__ void finish(const LogprobArgs &a, int row, int parts,
 template <bool BF16, bool TOP>
 __global__ __launch_bounds__(kThreads) void parts_kernel(LogprobArgs a, int parts, Work out)
 {
-    __shared__ float values[TOP ? kWaves : 1][TOP ? kList : 1];
-    __shared__ int indices[TOP ? kWaves : 1][TOP ? kList : 1];
+    __shared__ u32x2 lists[TOP ? kWaves : 1][TOP ? kList : 1];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const long id = (long)blockIdx.x * kWaves + wave;
     if (id >= (long)a.N * parts) return;
     const int row = (int)(id / parts), part = (int)(id % parts);
     Sums sums;
-    Best best{values[TOP ? wave : 0], indices[TOP ? wave : 0], a.k, max(2 * a.k, kWave)};
+    Best best{lists[TOP ? wave : 0], a.k, max(2 * a.k, kWave)};
     scan<BF16, TOP>(a, row, part, parts, sums, best);
-    if (TOP) {
-        float v;
-        int at;
-        const int rank = best.ranked(v, at);
-        if (rank < a.k) {
-            const long to = ((long)row * a.k + rank) * parts + part;
-            out.values[to] = v;
-            out.indices[to] = at;
-        }
-    }
-    if (lane == 0) out.heads[id] = Head{sums.s, sums.m, sums.a, min(best.count, a.k)};
+    if (TOP) best.leave(out.entries + id * a.k);
+    if (lane == 0) out.heads[id] = Head{sums.s, sums.m, sums.a};
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(kThreads) void join_kernel(LogprobArgs a, int parts, Work in)
+__global__ __launch_bounds__(kMostWaves *kWave) void join_kernel(LogprobArgs a, int parts, Work in)
 {
-    extern __shared__ uint32_t lists[];
+    extern __shared__ uint64_t lists[];
     const int row = blockIdx.x, lane = lane_id(), entries = a.k * parts;
-    const Head head = lane < parts ? in.heads[(long)row * parts + lane] : Head{0., kLowest, 0.f, 0};
-    for (int i = threadIdx.x; i < entries; i += blockDim.x) {
-        lists[i] = __float_as_uint(in.values[(long)row * entries + i]);
-        lists[entries + i] = (uint32_t)in.indices[(long)row * entries + i];
-    }
+    const Head head = lane < parts ? in.heads[(long)row * parts + lane] : Head{0., kLowest, 0.f};
+    for (int i = threadIdx.x; i < entries; i += blockDim.x) lists[i] = in.entries[(long)row * entries + i];
     __syncthreads();
-    finish<BF16>(a, row, parts, head, lists);
+    finish<BF16>(a, row, parts, head, lists, lists + entries);
 }
 
 // A row by one workgroup, a part by each of its wavefronts, joined in LDS.
@@ -490,24 +549,15 @@ __global__ __launch_bounds__(kMostWaves *kWave) void row_kernel(LogprobArgs a, i
 {
     extern __shared__ double shared[];
     Head *heads = reinterpret_cast<Head *>(shared);
-    uint32_t *lists = reinterpret_cast<uint32_t *>(heads + parts);
-    float *values = reinterpret_cast<float *>(lists + 2 * a.k * parts);
+    uint64_t *lists = reinterpret_cast<uint64_t *>(heads + parts), *spare = lists + a.k * parts;
     const int row = blockIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     Sums sums;
-    Best best{values + wave * kList, reinterpret_cast<int *>(values + (parts + wave) * kList), a.k, max(2 * a.k, kWave)};
+    Best best{reinterpret_cast<u32x2 *>(spare) + wave * kList, a.k, max(2 * a.k, kWave)};
     scan<BF16, TOP>(a, row, wave, parts, sums, best);
-    if (TOP) {
-        float v;
-        int at;
-        const int rank = best.ranked(v, at);
-        if (rank < a.k) {
-            lists[rank * parts + wave] = __float_as_uint(v);
-            lists[(a.k + rank) * parts + wave] = (uint32_t)at;
-        }
-    }
-    if (lane == 0) heads[wave] = Head{sums.s, sums.m, sums.a, min(best.count, a.k)};
+    if (TOP) best.leave(lists + wave * a.k);
+    if (lane == 0) heads[wave] = Head{sums.s, sums.m, sums.a};
     __syncthreads();
-    finish<BF16>(a, row, parts, lane < parts ? heads[lane] : Head{0., kLowest, 0.f, 0}, lists);
+    finish<BF16>(a, row, parts, lane < parts ? heads[lane] : Head{0., kLowest, 0.f}, lists, spare);
 }
 
 template <bool BF16, bool TOP>
@@ -527,14 +577,17 @@ hipError_t launch(const LogprobArgs &a, void *workspace, hipStream_t stream)
     const long n = (long)a.N * parts;
     Work w;
     w.heads = static_cast<Head *>(workspace);
-    w.values = reinterpret_cast<float *>(w.heads + n);
-    w.indices = reinterpret_cast<int *>(w.values + n * a.k);
+    w.entries = reinterpret_cast<uint64_t *>(w.heads + n);
     parts_kernel<BF16, TOP><<<(unsigned)((n + kWaves - 1) / kWaves), kThreads, 0, stream>>>(a, parts, w);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    // One wavefront does the merging; more of them bring long lists.
-    const int entries = a.k * parts, threads = entries > 4 * kWave ? kThreads : kWave;
-    join_kernel<BF16><<<(unsigned)a.N, threads, entries * 8, stream>>>(a, parts, w);
+    // Long lists are brought, and joined, by more than one wavefront (one row of 200000, k = 64: a call with four 48 us, with
+    // sixteen 36).
+    const bool steps = in_steps(a.k, parts);
+    const int entries = a.k * parts;
+    const int waves = steps ? (entries > 4 * kWave ? 4 : 1) : min((entries + kWave - 1) / kWave, kMostWaves);
+    const size_t lds = (entries + (steps ? 0 : a.k * ((parts + 1) / 2))) * sizeof(uint64_t);
+    join_kernel<BF16><<<(unsigned)a.N, waves * kWave, lds, stream>>>(a, parts, w);
     return hipGetLastError();
 }
 
@@ -543,7 +596,7 @@ hipError_t launch(const LogprobArgs &a, void *workspace, hipStream_t stream)
 size_t logprobs_workspace(int N)
 {
     // At most kMinParts parts, of at least one a row.
-    return ((size_t)kMinParts + N) * (sizeof(Head) + kKept * (sizeof(float) + sizeof(int)));
+    return ((size_t)kMinParts + N) * (sizeof(Head) + kKept * sizeof(uint64_t));
 }
 
 hipError_t launch_token_logprobs(const LogprobArgs &a, bool bf16, void *workspace, hipStream_t stream)

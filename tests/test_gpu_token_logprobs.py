@@ -111,7 +111,7 @@ def test_sizes(V, type):
 @pytest.mark.parametrize("type", TYPES)
 @pytest.mark.parametrize("kind", ["peaked", "equal", "ties", "rising", "falling", "masked", "lowest", "odd", "large"])
 def test_values(kind, type):
-    for N, V, k in ((12, 700, 64), (70, 3001, 20), (7, 40003, 64), (9, 40003, 5), (30, 33, 33)):
+    for N, V, k in ((12, 700, 64), (70, 3001, 20), (7, 40003, 64), (9, 40003, 5), (30, 33, 33), (2, 140003, 64)):
         print(f"logprobs {kind} N={N} V={V} {type} k={k}", flush=True)
         x = fill(kind, N, V, V).to(TYPES[type]).to(DEV)
         t = given(N, V, 3, V)
