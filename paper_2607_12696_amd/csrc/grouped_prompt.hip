@@ -33,8 +33,8 @@ constexpr int kKeys = 32, kWaves = 4, kThreads = kWaves * kWave, kRows = 32 * kW
 template <int D>
 constexpr int kSlots = (D == 64 ? 4 : 3) * kCus;
 constexpr int kFewSlots = 2 * kCus;
-constexpr int kMinTiles = 4, kLongTiles = 96;  // of a chunk
-constexpr int kJoinWaves = 8;
+constexpr int kMinTiles = 4, kLongTiles = 32;  // of a chunk
+constexpr int kJoinWaves = 8, kTogether = 4;   // most wavefronts of a joining workgroup; chunks that one takes together
 constexpr float kSlack = 8.f;  // powers of two that weights may pass 1 by before their reference maximum moves
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
@@ -79,6 +79,9 @@ struct Block {
         tiles = row0 < rows ? (limit(min(row0 + block_rows, rows) - 1) + kKeys - 1) / kKeys : 0;
     }
 };
+
+// Wavefronts that join so many chunks: by a block's own, so that its sums do not depend on what else a call has.
+__host__ __device__ inline int join_waves(int chunks) { return min((chunks + kTogether - 1) / kTogether, kJoinWaves); }
 
 // Sums of a chunk: for each row the reference maximum and the weights' sum, and the output sums in accumulator order.
 struct PromptParts {
@@ -356,22 +359,23 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void prompt_kernel(Group
 }
 
 // Adds up the chunks of a row block: a workgroup has 32 rows by 8 elements, what registers 4 i .. 4 i + 3 of one element tile
-// of the accumulators hold; each of its wavefronts takes every eighth chunk, four of them together, in one pass with a running
-// reference maximum.  What bounds it: latency (offsets, one read for 32 chunks, barrier).  7 tokens over 4008 keys, 31 chunks,
-// 8 MB: 4.1 us (with the references read first, behind a barrier of their own, 6.4).  The whole call for 3 tokens over 30003
-// keys, 8 heads on one, 234 chunks: 17.1 us (by four wavefronts 20.4; eight chunks together, or 16 wavefronts, are no better
-// here and 5 us worse for 50 tokens over 20050 keys, 64 heads on 4, where 52).
+// of the accumulators hold; its wavefronts, one for each four chunks and at most eight, take chunks in turn, four together, in
+// one pass with a running reference maximum.  What bounds it: latency (offsets, one read for 32 chunks, barrier).  7 tokens over
+// 4008 keys, 31 chunks, 8 MB: 4.1 us (with the references read first, behind a barrier of their own, 6.4).  The whole call for 3
+// tokens over 30003 keys, 8 heads on one, 234 chunks: 17.1 us (by four wavefronts 20.4; eight chunks together, or 16 wavefronts,
+// are no better here and 5 us worse for 50 tokens over 20050 keys, 64 heads on 4, where 52); for 29 prompts of up to 364 tokens,
+// two heads, two chunks at most, 26.6 (by eight wavefronts always 41.5).
 template <int D>
 __global__ __launch_bounds__(kJoinWaves *kWave) void join_prompt_kernel(GroupedPromptArgs a, int blocks, int most_chunks,
                                                                         PromptParts parts)
 {
     constexpr int kGroups = D / 32 * 4;
-    constexpr int kTogether = 4;  // chunks
     __shared__ f32x4 sums[kJoinWaves - 1][kWave];
     __shared__ float2 totals[kJoinWaves - 1][kWave];
     const int group = blockIdx.x % kGroups, of = blockIdx.x / kGroups % kWaves, pb = blockIdx.x / (kGroups * kWaves);
     const Block blk(a, pb / blocks, pb % blocks, kRows);
     const int chunks = chunks_of(blk.tiles, most_chunks), lane = lane_id(), wave = threadIdx.x / kWave;
+    const int waves = join_waves(chunks);  // the others have nothing to do
     const int row = blk.row0 + of * 32 + lane % 32;
     if (chunks == 1 || blk.row0 + of * 32 >= blk.rows) return;
     const float2 *ml = parts.ml + (long)pb * most_chunks * kRows + of * 32 + lane % 32;
@@ -396,19 +400,19 @@ __global__ __launch_bounds__(kJoinWaves *kWave) void join_prompt_kernel(GroupedP
         for (int n = 0; n < 4; ++n) sum[n] = fmaf(v[n], f, sum[n]);
     };
 #pragma unroll 1
-    for (int c0 = wave; c0 < chunks; c0 += kTogether * kJoinWaves) {
+    for (int c0 = wave; wave < waves && c0 < chunks; c0 += kTogether * waves) {
         float2 part[kTogether];
         f32x4 v[kTogether];
 #pragma unroll
         for (int i = 0; i < kTogether; ++i) {
-            const int c = min(c0 + i * kJoinWaves, chunks - 1);
+            const int c = min(c0 + i * waves, chunks - 1);
             part[i] = ml[c * kRows];
             v[i] = o[c * kStep];
         }
         float most = -INFINITY;
 #pragma unroll
         for (int i = 0; i < kTogether; ++i) {
-            if (c0 + i * kJoinWaves >= chunks) {  // the last one again
+            if (c0 + i * waves >= chunks) {  // the last one again
                 part[i] = float2{-INFINITY, 0.f};
                 v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
             }
@@ -425,11 +429,9 @@ __global__ __launch_bounds__(kJoinWaves *kWave) void join_prompt_kernel(GroupedP
     __syncthreads();
     if (wave || row >= blk.rows) return;
     float most = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kJoinWaves - 1; ++w) most = fmaxf(most, totals[w][lane].x);
+    for (int w = 0; w < waves - 1; ++w) most = fmaxf(most, totals[w][lane].x);
     reach(most);
-#pragma unroll
-    for (int w = 0; w < kJoinWaves - 1; ++w) add(totals[w][lane].x, totals[w][lane].y, sums[w][lane]);
+    for (int w = 0; w < waves - 1; ++w) add(totals[w][lane].x, totals[w][lane].y, sums[w][lane]);
     const float inv = total == 0.f ? 0.f : 1.f / total;
     const long at = (long)(blk.q0 + row / blk.G) * a.H + blk.hk * blk.G + row % blk.G;
     *reinterpret_cast<u32x2 *>(a.o + at * D + 8 * group + lane / 32 * 4) =
@@ -450,10 +452,9 @@ hipError_t launch(const GroupedPromptArgs &a, void *workspace, hipStream_t strea
     char *w = static_cast<char *>(workspace);
     const PromptParts parts{reinterpret_cast<float2 *>(w), reinterpret_cast<float *>(w + kSlots<D> * kRows * sizeof(float2))};
     const long groups = (long)pairs * blocks, tiles = a.M / ((long)a.B * kKeys);  // of the average sequence
-    // Chunks that fill the card, if they are long beside their sums (64 heads on 8 of 64, 20000 keys behind: 400 tokens 174 us, 208
-    // in the fewer, 600 270 and 351, but 800 383 and 364; 32 on 8 of 128, 50000 behind: 700 tokens 613 and 743), else few (64 on 4 of
-    // 128, 20000 behind: 16 tokens 29 us, for three workgroups a compute unit 33, 200 tokens 158 and 170; 32 on 8 of 128, 4000
-    // behind: 1200 tokens uncut 123, in two chunks 145).
+    // Chunks that fill the card, if they are long beside their sums (64 heads on 8 of 64, 20000 keys behind: 200 tokens 94 us, by two
+    // workgroups a compute unit 104; 8 prompts of up to 3021 tokens, two heads: 65 and 71), else few (64 on 4 of 128, 20000 behind: 16
+    // tokens 30 us, by three 34; 4000 behind, 7 tokens 17.3 and 19.5).
     const long full = kSlots<D> / groups, room = tiles >= kLongTiles * full ? full : kFewSlots / groups;
     // The longest sequence's keys are known on the device only; it is taken to have twice the average.  (40 sequences of up to
     // 53 tokens and keys: a second launch that joins nothing, 5.8 us.)
@@ -463,7 +464,7 @@ hipError_t launch(const GroupedPromptArgs &a, void *workspace, hipStream_t strea
         prompt_kernel<D, KT, true><<<(unsigned)(groups * chunks), kThreads, 0, stream>>>(a, blocks, chunks, parts);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        join_prompt_kernel<D><<<(unsigned)join_groups, kJoinWaves * kWave, 0, stream>>>(a, blocks, chunks, parts);
+        join_prompt_kernel<D><<<(unsigned)join_groups, join_waves(chunks) * kWave, 0, stream>>>(a, blocks, chunks, parts);
         return hipGetLastError();
     }
     prompt_kernel<D, KT, false><<<(unsigned)groups, kThreads, 0, stream>>>(a, blocks, 1, parts);
