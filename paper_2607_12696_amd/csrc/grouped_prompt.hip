@@ -251,7 +251,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void prompt_kernel(Group
             p[i / 8][i % 8 / 2] = to_bf16x2(s[i], s[i + 1]);
         }
         l += sum;
-        if (odd_tiles >> max(t - edge, 0) & 1) {  // no bit is set before tile `edge`
+        if (t >= edge && odd_tiles >> (t - edge) & 1) {  // a step's bits are there before its first tile, which may be before `edge`
             uint32_t set = 0;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {

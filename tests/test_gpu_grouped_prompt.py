@@ -139,6 +139,30 @@ def test_later_keys_are_not_felt(bad, D):
         assert torch.isnan(o[at + 5:n]).all()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B", [1, 40])
+def test_bad_values_in_every_tile(B, D):
+    """One value that is not a number, in each tile in turn, in cut and in whole row blocks: rows that do not see it are as without."""
+    n, H = 299, 8
+    c = case([n] * B, [n] * B, H, H, D, seed=12, spare=0)
+    clean, clean_lse = run(c)
+    kv = c["kv"].to(DEV)
+    for at in range(5, n, 32):
+        print(f"grouped prompt bad value B={B} D={D} key={at}", flush=True)
+        for b in (0, B - 1):
+            i = n * b + at
+            was = kv[i, 1].clone()
+            kv[i, 1, :, 7::19] = NAN
+            o, lse = moe.moe_grouped_prompt(c["q"].to(DEV), kv[:, 0], kv[:, 1], c["qo"].to(DEV), c["ko"].to(DEV), c["scale"], max_tokens=n)
+            felt = torch.isnan(o)
+            assert torch.equal(lse, clean_lse) and felt[i:n * (b + 1), :, 7::19].all()
+            felt[i:n * (b + 1), :, 7::19] = False
+            assert not felt.any()
+            o[i:n * (b + 1), :, 7::19] = clean[i:n * (b + 1), :, 7::19]
+            assert torch.equal(o, clean)
+            kv[i, 1] = was
+
+
 def test_values_that_all_see():
     """Infinities before every query's first key: they reach every row."""
     c = case([40], [400], 4, 2, 64, seed=8)
