@@ -11,13 +11,13 @@
 //   values (rows of 64 bytes: half a read is 256 in a row).  One barrier a step.
 //   Products, maximum, exponentials and sums of a tile follow each other in a wavefront; what overlaps them is the other
 //   wavefronts of its SIMD, of other workgroups, so registers are kept for four of them with heads of 64 and three with 128.
-//   Where there are few row blocks, each one's keys are cut into chunks, a workgroup each, whose sums join_prompt_kernel
-//   adds up in order.
+//   Where there are few row blocks, or sequences of keys far more than queries, each block's keys are cut into chunks, a
+//   workgroup each, whose sums join_prompt_kernel adds up in order.
 //   Measured: one prompt of 6007 tokens, 64 heads on 4 of 128, 525 us, 1.13 PFLOP/s (a bf16 product of 8192^3: 1.415): the
 //   matrix cores are busy 60% of the cycles and the vector unit issues in half of them, at 1.8 GHz, which the power leaves
 //   (operands of zeros run at 2.2); six prompts of 563 to 1201 tokens, 64 heads on 8 of 64, 84 us: the vector unit (five
 //   instructions a weight, half the products of a head of 128 to hide them), and wavefronts that end unevenly; 7 tokens over
-//   4008 keys, 64 heads on 4 of 128, 13 us and 4.1 of the join: a chain of offsets, queries, first tile, four tiles at 1.2 us
+//   4008 keys, 64 heads on 4 of 128, 13 us and 4.1 of the join: a chain of offsets, cuts, queries, first tile, six tiles at 1.2 us
 //   (a lone wavefront's latency), parts; loads two and three steps ahead, or two and four tiles a step, did not shorten it.
 //   With two wavefronts a SIMD, each with three tiles under way at once and a piece of the exponentials behind each product
 //   (176 and 248 registers), the first two took 575 and 100 us; with 64 rows a wavefront, one a SIMD, half the LDS reads,
@@ -33,7 +33,7 @@ constexpr int kKeys = 32, kWaves = 4, kThreads = kWaves * kWave, kRows = 32 * kW
 template <int D>
 constexpr int kSlots = (D == 64 ? 4 : 3) * kCus;
 constexpr int kFewSlots = 2 * kCus;
-constexpr int kMinTiles = 4, kLongTiles = 32;  // of a chunk
+constexpr int kMinTiles = 6, kLongTiles = 32;  // of a chunk
 constexpr int kJoinWaves = 8, kTogether = 4;   // most wavefronts of a joining workgroup; chunks that one takes together
 constexpr float kSlack = 8.f;  // powers of two that weights may pass 1 by before their reference maximum moves
 
@@ -56,27 +56,120 @@ __device__ __forceinline__ float max2(float a, float b)  // without the copies t
 // A number that is the same in all lanes, in a scalar register.
 __device__ __forceinline__ float uniform(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }
 
-// The chunks of a row block of `tiles` tiles.
-__device__ __forceinline__ int chunks_of(int tiles, int most) { return min(most, max(tiles / kMinTiles, 1)); }
+// A sequence: its queries and keys.
+struct Sequence {
+    int q0, nq, k0, nk;
+};
+
+__device__ __forceinline__ Sequence sequence(const GroupedPromptArgs &a, int b)
+{
+    Sequence s;
+    s.q0 = min(max(a.q_offsets[b], 0), a.N);
+    s.nq = min(max(a.q_offsets[b + 1], s.q0), a.N) - s.q0;
+    s.k0 = min(max(a.kv_offsets[b], 0), a.M);
+    s.nk = min(max(a.kv_offsets[b + 1], s.k0), a.M) - s.k0;
+    return s;
+}
+
+// That of a lane, or of the first one.
+__device__ __forceinline__ Sequence uniform(const Sequence &s, int lane = 0)
+{
+    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, lane); };
+    return Sequence{of(s.q0), of(s.nq), of(s.k0), of(s.nk)};
+}
 
 // A workgroup's row block: its sequence and key/value head, and what its rows see.
-struct Block {
-    int q0, nq, k0, nk, hk, rows, row0, tiles, G;
+struct Block : Sequence {
+    int hk, rows, row0, tiles, G;
 
     __device__ __forceinline__ int limit(int row) const { return min(max(row / G + 1 + nk - nq, 0), nk); }  // keys of a query row
 
-    __device__ __forceinline__ Block(const GroupedPromptArgs &a, int pair, int block, int block_rows)
+    __device__ __forceinline__ Block(const GroupedPromptArgs &a, const Sequence &s, int hk, int block) : Sequence(s), hk(hk)
     {
-        const int b = pair / a.Hkv;
-        hk = pair % a.Hkv;
         G = a.H / a.Hkv;
-        q0 = __builtin_amdgcn_readfirstlane(min(max(a.q_offsets[b], 0), a.N));
-        nq = __builtin_amdgcn_readfirstlane(min(max(a.q_offsets[b + 1], q0), a.N)) - q0;
-        k0 = __builtin_amdgcn_readfirstlane(min(max(a.kv_offsets[b], 0), a.M));
-        nk = __builtin_amdgcn_readfirstlane(min(max(a.kv_offsets[b + 1], k0), a.M)) - k0;
         rows = nq * G;
-        row0 = block * block_rows;
-        tiles = row0 < rows ? (limit(min(row0 + block_rows, rows) - 1) + kKeys - 1) / kKeys : 0;
+        row0 = block * kRows;
+        tiles = row0 < rows ? (limit(min(row0 + kRows, rows) - 1) + kKeys - 1) / kKeys : 0;
+    }
+};
+
+__device__ __forceinline__ int wave_total(int v) { return __builtin_amdgcn_readlane(wave_inclusive_sum(v), kWave - 1); }
+
+// How the keys of a call are cut: into chunks of about equal length, which follows from the lengths of all sequences, which only
+// the device knows.  Every wavefront works it out for itself, a lane to a sequence; all members are uniform.
+template <int D>
+struct Cuts {
+    struct Size {
+        int blocks, tiles, chunks;  // row blocks of a head; tiles of the longest, and its chunks
+    };
+    const GroupedPromptArgs &a;
+    int blocks;      // of a sequence, at most
+    int length = 1;  // tiles of a chunk, at most
+    Sequence mine;   // the lane's of the first 64
+
+    __device__ __forceinline__ Sequence of(int b) const
+    {
+        return b < kWave ? mine : b < a.B ? sequence(a, b) : Sequence{0, 0, 0, 0};
+    }
+
+    __device__ __forceinline__ Size size(const Sequence &s) const
+    {
+        const int t = (s.nk + kKeys - 1) / kKeys;
+        return Size{min((s.nq * (a.H / a.Hkv) + kRows - 1) / kRows, blocks), t, max((t + length - 1) / length, 1)};
+    }
+
+    // Places of a sequence's chunks among the parts, if it is cut.
+    __device__ __forceinline__ int slots(const Size &s) const { return s.chunks > 1 ? s.blocks * a.Hkv * s.chunks : 0; }
+
+    __device__ __forceinline__ Cuts(const GroupedPromptArgs &a, int blocks) : a(a), blocks(blocks)
+    {
+        const int lane = lane_id();
+        mine = lane < a.B ? sequence(a, lane) : Sequence{0, 0, 0, 0};
+        float work = 0.f;
+        for (int b = lane; b < a.B + lane; b += kWave) {
+            const Sequence q = of(b);
+            const Size s = size(q);
+            // A row block sees half of its sequence's queries' keys less than the last one, on average.
+            work += (float)(s.blocks * a.Hkv) * max((float)s.tiles - (float)q.nq / (2 * kKeys), 1.f);
+        }
+        work = wave_sum(work);
+        // Chunks that fill the card, if they are long beside their sums (64 heads on 8 of 64, 20000 keys behind: 200 tokens 94
+        // us, by two workgroups a compute unit 104), else few (64 on 4 of 128, 20000 behind: 16 tokens 30 us, by three 34).
+        const float n = work >= (float)kLongTiles * kSlots<D> ? kSlots<D> : kFewSlots;
+        length = __builtin_amdgcn_readfirstlane(max((int)ceilf(work / n), kMinTiles));
+        for (;; length += length / 8 + 1) {
+            int sum = 0;
+            for (int b = lane; b < a.B + lane; b += kWave) sum += slots(size(of(b)));
+            if (wave_total(sum) <= kSlots<D>) break;
+        }
+    }
+
+    // Sequence, head, row block and chunk of a workgroup, and the place of the row block's first chunk; false: nothing to do.
+    __device__ __forceinline__ bool find(int item, int &b, Sequence &seq, int &hk, int &block, int &chunk, int &slot) const
+    {
+        slot = 0;
+        for (int b0 = 0; b0 < a.B; b0 += kWave) {
+            const Sequence q = of(b0 + lane_id());
+            const Size s = size(q);
+            const int items = s.blocks * a.Hkv * s.chunks, upto = wave_inclusive_sum(items), places = wave_inclusive_sum(slots(s));
+            const uint64_t past = __ballot(upto > item);
+            if (past) {
+                const int l = (int)__builtin_ctzll(past), n = __builtin_amdgcn_readlane(s.blocks, l);
+                const int chunks = __builtin_amdgcn_readlane(s.chunks, l);
+                item -= __builtin_amdgcn_readlane(upto - items, l);
+                b = b0 + l;
+                seq = uniform(q, l);
+                hk = item % a.Hkv;
+                // The longest row blocks first.
+                block = n - 1 - item / a.Hkv / chunks;
+                chunk = item / a.Hkv % chunks;
+                slot += __builtin_amdgcn_readlane(places - slots(s), l) + (hk * n + block) * chunks;
+                return true;
+            }
+            item -= __builtin_amdgcn_readlane(upto, kWave - 1);
+            slot += __builtin_amdgcn_readlane(places, kWave - 1);
+        }
+        return false;
     }
 };
 
@@ -87,6 +180,7 @@ __host__ __device__ inline int join_waves(int chunks) { return min((chunks + kTo
 struct PromptParts {
     float2 *ml;  // [slot][kRows]
     float *o;    // [slot][wavefront][D / 8][lane][4]
+    int2 *cut;   // [sequence and head][row block]: the first chunk's slot, and how many
 };
 
 typedef __attribute__((ext_vector_type(2))) float f32x2;
@@ -98,7 +192,7 @@ __device__ __forceinline__ uint32_t to_bf16x2(float lo, float hi)  // one conver
 
 // D: width of a head; KT: key tiles a barrier; SPLIT: keys are cut into chunks.
 template <int D, int KT, bool SPLIT>
-__global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void prompt_kernel(GroupedPromptArgs a, int blocks, int most_chunks,
+__global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void prompt_kernel(GroupedPromptArgs a, int blocks,
                                                                            PromptParts parts)
 {
     constexpr int kSteps = D / 16, kPanels = D / 64, kTiles = D / 32;
@@ -112,15 +206,30 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void prompt_kernel(Group
     };
     __shared__ __attribute__((aligned(16))) Tiles lds;
 
-    const int pairs = a.B * a.Hkv;
-    // Workgroups are dealt to the eight XCDs in turn: with pairs innermost a head's row blocks meet on blocks of them.  The
-    // longest row blocks first, so that no long one is left for the end.
-    const int pair = blockIdx.x % pairs, item = blockIdx.x / pairs;
-    const int block = blocks - 1 - (SPLIT ? item / most_chunks : item), chunk = SPLIT ? item % most_chunks : 0;
-    const Block blk(a, pair, block, kRows);
+    int b, hk, block, chunk = 0, slot = 0, chunks = 1;
+    int length = 0;
+    Sequence seq;
+    if (SPLIT) {
+        const Cuts<D> cuts(a, blocks);
+        if (!cuts.find(blockIdx.x, b, seq, hk, block, chunk, slot)) return;
+        length = cuts.length;
+    } else {
+        // Workgroups are dealt to the eight XCDs in turn: with pairs innermost a head's row blocks meet on blocks of them.  The
+        // longest row blocks first, so that no long one is left for the end.
+        const int pairs = a.B * a.Hkv, pair = blockIdx.x % pairs;
+        block = blocks - 1 - blockIdx.x / pairs;
+        b = pair / a.Hkv;
+        hk = pair % a.Hkv;
+        seq = uniform(sequence(a, b));
+    }
+    const Block blk(a, seq, hk, block);
     if (blk.row0 >= blk.rows) return;
-    const int chunks = SPLIT ? chunks_of(blk.tiles, most_chunks) : 1;
-    if (SPLIT && chunk >= chunks) return;
+    if (SPLIT) {
+        chunks = max((blk.tiles + length - 1) / length, 1);
+        if (chunk >= chunks) return;
+        if (chunk == 0 && threadIdx.x == 0) parts.cut[(b * a.Hkv + hk) * blocks + block] = int2{slot, chunks};
+        slot += chunk;
+    }
     // From here on keys and tiles are counted from the chunk's first.
     const int from = SPLIT ? (int)((long)blk.tiles * chunk / chunks) : 0;
     const int tiles = SPLIT ? (int)((long)blk.tiles * (chunk + 1) / chunks) - from : blk.tiles;
@@ -251,7 +360,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void prompt_kernel(Group
             p[i / 8][i % 8 / 2] = to_bf16x2(s[i], s[i + 1]);
         }
         l += sum;
-        if (t >= edge && odd_tiles >> (t - edge) & 1) {  // a step's bits are there before its first tile, which may be before `edge`
+        if (t >= edge && odd_tiles >> (t - edge) & 1) {  // a step's bits come before its first tile, which may be before `edge`
             uint32_t set = 0;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -316,7 +425,6 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void prompt_kernel(Group
     l = halves_sum(l);
     const bool whole = !SPLIT || chunks == 1;
     const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
-    const long slot = ((long)pair * blocks + block) * most_chunks + chunk;
     if (row >= rows) return;
     const long at = (long)(blk.q0 + row / G) * a.H + blk.hk * G + row % G;
 #pragma unroll
@@ -328,7 +436,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void prompt_kernel(Group
                 *reinterpret_cast<u32x2 *>(a.o + at * D + 32 * d + 8 * i + 4 * half) =
                     u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
             else
-                reinterpret_cast<f32x4 *>(parts.o)[(((slot * kWaves + wave) * kTiles + d) * 4 + i) * kWave + lane] = x;
+                reinterpret_cast<f32x4 *>(parts.o)[((((long)slot * kWaves + wave) * kTiles + d) * 4 + i) * kWave + lane] = x;
         }
     if (odd_tiles) {
         for (int n = 0; n < D / 2; ++n) {  // the lane's own elements, as above
@@ -349,7 +457,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void prompt_kernel(Group
                 uint16_t *to = a.o + at * D + el;
                 *to = f32_to_bf16_bits(bf16_bits_to_f32(*to) + c);
             } else {
-                parts.o[((((slot * kWaves + wave) * kTiles + n / 16) * 4 + n % 16 / 4) * kWave + lane) * 4 + n % 4] += c;
+                parts.o[(((((long)slot * kWaves + wave) * kTiles + n / 16) * 4 + n % 16 / 4) * kWave + lane) * 4 + n % 4] += c;
             }
         }
     }
@@ -366,21 +474,24 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void prompt_kernel(Group
 // are no better here and 5 us worse for 50 tokens over 20050 keys, 64 heads on 4, where 52); for 29 prompts of up to 364 tokens,
 // two heads, two chunks at most, 26.6 (by eight wavefronts always 41.5).
 template <int D>
-__global__ __launch_bounds__(kJoinWaves *kWave) void join_prompt_kernel(GroupedPromptArgs a, int blocks, int most_chunks,
-                                                                        PromptParts parts)
+__global__ __launch_bounds__(kJoinWaves *kWave) void join_prompt_kernel(GroupedPromptArgs a, int blocks, PromptParts parts)
 {
     constexpr int kGroups = D / 32 * 4;
     __shared__ f32x4 sums[kJoinWaves - 1][kWave];
     __shared__ float2 totals[kJoinWaves - 1][kWave];
     const int group = blockIdx.x % kGroups, of = blockIdx.x / kGroups % kWaves, pb = blockIdx.x / (kGroups * kWaves);
-    const Block blk(a, pb / blocks, pb % blocks, kRows);
-    const int chunks = chunks_of(blk.tiles, most_chunks), lane = lane_id(), wave = threadIdx.x / kWave;
-    const int waves = join_waves(chunks);  // the others have nothing to do
+    const int pair = pb / blocks, b = pair / a.Hkv, hk = pair % a.Hkv, block = pb % blocks;
+    const Block blk(a, uniform(sequence(a, b)), hk, block);
+    if (blk.row0 + of * 32 >= blk.rows) return;
+    const int2 cut = parts.cut[pb];
+    const int chunks = cut.y, lane = lane_id(), wave = threadIdx.x / kWave;
     const int row = blk.row0 + of * 32 + lane % 32;
-    if (chunks == 1 || blk.row0 + of * 32 >= blk.rows) return;
-    const float2 *ml = parts.ml + (long)pb * most_chunks * kRows + of * 32 + lane % 32;
-    const long first = ((long)pb * most_chunks * kWaves + of) * kGroups + group;
-    const f32x4 *o = reinterpret_cast<const f32x4 *>(parts.o) + first * kWave + lane;
+    // One chunk: it is written already.  (The bounds: offsets that decrease, which no call may have, can leave a block without.)
+    if (chunks < 2 || (uint32_t)cut.x >= kSlots<D> || chunks > kSlots<D> - cut.x) return;
+    const int waves = min(join_waves(chunks), (int)blockDim.x / kWave);  // the others have nothing to do
+    const long slot = cut.x;
+    const float2 *ml = parts.ml + slot * kRows + of * 32 + lane % 32;
+    const f32x4 *o = reinterpret_cast<const f32x4 *>(parts.o) + ((slot * kWaves + of) * kGroups + group) * kWave + lane;
     constexpr long kStep = kWaves * kGroups * kWave;
     float top = -INFINITY, base = 0.f, total = 0.f;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
@@ -450,24 +561,29 @@ hipError_t launch(const GroupedPromptArgs &a, void *workspace, hipStream_t strea
     const long rows = (long)a.max_tokens * (a.H / a.Hkv);
     const int pairs = a.B * a.Hkv, blocks = (int)((rows + kRows - 1) / kRows);
     char *w = static_cast<char *>(workspace);
-    const PromptParts parts{reinterpret_cast<float2 *>(w), reinterpret_cast<float *>(w + kSlots<D> * kRows * sizeof(float2))};
+    PromptParts parts;
+    parts.ml = reinterpret_cast<float2 *>(w);
+    parts.o = reinterpret_cast<float *>(parts.ml + kSlots<D> * kRows);
+    parts.cut = reinterpret_cast<int2 *>(parts.o + (size_t)kSlots<D> * kRows * D);
     const long groups = (long)pairs * blocks, tiles = a.M / ((long)a.B * kKeys);  // of the average sequence
-    // Chunks that fill the card, if they are long beside their sums (64 heads on 8 of 64, 20000 keys behind: 200 tokens 94 us, by two
-    // workgroups a compute unit 104; 8 prompts of up to 3021 tokens, two heads: 65 and 71), else few (64 on 4 of 128, 20000 behind: 16
-    // tokens 30 us, by three 34; 4000 behind, 7 tokens 17.3 and 19.5).
-    const long full = kSlots<D> / groups, room = tiles >= kLongTiles * full ? full : kFewSlots / groups;
-    // The longest sequence's keys are known on the device only; it is taken to have twice the average.  (40 sequences of up to
-    // 53 tokens and keys: a second launch that joins nothing, 5.8 us.)
-    const int chunks = (int)min(room, 2 * tiles / kMinTiles), join_groups = (int)groups * kWaves * (D / 8);
     constexpr int KT = kTilesAStep<D>;
-    if (chunks > 1) {
-        prompt_kernel<D, KT, true><<<(unsigned)(groups * chunks), kThreads, 0, stream>>>(a, blocks, chunks, parts);
+    // Cut where there are few row blocks; or not so many, and keys behind that are more than the queries: of several sequences,
+    // which may differ much, the longest would take all the time.  (24 of up to 66 tokens, half of them behind up to 9176 keys,
+    // 32 heads on 2 of 128: 76 us, uncut 222.)  Not where keys are few: 30 of up to 246 tokens, 4 heads on 2 of 128, take 13.9
+    // us, cut 19.3.
+    const bool few = tiles >= kLongTiles * (kSlots<D> / groups) ? kSlots<D> / groups > 1 : kFewSlots / groups > 1;
+    const bool ragged = a.B > 1 && groups <= kSlots<D> && a.M >= 2L * a.N;
+    if (tiles >= 8 && (few || ragged)) {
+        // Workgroups for every chunk that the device may make: row blocks that are not cut, and parts.
+        const long heads = (long)a.Hkv * blocks, most = heads * ((a.M / kKeys + a.B) / kMinTiles + 1 + a.B);
+        const int grid = (int)min(groups + kSlots<D>, most), spread = (int)((a.B > 1 ? 2 : 1) * kSlots<D> / groups) + 1;
+        prompt_kernel<D, KT, true><<<(unsigned)grid, kThreads, 0, stream>>>(a, blocks, parts);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        join_prompt_kernel<D><<<(unsigned)join_groups, join_waves(chunks) * kWave, 0, stream>>>(a, blocks, chunks, parts);
+        join_prompt_kernel<D><<<(unsigned)(groups * kWaves * (D / 8)), join_waves(spread) * kWave, 0, stream>>>(a, blocks, parts);
         return hipGetLastError();
     }
-    prompt_kernel<D, KT, false><<<(unsigned)groups, kThreads, 0, stream>>>(a, blocks, 1, parts);
+    prompt_kernel<D, KT, false><<<(unsigned)groups, kThreads, 0, stream>>>(a, blocks, parts);
     return hipGetLastError();
 }
 
@@ -475,7 +591,7 @@ hipError_t launch(const GroupedPromptArgs &a, void *workspace, hipStream_t strea
 
 size_t grouped_prompt_workspace(int D)
 {
-    return (size_t)(D == 64 ? kSlots<64> : kSlots<128>) * kRows * (sizeof(float2) + D * sizeof(float));
+    return (size_t)(D == 64 ? kSlots<64> : kSlots<128>) * (kRows * (sizeof(float2) + D * sizeof(float)) + sizeof(int2));
 }
 
 hipError_t launch_grouped_prompt(const GroupedPromptArgs &a, int D, void *workspace, hipStream_t stream)

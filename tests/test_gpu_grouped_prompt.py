@@ -105,6 +105,22 @@ def test_many_sequences(D):
 
 
 @pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B,H,Hkv", [(5, 16, 2), (64, 2, 1), (65, 2, 2), (100, 1, 1), (300, 4, 2)])
+def test_few_long_ones_among_short(B, H, Hkv, D):
+    """Sequences of a few queries, of which some have long keys behind, some nothing: cut by what the device finds."""
+    rng = np.random.default_rng(B)
+    nq = [int(n) for n in rng.integers(0, 4, B)]
+    nk = [n + int(rng.choice([0, rng.integers(0, 300), 6000 if rng.random() < 0.3 else 900])) for n in nq]
+    nq[0], nk[0], nk[B // 2], nk[-1] = 40, 9041, 0, nq[-1] + 7777
+    c = case(nq, nk, H, Hkv, D, seed=B)
+    o, lse = run(c)
+    last = [(b, n - 1, H - 1) for b, n in enumerate(nq) if n][-30:]
+    check(c, o, lse, some_rows(c, rng, most=60) + last)
+    again, N = run(c), sum(nq)  # rows behind are left as they were
+    assert torch.equal(o[:N], again[0][:N]) and torch.equal(lse[:N], again[1][:N])
+
+
+@pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("what", ["peaked", "large", "zero", "negative", "tiny"])
 def test_scores(what, D):
     """Scores that a few keys win, that are far from zero and grow along the keys, and scales that are not positive."""
