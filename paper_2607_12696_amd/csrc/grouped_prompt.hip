@@ -17,7 +17,7 @@
 //   matrix cores are busy 60% of the cycles and the vector unit issues in half of them, at 1.8 GHz, which the power leaves
 //   (operands of zeros run at 2.2); six prompts of 563 to 1201 tokens, 64 heads on 8 of 64, 84 us: the vector unit (five
 //   instructions a weight, half the products of a head of 128 to hide them), and wavefronts that end unevenly; 7 tokens over
-//   4008 keys, 64 heads on 4 of 128, 13 us and 4.1 of the join: a chain of offsets, cuts, queries, first tile, six tiles at 1.2 us
+//   4008 keys, 64 heads on 4 of 128, 14 us and 4.0 of the join: a chain of offsets, cuts, queries, first tile, six tiles at 1.2 us
 //   (a lone wavefront's latency), parts; loads two and three steps ahead, or two and four tiles a step, did not shorten it.
 //   With two wavefronts a SIMD, each with three tiles under way at once and a piece of the exponentials behind each product
 //   (176 and 248 registers), the first two took 575 and 100 us; with 64 rows a wavefront, one a SIMD, half the LDS reads,
@@ -469,10 +469,10 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void prompt_kernel(Group
 // Adds up the chunks of a row block: a workgroup has 32 rows by 8 elements, what registers 4 i .. 4 i + 3 of one element tile
 // of the accumulators hold; its wavefronts, one for each four chunks and at most eight, take chunks in turn, four together, in
 // one pass with a running reference maximum.  What bounds it: latency (offsets, one read for 32 chunks, barrier).  7 tokens over
-// 4008 keys, 31 chunks, 8 MB: 4.1 us (with the references read first, behind a barrier of their own, 6.4).  The whole call for 3
-// tokens over 30003 keys, 8 heads on one, 234 chunks: 17.1 us (by four wavefronts 20.4; eight chunks together, or 16 wavefronts,
-// are no better here and 5 us worse for 50 tokens over 20050 keys, 64 heads on 4, where 52); for 29 prompts of up to 364 tokens,
-// two heads, two chunks at most, 26.6 (by eight wavefronts always 41.5).
+// 4008 keys, 21 chunks, 5.5 MB: 4.0 us (31 chunks 4.1, with the references read first, behind a barrier of their own, 6.4).
+// The whole call for 3 tokens over 30003 keys, 8 heads on one, 234 chunks, takes 17 us (by four wavefronts 3 more; eight chunks
+// together, or 16 wavefronts, are no better here and 5 us worse for 50 tokens over 20050 keys, 64 heads on 4).  Eight wavefronts
+// where two chunks are joined cost 15 us of 42, for 29 prompts of up to 364 tokens, two heads.
 template <int D>
 __global__ __launch_bounds__(kJoinWaves *kWave) void join_prompt_kernel(GroupedPromptArgs a, int blocks, PromptParts parts)
 {

@@ -22,7 +22,7 @@
 // elements come first); for a larger one the lists in pairs.
 // What bounds it: memory, for many rows (2048 of 200000 in bf16, k = 5: 157 us,
 // 5.2 TB/s; k = 20 168, k = 64 234); for few the chain of load, bound, list, join
-// and the launches (4 of 128000, k = 2: 5 us, and 3.7 the join; one of 32000, k =
+// and the launches (4 of 128000, k = 2: 5 us, and 3.1 the join; one of 32000, k =
 // 5, 20 and 64: 8, 11.4 and 24).  Rising logits, of which every tile passes whole,
 // take four times as long as others.
 #include "device.hpp"
