@@ -23,8 +23,8 @@
 // What bounds it: memory, for many rows (2048 of 200000 in bf16, k = 5: 157 us,
 // 5.2 TB/s; k = 20 168, k = 64 234); for few the chain of load, bound, list, join
 // and the launches (4 of 128000, k = 2: 5 us, and 3.1 the join; one of 32000, k =
-// 5, 20 and 64: 8, 11.4 and 24).  Rising logits, of which every tile passes whole,
-// take four times as long as others.
+// 5, 20 and 64: 8, 11.4 and 24).  Rising logits, of which every tile passes, take
+// six times as long as others (512 of 200000, k = 5: 300 and 51 us).
 #include "device.hpp"
 #include "step.hpp"
 
@@ -288,8 +288,9 @@ struct Best {
         if (lane_id() >= count && lane_id() < k) to[lane_id()] = 0;
     }
 
-    // A tile of E elements a lane, of higher index than all before; top: the lane's largest, group[g]: of the g-th kGroup.
-    template <int E, int G, class F>
+    // A tile of E elements a lane, of higher index than all before, by vectors of VEC of which all lanes' come before all lanes' next;
+    // top: the lane's largest, group[g]: of the g-th kGroup.
+    template <int VEC, int E, int G, class F>
     __device__ __forceinline__ void tile(const float (&v)[E], float top, const float (&group)[G], F index_of)
     {
         const uint64_t pass = __ballot(top > bound);
@@ -320,7 +321,9 @@ struct Best {
             for (int e = g * kGroup; e < min(E, (g + 1) * kGroup); ++e) {
                 if (e % (kRoom / kWave) == 0 && count > longest) {
                     cut();
-                    from = fmaxf(from, bound);  // equal ones of this tile may have a lower index than what is listed
+                    // What comes behind whole vectors of all lanes is of higher index than what is listed; within them an equal
+                    // one's may be lower.  (512 rows of 200000 equal logits: 66 us, always taken as lower 150.)
+                    from = fmaxf(from, e % VEC ? bound : above(bound));
                 }
                 const bool in = v[e] >= from;
                 const uint64_t mask = __ballot(in);
@@ -370,7 +373,7 @@ __device__ __forceinline__ void scan(const LogprobArgs &a, int row, int part, in
             if (v[0] > sums.m) sums.move(v[0], c);
             sums.add(v, c);
         }
-        if (TOP) best.tile(v, v[0], v, [&](int) { return from + lane; });
+        if (TOP) best.tile<1>(v, v[0], v, [&](int) { return from + lane; });
     };
     if (part == 0 && head) edge(0, head);
     const u32x4 *src = reinterpret_cast<const u32x4 *>(p + (long)head * kBytes);
@@ -401,7 +404,7 @@ __device__ __forceinline__ void scan(const LogprobArgs &a, int row, int part, in
         if (top > sums.m) sums.move(top, c);
         sums.add(v, c);
         if (TOP)
-            best.tile(v, top, group, [&](int e) { return head + (at + e / kVec * kWave) * kVec + e % kVec; });
+            best.tile<kVec>(v, top, group, [&](int e) { return head + (at + e / kVec * kWave) * kVec + e % kVec; });
     }
     if (part == parts - 1 && tail < a.V) edge(tail, a.V);
 
