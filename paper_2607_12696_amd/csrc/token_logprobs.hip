@@ -273,7 +273,8 @@ struct Best {
         int rank = has ? 0 : kWave;
 #pragma unroll 4
         for (int i = 0; i < count; ++i) {
-            const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(mine >> 32), i), lo = __builtin_amdgcn_readlane((uint32_t)mine, i);
+            const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(mine >> 32), i);
+            const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)mine, i);
             rank += ((uint64_t)hi << 32 | lo) > mine;
         }
         return rank;
@@ -288,8 +289,8 @@ struct Best {
         if (lane_id() >= count && lane_id() < k) to[lane_id()] = 0;
     }
 
-    // A tile of E elements a lane, of higher index than all before, by vectors of VEC of which all lanes' come before all lanes' next;
-    // top: the lane's largest, group[g]: of the g-th kGroup.
+    // A tile of E elements a lane, of higher index than all before, by vectors of VEC of which all lanes' come before all lanes'
+    // next; top: the lane's largest, group[g]: of the g-th kGroup.
     template <int VEC, int E, int G, class F>
     __device__ __forceinline__ void tile(const float (&v)[E], float top, const float (&group)[G], F index_of)
     {
@@ -453,7 +454,8 @@ __device__ __forceinline__ const uint64_t *join_lists(uint64_t *from, uint64_t *
 // A row's results from its parts (head: the lane's part's), by a whole workgroup.  Lists in LDS, one after the other, and room
 // for half of them.
 template <bool BF16>
-__device__ __forceinline__ void finish(const LogprobArgs &a, int row, int parts, const Head &head, uint64_t *lists, uint64_t *spare)
+__device__ __forceinline__ void finish(const LogprobArgs &a, int row, int parts, const Head &head, uint64_t *lists,
+                                       uint64_t *spare)
 {
     constexpr int kBytes = BF16 ? 2 : 4;
     const int lane = lane_id(), wave = threadIdx.x / kWave;
