@@ -13,15 +13,15 @@
 //   wavefronts of its SIMD, of other workgroups, so registers are kept for four of them with heads of 64 and three with 128.
 //   Where there are few row blocks, or sequences of keys far more than queries, each block's keys are cut into chunks, a
 //   workgroup each, whose sums join_prompt_kernel adds up in order.
-//   Measured: one prompt of 6007 tokens, 64 heads on 4 of 128, 524 to 538 us, up to 1.13 PFLOP/s (a bf16 product of 8192^3: 1.415): the
-//   matrix cores are busy 60% of the cycles and the vector unit issues in half of them, at 1.8 GHz, which the power leaves
-//   (operands of zeros run at 2.2); six prompts of 563 to 1201 tokens, 64 heads on 8 of 64, 84 us: the vector unit (five
-//   instructions a weight, half the products of a head of 128 to hide them), and wavefronts that end unevenly; 7 tokens over
-//   4008 keys, 64 heads on 4 of 128, 14 us and 4.0 of the join: a chain of offsets, cuts, queries, first tile, six tiles at 1.2 us
-//   (a lone wavefront's latency), parts; loads two and three steps ahead, or two and four tiles a step, did not shorten it.
-//   With two wavefronts a SIMD, each with three tiles under way at once and a piece of the exponentials behind each product
-//   (176 and 248 registers), the first two took 575 and 100 us; with 64 rows a wavefront, one a SIMD, half the LDS reads,
-//   580 and 143: one wavefront issues an instruction every seven cycles at best.
+//   Measured: one prompt of 6007 tokens, 64 heads on 4 of 128, 524 to 538 us, up to 1.13 PFLOP/s (a bf16 product of 8192^3:
+//   1.415): the matrix cores are busy 60% of the cycles and the vector unit issues in half of them, at 1.8 GHz, which the
+//   power leaves (operands of zeros run at 2.2); six prompts of 706 to 1201 tokens, 64 heads on 8 of 64, 84 us: the vector
+//   unit (five instructions a weight, half the products of a head of 128 to hide them), and wavefronts that end unevenly; 7
+//   tokens over 4008 keys, 64 heads on 4 of 128, 14 us and 4.0 of the join: a chain of offsets, cuts, queries, first tile,
+//   six tiles at 1.2 us (a lone wavefront's latency), parts; loads two and three steps ahead, or two and four tiles a step,
+//   did not shorten it. With two wavefronts a SIMD, each with three tiles under way at once and a piece of the exponentials
+//   behind each product (176 and 248 registers), the first two took 575 and 100 us; with 64 rows a wavefront, one a SIMD,
+//   half the LDS reads, 580 and 143: one wavefront issues an instruction every seven cycles at best.
 #include "attn_plan.hpp"
 #include "step.hpp"
 
