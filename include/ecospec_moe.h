@@ -554,6 +554,18 @@ moe_status_t moe_cache_append(const moe_cache_t *cache, const void *k_new, const
                               void *stream);
 
 /*
+ * The same behind a moe_pages_update: entry i goes to row slots[i] of the
+ * pages, and cache_len and block_table are not read.  A sequence whose first
+ * slot lies outside [0, n_pages * page) gets nothing, as one that the update
+ * refused; where it kept fewer tokens than it had, the new ones follow those.
+ * slots [N] int64, 8-byte aligned: a sequence's slots on one page follow each
+ * other, and the first on each of its further pages is that page's first row.
+ */
+moe_status_t moe_cache_append_slots(const moe_cache_t *cache, const void *k_new, const void *v_new, int n_rows,
+                                    const int32_t *rows, int N, int B, const int32_t *token_offsets, int max_tokens,
+                                    const int64_t *slots, void *stream);
+
+/*
  * Grouped-query attention of draft tokens over the 8-bit cache and the drafts
  * themselves.  Query head h uses key/value head h / (H / Hkv).
  *   s_j = scale * q[t][h] . k_j,  o[t][h] = sum_j softmax(s)_j v_j,
@@ -622,9 +634,13 @@ typedef struct {
  *   array of n_pages * page rows.  Both are -1 for tokens of a refused
  *   sequence and for entries from token_offsets[B] on.  Each may be NULL.
  * new_len and n_free_out are buffers of their own (not cache_len, keep_len or
- * n_free): the update reads the old counts throughout, and so do the calls that
- * append the new tokens.  The same call again, on the same counts, gives the
- * same results.  1 <= N <= 2^30.  One kernel, deterministic.
+ * n_free): the update reads the old counts throughout.  The same call again, on
+ * the same counts, gives the same results; so an update whose new counts are not
+ * taken over has changed nothing.  The new tokens go where slots says
+ * (moe_latent_append, moe_cache_append_slots).  moe_cache_append would put
+ * them behind cache_len[b]: not where fewer are kept, and for a refused sequence
+ * into pages that are not its own.
+ *   1 <= N <= 2^30.  One kernel, deterministic.
  */
 moe_status_t moe_pages_update(const moe_page_pool_t *pool, const int32_t *keep_len, const int32_t *token_offsets, int N,
                               int32_t *new_len, int32_t *n_free_out, int32_t *refused, int64_t *slots,

@@ -60,7 +60,7 @@ EXPORTED = ("moe_route_topk", "moe_route_union", "moe_route_topk_grouped", "moe_
             "moe_verify_layer_timed", "moe_packed_size", "moe_pack_weights", "moe_pack_gate_up", "moe_pack_down",
             "moe_select_tree", "moe_status_string", "moe_last_error", "moe_verify_layer_noalloc",
             "moe_add_rmsnorm", "moe_latent_attn_workspace_size", "moe_latent_attn", "moe_latent_prompt",
-            "moe_cache_append", "moe_cache_attn_workspace_size", "moe_cache_attn",
+            "moe_cache_append", "moe_cache_append_slots", "moe_cache_attn_workspace_size", "moe_cache_attn",
             "moe_pages_update", "moe_latent_append", "moe_grouped_prompt_workspace_size", "moe_grouped_prompt",
             "moe_token_logprobs_workspace_size", "moe_token_logprobs")
 
@@ -154,6 +154,7 @@ def lib() -> C.CDLL:
                                           C.c_size_t, p]
             L.moe_latent_prompt.argtypes = [st(moe_prompt_t), p, p, p]
             L.moe_cache_append.argtypes = [st(moe_cache_t), p, p, i, p, i, i, p, i, p]
+            L.moe_cache_append_slots.argtypes = [st(moe_cache_t), p, p, i, p, i, i, p, i, p, p]
             L.moe_cache_attn_workspace_size.argtypes = [st(moe_cache_t), i, i, i, st(C.c_size_t)]
             L.moe_cache_attn.argtypes = [st(moe_cache_t), st(moe_drafts_t), p, p, p, i, C.c_float, p, p, p, C.c_size_t, p]
             L.moe_pages_update.argtypes = [st(moe_page_pool_t), p, p, i, p, p, p, p, p, p]
@@ -168,8 +169,8 @@ def lib() -> C.CDLL:
             for f in ("moe_route_topk", "moe_route_union", "moe_route_topk_grouped", "moe_router_workspace_size", "moe_route_topk_hidden", "moe_expert_union", "moe_verify_workspace_size", "moe_verify_layer",
                       "moe_verify_layer_noalloc", "moe_verify_layer_timed", "moe_packed_size", "moe_pack_weights", "moe_pack_gate_up",
                       "moe_pack_down", "moe_select_tree", "moe_add_rmsnorm", "moe_latent_attn_workspace_size",
-                      "moe_latent_attn", "moe_latent_prompt", "moe_cache_append", "moe_cache_attn_workspace_size",
-                      "moe_cache_attn", "moe_pages_update", "moe_latent_append", "moe_grouped_prompt_workspace_size",
+                      "moe_latent_attn", "moe_latent_prompt", "moe_cache_append", "moe_cache_append_slots",
+                      "moe_cache_attn_workspace_size", "moe_cache_attn", "moe_pages_update", "moe_latent_append", "moe_grouped_prompt_workspace_size",
                       "moe_grouped_prompt", "moe_token_logprobs_workspace_size", "moe_token_logprobs"):
                 getattr(L, f).restype = i
             _lib = L
@@ -727,19 +728,25 @@ def _cache(k, v, k_scale, v_scale, block_table, cache_len, B: int) -> moe_cache_
 
 
 def moe_cache_append(k_new, v_new, token_offsets, k, v, k_scale, v_scale, block_table, cache_len, rows=None,
-                     max_tokens: int | None = None) -> None:
+                     max_tokens: int | None = None, slots=None) -> None:
     """New tokens into the 8-bit cache, in place: sequence b's, entries token_offsets[b] .. token_offsets[b + 1] - 1 of
     `rows` (indices into k_new, v_new [n_rows, Hkv, D] bf16; None: the entries themselves), at positions cache_len[b] on.
     k [n_pages, Hkv, page, D] and v [n_pages, Hkv, D, page] uint8 codes, k_scale, v_scale [n_pages, Hkv] fp32.
-    cache_len is not changed.  max_tokens: at least the most new tokens of a sequence (None: all)."""
+    cache_len is not changed.  max_tokens: at least the most new tokens of a sequence (None: all).
+    slots: int64 [N] of a moe_pages_update, for which the entries go there instead and cache_len is not read: a refused
+    sequence gets nothing, and what follows fewer kept tokens than cached ones follows those."""
     B = token_offsets.shape[0] - 1
     c = _cache(k, v, k_scale, v_scale, block_table, cache_len, B)
     n_rows = k_new.shape[0]
     N = n_rows if rows is None else rows.shape[0]
-    _check("moe_cache_append", lib().moe_cache_append(
-        C.byref(c), _bf16_ptr(k_new, "k_new", n_rows, c.Hkv, c.D), _bf16_ptr(v_new, "v_new", n_rows, c.Hkv, c.D), n_rows,
-        None if rows is None else _int32_ptr(rows, "rows", N), N, B, _int32_ptr(token_offsets, "token_offsets", B + 1),
-        N if max_tokens is None else max_tokens, _stream(k_new)))
+    args = (C.byref(c), _bf16_ptr(k_new, "k_new", n_rows, c.Hkv, c.D), _bf16_ptr(v_new, "v_new", n_rows, c.Hkv, c.D), n_rows,
+            None if rows is None else _int32_ptr(rows, "rows", N), N, B, _int32_ptr(token_offsets, "token_offsets", B + 1),
+            N if max_tokens is None else max_tokens)
+    if slots is None:
+        _check("moe_cache_append", lib().moe_cache_append(*args, _stream(k_new)))
+    else:
+        slots = _typed_ptr(slots, _torch().int64, "slots", (N,))
+        _check("moe_cache_append_slots", lib().moe_cache_append_slots(*args, slots, _stream(k_new)))
 
 
 def moe_cache_attn_workspace_size(k, v, k_scale, v_scale, block_table, cache_len, N: int, H: int) -> int:

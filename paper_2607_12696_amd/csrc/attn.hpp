@@ -46,6 +46,7 @@ struct AppendArgs {
     int Hkv, D, n_pages, page, max_blocks;
     const uint16_t *k_new, *v_new;
     const int32_t *rows, *token_offsets, *block_table, *cache_len;
+    const int64_t *slots;  // or null: places follow from block_table and cache_len
     uint8_t *k, *v;
     float *k_scale, *v_scale;
 };

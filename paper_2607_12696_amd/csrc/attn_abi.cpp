@@ -75,6 +75,41 @@ void set_paged(ecospec::PagedArgs &a, const moe_drafts_t *d, int H, float scale,
     a.lse = lse;
 }
 
+// slots: null where places follow from block_table and cache_len.
+moe_status_t append(const moe_cache_t *cache, const void *k_new, const void *v_new, int n_rows, const int32_t *rows, int N, int B,
+                    const int32_t *token_offsets, int max_tokens, const int64_t *slots, void *stream)
+{
+    const moe_status_t st = check_cache(cache);
+    if (st != MOE_OK) return st;
+    if (!k_new || !v_new || !token_offsets || N < 1 || n_rows < 1 || B < 1 || B > kMaxBatch || max_tokens < 1)
+        return MOE_ERR_INVALID_ARG;
+    if (!rows && n_rows < N) return MOE_ERR_INVALID_ARG;
+    if (!aligned(k_new, 16) || !aligned(v_new, 16)) return MOE_ERR_INVALID_ARG;
+    ecospec::AppendArgs a{};
+    a.N = N;
+    a.B = B;
+    a.n_rows = n_rows;
+    a.max_tokens = max_tokens < N ? max_tokens : N;
+    a.Hkv = cache->Hkv;
+    a.D = cache->D;
+    a.n_pages = cache->n_pages;
+    a.page = cache->page;
+    a.max_blocks = cache->max_blocks;
+    a.k_new = static_cast<const uint16_t *>(k_new);
+    a.v_new = static_cast<const uint16_t *>(v_new);
+    a.rows = rows;
+    a.token_offsets = token_offsets;
+    a.slots = slots;
+    a.block_table = cache->block_table;
+    a.cache_len = cache->cache_len;
+    a.k = cache->k;
+    a.v = cache->v;
+    a.k_scale = cache->k_scale;
+    a.v_scale = cache->v_scale;
+    if (!ecospec::cache_append_fits(a)) return MOE_ERR_UNSUPPORTED;
+    return from_hip(ecospec::launch_cache_append(a, (hipStream_t)stream));
+}
+
 }  // namespace
 
 extern "C" {
@@ -178,34 +213,15 @@ moe_status_t moe_cache_append(const moe_cache_t *cache, const void *k_new, const
                               const int32_t *rows, int N, int B, const int32_t *token_offsets, int max_tokens,
                               void *stream)
 {
-    const moe_status_t st = check_cache(cache);
-    if (st != MOE_OK) return st;
-    if (!k_new || !v_new || !token_offsets || N < 1 || n_rows < 1 || B < 1 || B > kMaxBatch || max_tokens < 1)
-        return MOE_ERR_INVALID_ARG;
-    if (!rows && n_rows < N) return MOE_ERR_INVALID_ARG;
-    if (!aligned(k_new, 16) || !aligned(v_new, 16)) return MOE_ERR_INVALID_ARG;
-    ecospec::AppendArgs a{};
-    a.N = N;
-    a.B = B;
-    a.n_rows = n_rows;
-    a.max_tokens = max_tokens < N ? max_tokens : N;
-    a.Hkv = cache->Hkv;
-    a.D = cache->D;
-    a.n_pages = cache->n_pages;
-    a.page = cache->page;
-    a.max_blocks = cache->max_blocks;
-    a.k_new = static_cast<const uint16_t *>(k_new);
-    a.v_new = static_cast<const uint16_t *>(v_new);
-    a.rows = rows;
-    a.token_offsets = token_offsets;
-    a.block_table = cache->block_table;
-    a.cache_len = cache->cache_len;
-    a.k = cache->k;
-    a.v = cache->v;
-    a.k_scale = cache->k_scale;
-    a.v_scale = cache->v_scale;
-    if (!ecospec::cache_append_fits(a)) return MOE_ERR_UNSUPPORTED;
-    return from_hip(ecospec::launch_cache_append(a, (hipStream_t)stream));
+    return append(cache, k_new, v_new, n_rows, rows, N, B, token_offsets, max_tokens, nullptr, stream);
+}
+
+moe_status_t moe_cache_append_slots(const moe_cache_t *cache, const void *k_new, const void *v_new, int n_rows,
+                                    const int32_t *rows, int N, int B, const int32_t *token_offsets, int max_tokens,
+                                    const int64_t *slots, void *stream)
+{
+    if (!slots || !aligned(slots, 8)) return MOE_ERR_INVALID_ARG;
+    return append(cache, k_new, v_new, n_rows, rows, N, B, token_offsets, max_tokens, slots, stream);
 }
 
 moe_status_t moe_cache_attn_workspace_size(const moe_cache_t *cache, int N, int B, int H, size_t *bytes)
