@@ -52,8 +52,11 @@ class Pages:
 
     def grow(self, off, n, keep=None):
         """Pages for n new tokens (sequence b's are off[b] .. off[b + 1] - 1): their slots and positions.  The old lengths
-        hold until `settle`."""
-        return moe.moe_pages_update(self.len, off, self.table, self.free, self.n_free, self.page, n, keep_len=keep)
+        hold until `settle`, so where some sequence's tokens do not fit nothing has changed for any."""
+        update = moe.moe_pages_update(self.len, off, self.table, self.free, self.n_free, self.page, n, keep_len=keep)
+        if refused := update.refused.item():
+            raise RuntimeError(f"there are no pages for the new tokens of {refused} sequences")
+        return update
 
     def settle(self, update):
         self.len, self.n_free = update.new_len, update.n_free
@@ -129,7 +132,7 @@ class GroupedAttention:
         return o.flatten(1) @ self.w_o
 
     def append(self, new, off, rows, slots):
-        moe.moe_cache_append(*new, off, self.k, self.v, self.ks, self.vs, self.pages.table, self.pages.len, rows=rows)
+        moe.moe_cache_append(*new, off, self.k, self.v, self.ks, self.vs, self.pages.table, self.pages.len, rows=rows, slots=slots)
 
 
 class Model:
@@ -232,8 +235,9 @@ class Model:
             rows += [base[b] + i for i in path]
             counts.append(len(path))
             out.append([toks[i] for i in path[1:]] + [best[base[b] + at]])
-            self.scores[b] += [scores[base[b] + i] for i in path]
         self.append(kept, torch.tensor(rows, dtype=torch.int32, device=self.dev), counts)
+        for mine, at, n in zip(self.scores, self.offsets(counts).tolist(), counts):
+            mine += [scores[i] for i in rows[at:at + n]]
         return out
 
 
