@@ -464,7 +464,8 @@ __device__ __forceinline__ void finish(const LogprobArgs &a, int row, int parts,
     Sums sums{head.m, head.a, head.s};
     sums.join_lanes(c);
     const bool nothing = sums.s == 0.;  // every logit is -inf
-    const float log_s = (float)log(sums.s);
+    // The sums know differences from the largest logit alone: where that one, scaled, is past fp32's range, it is said here.
+    const float log_s = sums.m * a.scale == INFINITY ? __uint_as_float(0x7fc00000u) : (float)log(sums.s);
     if (threadIdx.x == 0) {
         if (a.lse) a.lse[row] = nothing ? -INFINITY : fmaf(sums.m, a.scale, log_s);
         if (a.entropy) a.entropy[row] = nothing ? 0.f : fmaf(-kLn2, sums.a / (float)sums.s, log_s);
