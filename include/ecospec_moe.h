@@ -726,7 +726,8 @@ typedef enum {
  * Arithmetic: exponentials in fp32, relative to the largest logits so far, their
  * sum in fp64; the logits are read once.  Deterministic.
  * Limits: 1 <= N <= 2^22, 1 <= V <= 2^24, 0 <= k <= min(V, 64), 0 <= M <= 65536,
- * N * M <= 2^30, scale finite and > 0.  One or two kernels.
+ * N * M <= 2^30, scale finite and > 0, at most 2^126 (else
+ * MOE_ERR_UNSUPPORTED).  One or two kernels.
  */
 moe_status_t moe_token_logprobs_workspace_size(int N, size_t *bytes);
 moe_status_t moe_token_logprobs(const void *logits, int dtype, int64_t stride, int N, int V, float scale,

@@ -74,6 +74,7 @@ constexpr int kMaxHeads = 1024;
 constexpr long kMaxPromptRows = 1L << 30;  // query rows (token, head)
 constexpr int64_t kMaxStride = 1L << 23;   // elements between a prompt's keys: a tile is addressed in 32 bits
 constexpr int kMaxLogitRows = 1 << 22, kMaxVocabulary = 1 << 24, kMaxGiven = 1 << 16, kMaxTop = 64;
+constexpr float kMaxScale = 0x1p126f;  // of logits: twice its product with log2 e is a number
 
 }  // namespace
 
@@ -222,6 +223,7 @@ moe_status_t moe_token_logprobs(const void *logits, int dtype, int64_t stride, i
     if ((k == 0) != (top_idx == nullptr) || (k == 0 && top_logprob)) return MOE_ERR_INVALID_ARG;
     if (!logprob && !lse && !entropy && !top_idx) return MOE_ERR_INVALID_ARG;
     if (!aligned(logits, dtype == MOE_BF16 ? 2 : 4) || !aligned(workspace, 256)) return MOE_ERR_INVALID_ARG;
+    if (scale > kMaxScale) return MOE_ERR_UNSUPPORTED;
     if (workspace_bytes < ecospec::logprobs_workspace(N)) return MOE_ERR_WORKSPACE;
     const size_t n = N;
     const Range out[] = {{logprob, n * M * 4}, {lse, n * 4}, {entropy, n * 4}, {top_idx, n * k * 4}, {top_logprob, n * k * 4},

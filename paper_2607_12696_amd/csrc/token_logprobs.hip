@@ -138,6 +138,10 @@ __device__ __forceinline__ T last_lane(T v)
     }
 }
 
+// (l - m) c.  The difference may pass fp32's range where its product does not, so it is taken of the halves, which are exact:
+// one fma, and the factor of two is in c's.
+__device__ __forceinline__ float scaled_difference(float l, float m, float c) { return fmaf(l, 0.5f, -0.5f * m) * (2.f * c); }
+
 // S is held in 64 bits: where one token has almost all of the probability, S is 1 and a little, and ln S, the token's log
 // probability and most of the entropy are that little.
 struct Sums {
@@ -146,7 +150,7 @@ struct Sums {
 
     __device__ __forceinline__ void move(float to, float c)  // to >= m
     {
-        const float d = fmaxf((m - to) * c, kFloor), f = __builtin_amdgcn_exp2f(d);
+        const float d = fmaxf(scaled_difference(m, to, c), kFloor), f = __builtin_amdgcn_exp2f(d);
         a = fmaf(d, (float)s, a) * f;
         s *= f;
         m = to;
@@ -169,7 +173,7 @@ struct Sums {
             u[0] = u[1] = 0.f;
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                const float x = (l[i] - m) * c, e = __builtin_amdgcn_exp2f(x);
+                const float x = scaled_difference(l[i], m, c), e = __builtin_amdgcn_exp2f(x);
                 t[i % 2] += e;
                 u[i % 2] = fmaf(e, floor == 0.f ? x : fmaxf(x, floor), u[i % 2]);
             }
@@ -470,7 +474,7 @@ __device__ __forceinline__ void finish(const LogprobArgs &a, int row, int parts,
         if (a.lse) a.lse[row] = nothing ? -INFINITY : fmaf(sums.m, a.scale, log_s);
         if (a.entropy) a.entropy[row] = nothing ? 0.f : fmaf(-kLn2, sums.a / (float)sums.s, log_s);
     }
-    auto logprob = [&](float l) { return nothing ? -INFINITY : fmaf(l - sums.m, a.scale, -log_s); };
+    auto logprob = [&](float l) { return nothing ? -INFINITY : fmaf(fmaf(l, 0.5f, -0.5f * sums.m), 2.f * a.scale, -log_s); };
     for (int i = threadIdx.x; i < a.M; i += blockDim.x) {
         const int t = a.tokens[(long)row * a.M + i];
         a.logprob[(long)row * a.M + i] = t >= 0 && t < a.V ? logprob(logit<BF16>(p, t)) : -INFINITY;
