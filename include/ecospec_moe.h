@@ -721,8 +721,8 @@ typedef enum {
  *   entropy [N], each or NULL, top_idx [N][k], top_logprob [N][k] (top_idx NULL
  *   exactly when k is 0; top_logprob may be NULL).
  *   workspace: device scratch of moe_token_logprobs_workspace_size bytes,
- *   256-byte aligned; its contents on entry do not matter.  The size for N rows
- *   is enough for every call of no more rows.
+ *   256-byte aligned; its contents on entry do not matter.  The size is 2.2 MB
+ *   for any number of rows.
  * Arithmetic: exponentials in fp32, relative to the largest logits so far, their
  * sum in fp64; the logits are read once.  Deterministic.
  * Limits: 1 <= N <= 2^22, 1 <= V <= 2^24, 0 <= k <= min(V, 64), 0 <= M <= 65536,

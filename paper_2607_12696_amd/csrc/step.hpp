@@ -54,7 +54,7 @@ struct LogprobArgs {
     float *logprob, *lse, *entropy, *top_logprob;  // each or null
     int32_t *top_idx;
 };
-size_t logprobs_workspace(int N);
+size_t logprobs_workspace();
 hipError_t launch_token_logprobs(const LogprobArgs &a, bool bf16, void *workspace, hipStream_t stream);
 
 }  // namespace ecospec

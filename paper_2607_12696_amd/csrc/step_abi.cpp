@@ -205,7 +205,7 @@ moe_status_t moe_grouped_prompt(const moe_grouped_prompt_t *p, void *o, float *l
 moe_status_t moe_token_logprobs_workspace_size(int N, size_t *bytes)
 {
     if (!bytes || N < 1 || N > kMaxLogitRows) return MOE_ERR_INVALID_ARG;
-    *bytes = ecospec::logprobs_workspace(N);
+    *bytes = ecospec::logprobs_workspace();
     return MOE_OK;
 }
 
@@ -224,10 +224,10 @@ moe_status_t moe_token_logprobs(const void *logits, int dtype, int64_t stride, i
     if (!logprob && !lse && !entropy && !top_idx) return MOE_ERR_INVALID_ARG;
     if (!aligned(logits, dtype == MOE_BF16 ? 2 : 4) || !aligned(workspace, 256)) return MOE_ERR_INVALID_ARG;
     if (scale > kMaxScale) return MOE_ERR_UNSUPPORTED;
-    if (workspace_bytes < ecospec::logprobs_workspace(N)) return MOE_ERR_WORKSPACE;
+    if (workspace_bytes < ecospec::logprobs_workspace()) return MOE_ERR_WORKSPACE;
     const size_t n = N;
     const Range out[] = {{logprob, n * M * 4}, {lse, n * 4}, {entropy, n * 4}, {top_idx, n * k * 4}, {top_logprob, n * k * 4},
-                         {workspace, ecospec::logprobs_workspace(N)}};
+                         {workspace, ecospec::logprobs_workspace()}};
     const Range in[] = {{logits, ((n - 1) * (size_t)stride + V) * (dtype == MOE_BF16 ? 2 : 4)}, {tokens, n * M * 4}};
     if (any_overlap(out, in)) return MOE_ERR_INVALID_ARG;
     ecospec::LogprobArgs a{};

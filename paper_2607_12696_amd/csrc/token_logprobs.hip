@@ -603,10 +603,10 @@ hipError_t launch(const LogprobArgs &a, void *workspace, hipStream_t stream)
 
 }  // namespace
 
-size_t logprobs_workspace(int N)
+size_t logprobs_workspace()
 {
-    // At most kMinParts parts, of at least one a row.
-    return ((size_t)kMinParts + N) * (sizeof(Head) + kKept * sizeof(uint64_t));
+    // At most kMinParts parts, whatever the rows: in one launch there are none.
+    return (size_t)kMinParts * (sizeof(Head) + kKept * sizeof(uint64_t));
 }
 
 hipError_t launch_token_logprobs(const LogprobArgs &a, bool bf16, void *workspace, hipStream_t stream)
