@@ -56,7 +56,8 @@ class Row:
 def logprobs(row: np.ndarray, scale: float) -> Row:
     """Bounds, u = 2^-24: an exponent x = (l - m) scale log2 e has 4 roundings (difference, two in the constant, product), so a
     term 2^x is off by 4 u ln2 |x| and 2 u of the exponential itself; a moved reference adds the same again for the way that it
-    moves.  Sums run over at most n = V / 64 + 200 terms, joins and moves in a row, a rounding each.  The logarithm is off by
+    moves.  Sums run over at most n = V / 64 + 200 terms, joins and moves in a row, a rounding each (of an fp64 sum they are
+    less, which the tests of single elements bound for themselves).  The logarithm is off by
     4 u of itself, a result by one rounding."""
     row = np.asarray(row, np.float64)
     V = len(row)
