@@ -186,29 +186,31 @@ class Model:
         return r.top_idx[:, 0].tolist(), r.top_logprob[:, 0].tolist()
 
     def prompt(self, prompts):
-        """Whole prompts into the cache (an empty one leaves its sequence as it is) -> each one's next token.  Where some come
-        behind tokens that are cached, they go through the cached attention, 64 tokens at a time."""
+        """Whole prompts into the cache -> each one's next token; None for an empty one, which leaves its sequence as it is.
+        Where some come behind tokens that are cached, they go through the cached attention, 64 tokens at a time."""
+        if not any(prompts):
+            return [None] * len(prompts)
         if not any(n and p for n, p in zip(self.pages.len.tolist(), prompts)):
             last = self._piece(prompts, lambda a, q, n, off: a.prompt(q, n, off, max(map(len, prompts))))
         else:
             self.pages.grow(self.offsets([len(p) for p in prompts]), sum(map(len, prompts)))  # raises before the first piece does
-            last = [(0, None)] * len(prompts)
+            last = [None] * len(prompts)
             for at in range(0, max(map(len, prompts)), 64):
                 piece = self._piece([p[at:at + 64] for p in prompts], lambda a, q, n, off: a.drafts(q, n, off, None))
-                last = [new if len(p) > at else old for p, old, new in zip(prompts, last, piece)]
-        for mine, p, (_, score) in zip(self.scores, prompts, last):
-            mine += [score] if p else []
-        return [token for token, _ in last]
+                last = [new or old for old, new in zip(last, piece)]
+        for mine, new in zip(self.scores, last):
+            mine += [new[1]] if new else []
+        return [new and new[0] for new in last]
 
     def _piece(self, prompts, attend):
-        """These tokens into the cache -> each sequence's next one and its log probability."""
+        """These tokens into the cache -> each sequence's next one and its log probability, if it has any."""
         off, n = self.offsets([len(p) for p in prompts]), sum(map(len, prompts))
         update = self.pages.grow(off, n)
         tokens = torch.tensor([t for p in prompts for t in p], device=self.dev)
         logits, kept = self.forward(tokens, update.positions, lambda a, q, n: attend(a, q, n, off))
         self.store(kept, None, off, update)
         best, scores = self.best(logits)
-        return [(best[max(e - 1, 0)], scores[max(e - 1, 0)]) for e in off[1:].tolist()]
+        return [(best[e - 1], scores[e - 1]) if p else None for p, e in zip(prompts, off[1:].tolist())]
 
     def draft_tree(self, token, depth=3):
         """Tokens, parents and depths of a tree below `token`: two guesses a level by the embedding alone, the better one

@@ -79,3 +79,15 @@ def test_a_second_prompt_that_does_not_fit_leaves_everything(kind):
     assert model.pages.len.tolist() == lens and int(model.pages.n_free) == free and model.scores == scores
     model.prompt([text(110, 3), text(20, 4)])
     assert model.pages.len.tolist() == [160, 29]
+
+
+@pytest.mark.parametrize("kind", ["latent", "grouped"])
+def test_a_sequence_without_a_prompt_has_no_next_token(kind):
+    print(f"no prompt {kind}", flush=True)
+    model, _ = recorded(kind, B=3)
+    assert model.prompt([[], [], []]) == [None] * 3 and model.pages.len.tolist() == [0, 0, 0]
+    first = model.prompt([text(5, 1), [], text(3, 2)])
+    assert first[1] is None and all(isinstance(first[b], int) for b in (0, 2))
+    second = model.prompt([[], text(4, 3), text(90, 4)])  # one behind cached tokens
+    assert second[0] is None and all(isinstance(second[b], int) for b in (1, 2))
+    assert model.pages.len.tolist() == [5, 4, 93] and [len(s) for s in model.scores] == [1, 1, 2]
