@@ -674,10 +674,13 @@ moe_status_t moe_latent_append(void *pages, int n_pages, int page, int r, int p,
  *   of one projection's output may be passed as they lie.
  *   o [N][H][D] bf16; lse [N][H] fp32 or NULL.  Rows from q_offsets[B] on are
  *   left as they were.
- *   max_tokens: at least the most queries of a sequence.
+ *   max_tokens: at least the most queries of a sequence.  The launch has
+ *   workgroups for that many of each, and whether long keys are cut into chunks
+ *   follows from them: a number far above the most costs time.
  *   workspace: device scratch of moe_grouped_prompt_workspace_size bytes, 256-byte
  *   aligned; its contents on entry do not matter.  The size depends on D alone.
- * Arithmetic as for moe_latent_attn.  Deterministic.
+ * Arithmetic as for moe_latent_attn.  Deterministic: the same call gives the
+ * same bits; in another batch a sequence's keys may be summed in other chunks.
  * Limits: D 64 or 128 (else MOE_ERR_UNSUPPORTED); 1 <= Hkv <= 256, H % Hkv == 0,
  * H <= 1024, 1 <= B <= 1024, N, M >= 1, scale finite; strides >= 0 and multiples
  * of 8, 16-byte aligned pointers; k_stride, v_stride <= 2^23, N * H <= 2^30 and

@@ -850,7 +850,8 @@ def moe_grouped_prompt(q, k, v, q_offsets, kv_offsets, scale: float, max_tokens:
 
     q [N, H, D], k, v [M, Hkv, D] bf16 (strided views of a projection's output, contiguous along D); q_offsets, kv_offsets
     [B + 1] int32.  A sequence's queries are the last of its keys' tokens.  max_tokens: at least the most queries of a
-    sequence (None: N)."""
+    sequence.  None stands for N: right, but with several sequences most workgroups are then empty, long keys are not cut into
+    chunks, and B * H * N may pass the limit of 2^30."""
     torch = _torch()
     N, H = q.shape[:2]
     M, Hkv = k.shape[:2]
